@@ -10,6 +10,7 @@
  *                        hippo_*_attention_append, hippo_*_attention_paged and
  *                        hippo_*_attention_fp8kv with hippo_quantize_kv_e4m3 (cache-format variants),
  *                        hippo_spec_verify (the speculative-sampling verdict of Eq. 1),
+ *                        hippo_token_logprobs (log probabilities of an answer's words),
  *                        hippo_vpsd_* (host-side control of the parallel decoding rounds).
  *
  * Conventions common to every entry point
@@ -384,6 +385,28 @@ int hippo_spec_verify(const void* p_logits, const void* q_logits, int32_t dtype,
                       int32_t batch, int32_t gamma, int32_t vocab, float temperature,
                       int32_t* n_accept_out, int32_t* next_token_out, float* alpha_out,
                       void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Log probabilities of given words under rows of logits, with each row's entropy and its most likely words: what an answer's
+ * tokens were worth (for a verified chain, row i of hippo_spec_verify's p_logits judges token i).
+ *   y = logits[r, :vocab] / temperature,  log p_v = y_v - log sum_u exp(y_u)
+ *   logprob_out[r] = log p of tokens[r];  entropy_out[r] = - sum_v p_v log p_v  (natural logarithms)
+ *   top_ids_out[r, :], top_logprobs_out[r, :]: the n_top words with the largest logits, the largest first, equal ones by
+ *   the lower word first (-0 == +0), and their log p.  NULL for n_top = 0.
+ * Logits may be -inf (masked words: p = 0, log p = -inf, nothing added to the entropy).  A row of -inf alone has log p = -inf for
+ * every word and entropy 0.  A row with a NaN gives NaN, one with +inf unspecified values; the words named are in the vocabulary
+ * all the same.  A token outside [0, vocab) has log p = -inf.
+ * logits [rows, stride_row], dtype F32 or BF16, rows 16-byte aligned, stride_row >= vocab; the first `vocab` entries of a row
+ * are read.  tokens [rows] int32; outputs fp32 [rows], int32 and fp32 [rows, n_top].  1 <= rows <= 2^22, vocab <= 2^20,
+ * 0 <= n_top <= 32 and <= vocab, temperature > 0 and finite (at least 1e-38).  Sums are fp32, of the words other than
+ * the largest, so that a row whose best word has nearly all the weight keeps its entropy.  Deterministic.
+ * Errors: NULL_ARG, BAD_SHAPE, BAD_DTYPE, BAD_ALIGN, WORKSPACE_TOO_SMALL, HIP.
+ */
+size_t hippo_token_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t dtype, int32_t n_top);
+int hippo_token_logprobs(const void* logits, int32_t dtype, int64_t stride_row, const int32_t* tokens, int32_t rows,
+                         int32_t vocab, float temperature, int32_t n_top,
+                         float* logprob_out, float* entropy_out, int32_t* top_ids_out, float* top_logprobs_out,
+                         void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------------
  * Host-side control of video parallel speculative decoding (Method, "Video Parallel Speculative

@@ -28,7 +28,8 @@ EXPORTS = ("hippo_status_string", "hippo_workspace_bytes", "hippo_score_tokens",
            "hippo_verify_attention_paged", "hippo_draft_attention_paged",
            "hippo_verify_attention_fp8kv", "hippo_draft_attention_fp8kv",
            "hippo_quantize_kv_workspace_bytes", "hippo_quantize_kv_e4m3",
-           "hippo_spec_verify_workspace_bytes", "hippo_spec_verify", "hippo_vpsd_prefill_buffer",
+           "hippo_spec_verify_workspace_bytes", "hippo_spec_verify",
+           "hippo_token_logprobs_workspace_bytes", "hippo_token_logprobs", "hippo_vpsd_prefill_buffer",
            "hippo_vpsd_init", "hippo_vpsd_plan", "hippo_vpsd_commit", "hippo_vpsd_simulate")
 VPSD_CONSERVATIVE, VPSD_OPTIMISTIC = 0, 1
 POLICY_AUTOREGRESSIVE, POLICY_SERIAL_SD, POLICY_VPSD = 0, 1, 2
@@ -136,6 +137,10 @@ def load():
     lib.hippo_spec_verify_workspace_bytes.restype = C.c_size_t
     lib.hippo_spec_verify.argtypes = [vp, vp, i32, i64, i64, vp, vp, vp, i32, i32, i32, f32, vp, vp, vp, vp, sz, vp]
     lib.hippo_spec_verify.restype = C.c_int
+    lib.hippo_token_logprobs_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    lib.hippo_token_logprobs_workspace_bytes.restype = C.c_size_t
+    lib.hippo_token_logprobs.argtypes = [vp, i32, i64, vp, i32, i32, f32, i32, vp, vp, vp, vp, vp, sz, vp]
+    lib.hippo_token_logprobs.restype = C.c_int
     _lib = lib
     return lib
 
@@ -348,6 +353,14 @@ def hippo_spec_verify(p_logits, q_logits, draft_tokens, u_accept, u_sample, temp
     (n_accept [B] int32, next_token [B] int32[, alpha [B,gamma] fp32])."""
     return _call(stream, (_native or _bound()).spec_verify, p_logits, q_logits, draft_tokens, u_accept, u_sample,
                  temperature, want_alpha, n_accept_out, next_token_out, workspace)
+
+
+def hippo_token_logprobs(logits, tokens, temperature: float = 1.0, n_top: int = 0, logprob_out=None, entropy_out=None,
+                         top_ids_out=None, top_logprobs_out=None, workspace=None, stream=None):
+    """logits [..., V] (rows may be padded, and lie evenly spaced), tokens [...] int32 -> (logprob [...], entropy [...]) fp32,
+    with n_top > 0 also (top_ids [..., n_top] int32, top_logprobs [..., n_top] fp32), the most likely word first."""
+    return _call(stream, (_native or _bound()).token_logprobs, logits, tokens, temperature, n_top, logprob_out, entropy_out,
+                 top_ids_out, top_logprobs_out, workspace)
 
 
 # ---------------------------------------------------------------------------------------------

@@ -292,6 +292,24 @@ int plan_spec(int batch, int gamma, int vocab, int dtype, SpecPlan* pl) {
   return HIPPO_OK;
 }
 
+// ---- log probabilities: planning ------------------------------------------------------------------
+struct LogprobPlan {
+  int n_range, range_words;
+  bool wide;
+  size_t off_best, bytes;
+};
+
+int plan_logprobs(int rows, int vocab, int dtype, int n_top, LogprobPlan* pl) {
+  if (dtype != HIPPO_DTYPE_F32 && dtype != HIPPO_DTYPE_BF16) return HIPPO_ERR_BAD_DTYPE;
+  if (rows < 1 || rows > (1 << 22) || vocab < 1 || vocab > kLpMaxVocab || n_top < 0 || n_top > kLpMaxTop || n_top > vocab)
+    return HIPPO_ERR_BAD_SHAPE;
+  logprob_plan(rows, vocab, &pl->n_range, &pl->range_words, &pl->wide);
+  const size_t ranges = pl->n_range > 1 ? (size_t)rows * pl->n_range : 0;
+  pl->off_best = align_up(ranges * kLpStatBytes, 256);
+  pl->bytes = std::max<size_t>(256, pl->off_best + align_up(ranges * n_top * sizeof(unsigned long long), 256));
+  return HIPPO_OK;
+}
+
 }  // namespace
 
 // ---- scratch for callers that cannot allocate -----------------------------------------------------
@@ -593,6 +611,40 @@ int hippo_spec_verify(const void* p_logits, const void* q_logits, int32_t dtype,
   p.cells = reinterpret_cast<float*>(ws + pl.off_cells);
   p.arrived = reinterpret_cast<int*>(ws + pl.off_arrived);
   const hipError_t e = launch_spec_verify(p, dtype, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? HIPPO_OK : HIPPO_ERR_HIP;
+}
+
+size_t hippo_token_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t dtype, int32_t n_top) {
+  LogprobPlan pl;
+  return plan_logprobs(rows, vocab, dtype, n_top, &pl) == HIPPO_OK ? pl.bytes : 0;
+}
+
+int hippo_token_logprobs(const void* logits, int32_t dtype, int64_t stride_row, const int32_t* tokens, int32_t rows,
+                         int32_t vocab, float temperature, int32_t n_top, float* logprob_out, float* entropy_out,
+                         int32_t* top_ids_out, float* top_logprobs_out, void* workspace, size_t workspace_bytes, void* stream) {
+  LogprobPlan pl;
+  const int rc = plan_logprobs(rows, vocab, dtype, n_top, &pl);
+  if (rc != HIPPO_OK) return rc;
+  if (!(temperature > 0.f) || isinf(temperature) || isinf(kLog2e / temperature)) return HIPPO_ERR_BAD_SHAPE;
+  if (logits == nullptr || tokens == nullptr || logprob_out == nullptr || entropy_out == nullptr || workspace == nullptr)
+    return HIPPO_ERR_NULL_ARG;
+  if (n_top > 0 && (top_ids_out == nullptr || top_logprobs_out == nullptr)) return HIPPO_ERR_NULL_ARG;
+  if (stride_row < vocab) return HIPPO_ERR_BAD_SHAPE;
+  if (stride_row % (16 / elem_bytes(dtype)) || !aligned16(logits) || (reinterpret_cast<uintptr_t>(workspace) & 255u))
+    return HIPPO_ERR_BAD_ALIGN;
+  for (const void* p : {(const void*)tokens, (const void*)logprob_out, (const void*)entropy_out, (const void*)top_ids_out,
+                        (const void*)top_logprobs_out})
+    if (reinterpret_cast<uintptr_t>(p) & 3u) return HIPPO_ERR_BAD_ALIGN;
+  if (workspace_bytes < pl.bytes) return HIPPO_ERR_WORKSPACE_TOO_SMALL;
+
+  LogprobParams p;
+  p.logits = logits; p.stride = stride_row; p.tokens = tokens; p.R = rows; p.V = vocab; p.n_top = n_top;
+  p.n_range = pl.n_range; p.range_words = pl.range_words; p.wide = pl.wide;
+  p.c = kLog2e / temperature; p.inv_t = 1.0f / temperature;
+  p.logprob = logprob_out; p.entropy = entropy_out; p.top_ids = top_ids_out; p.top_logprobs = top_logprobs_out;
+  p.stats = workspace;
+  p.best = reinterpret_cast<unsigned long long*>(static_cast<char*>(workspace) + pl.off_best);
+  const hipError_t e = launch_logprobs(p, dtype, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? HIPPO_OK : HIPPO_ERR_HIP;
 }
 

@@ -34,7 +34,8 @@ namespace {
   X(hippo_select_gather_kv) X(hippo_verify_attention) X(hippo_draft_attention) X(hippo_verify_attention_append)         \
   X(hippo_draft_attention_append) X(hippo_verify_attention_paged) X(hippo_draft_attention_paged)                        \
   X(hippo_verify_attention_fp8kv) X(hippo_draft_attention_fp8kv) X(hippo_quantize_kv_workspace_bytes)                   \
-  X(hippo_quantize_kv_e4m3) X(hippo_spec_verify_workspace_bytes) X(hippo_spec_verify)
+  X(hippo_quantize_kv_e4m3) X(hippo_spec_verify_workspace_bytes) X(hippo_spec_verify)                   \
+  X(hippo_token_logprobs_workspace_bytes) X(hippo_token_logprobs)
 struct Library {
 #define X(name) decltype(&::name) name;
   HIPPO_LIBRARY(X)
@@ -445,6 +446,54 @@ PyObject* spec_verify(PyObject* const* a) {
   return want ? tuple({wrap(n_acc), wrap(next), wrap(alpha)}) : tuple({wrap(n_acc), wrap(next)});
 }
 
+// an output of this type and shape: `given`, or a new one
+Tensor output(PyObject* given, at::IntArrayRef sizes, at::ScalarType type, const Tensor& like) {
+  if (given == Py_None) return empty(sizes, type, like);
+  const Tensor t = tensor(given);
+  REQUIRE(t.sizes() == sizes && t.is_contiguous() && t.scalar_type() == type && t.device() == like.device());
+  return t;
+}
+
+// logits, tokens, temperature, n_top, logprob_out, entropy_out, top_ids_out, top_logprobs_out, workspace
+PyObject* token_logprobs(PyObject* const* a) {
+  const Tensor &x = tensor(a[0]), &tokens = tensor(a[1]);
+  REQUIRE(x.dim() >= 2 && x.stride(-1) == 1);
+  const int code = dtype_code(x);
+  const long long V = x.size(-1), n_top = integer(a[3]);
+  long long rows = 1, stride = x.stride(-2);
+  std::vector<int64_t> shape;
+  for (int64_t i = 0; i < x.dim() - 1; ++i) {
+    rows *= x.size(i);
+    shape.push_back(x.size(i));
+  }
+  // rows evenly spaced: every dimension steps over the ones inside it (the stride of a single element is nobody's)
+  long long step = 0;
+  for (int64_t i = x.dim() - 2, inside = 1; i >= 0; inside *= x.size(i--)) {
+    if (x.size(i) == 1) continue;
+    if (inside == 1) stride = step = x.stride(i);
+    else REQUIRE(x.stride(i) == inside * step);
+  }
+  if (rows == 1) stride = std::max<long long>(stride, (V + 7) / 8 * 8);       // nobody steps over the only row
+  REQUIRE(rows <= 0x7fffffff && V <= 0x7fffffff && n_top >= 0 && n_top <= 0x7fffffff);
+  REQUIRE(tokens.sizes() == at::IntArrayRef(shape) && tokens.is_contiguous() && tokens.scalar_type() == at::kInt);
+  const float temperature = (float)number(a[2]);
+  const Tensor logprob = output(a[4], shape, at::kFloat, x), entropy = output(a[5], shape, at::kFloat, x);
+  Tensor ids, top;
+  if (n_top > 0) {
+    shape.push_back(n_top);
+    ids = output(a[6], shape, at::kInt, x);
+    top = output(a[7], shape, at::kFloat, x);
+  }
+  const Tensor ws = workspace(a[8], x, [&] {
+    return lib.hippo_token_logprobs_workspace_bytes((int32_t)rows, (int32_t)V, code, (int32_t)n_top);
+  });
+  check(unlocked(lib.hippo_token_logprobs, ptr<const void>(x), code, (int64_t)stride, ptr<const int32_t>(tokens), (int32_t)rows,
+                 (int32_t)V, temperature, (int32_t)n_top, ptr<float>(logprob), ptr<float>(entropy), ptr<int32_t>(ids),
+                 ptr<float>(top), ptr(ws), (size_t)ws.numel(), stream()),
+        "hippo_token_logprobs");
+  return n_top > 0 ? tuple({wrap(logprob), wrap(entropy), wrap(ids), wrap(top)}) : tuple({wrap(logprob), wrap(entropy)});
+}
+
 // bind(path of libhippo.so, VideoDesc, HippoError)
 PyObject* bind(PyObject* const* a) {
   const char* path = PyUnicode_AsUTF8(a[0]);
@@ -489,7 +538,8 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #define ENTRY(name, n) {#name, (PyCFunction)(void (*)(void))entry<name, n>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     ENTRY(bind, 3), ENTRY(score_tokens, 9), ENTRY(score_tokens_layers, 10), ENTRY(select_gather, 11), ENTRY(attention, 12),
-    ENTRY(attention_fp8kv, 12), ENTRY(attention_paged, 11), ENTRY(quantize, 6), ENTRY(spec_verify, 10), {nullptr, nullptr, 0, nullptr}};
+    ENTRY(attention_fp8kv, 12), ENTRY(attention_paged, 11), ENTRY(quantize, 6), ENTRY(spec_verify, 10), ENTRY(token_logprobs, 9),
+    {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -417,4 +417,30 @@ struct SpecParams {
 hipError_t launch_spec_verify(const SpecParams& p, int dtype, hipStream_t st);
 int spec_cells_per_segment(int dtype);
 
+// ---- log probabilities of words -----------------------------------------------------------------
+constexpr int kLpMaxVocab = 1 << 20;
+constexpr int kLpMaxTop = 32;       // most likely words of a row
+constexpr int kLpThreads = 256, kLpWide = 1024;
+constexpr int kLpMaxRanges = 128;   // blocks of a row
+
+struct LogprobParams {
+  const void* logits;        // [R, stride]
+  long long stride;
+  const int32_t* tokens;     // [R]
+  int R, V, n_top;
+  int n_range, range_words;  // blocks of a row and a block's words (whole chunks, but for one that takes the row)
+  bool wide;                 // blocks of 1024 threads
+  float c, inv_t;            // log2(e) / temperature, 1 / temperature
+  float* logprob;            // [R]
+  float* entropy;            // [R]
+  int32_t* top_ids;          // [R, n_top]
+  float* top_logprobs;
+  // workspace pieces, where a row has several blocks
+  void* stats;               // [R, n_range] 16 bytes each
+  unsigned long long* best;  // [R, n_range, n_top]
+};
+constexpr size_t kLpStatBytes = 16;
+hipError_t launch_logprobs(const LogprobParams& p, int dtype, hipStream_t st);
+void logprob_plan(int rows, int vocab, int* n_range, int* range_words, bool* wide);
+
 }  // namespace hippo
