@@ -10,6 +10,7 @@
  *                        hippo_*_attention_append, hippo_*_attention_paged and
  *                        hippo_*_attention_fp8kv with hippo_quantize_kv_e4m3 (cache-format variants),
  *                        hippo_spec_verify (the speculative-sampling verdict of Eq. 1),
+ *                        hippo_evict_kv (a draft cache that stays within a budget),
  *                        hippo_token_logprobs (log probabilities of an answer's words),
  *                        hippo_vpsd_* (host-side control of the parallel decoding rounds).
  *
@@ -187,6 +188,31 @@ int hippo_select_gather_kv(const float* scores, int32_t k,
                            void* k_dst, void* v_dst, const hippo_kv_desc* dst,
                            int32_t* idx_out,
                            void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Eviction from a cache that has outgrown its budget, by accumulated attention weight (hippo_*_attention_mass): what a draft
+ * cache needs that is pruned once, at prefill, and then grows with the answer.  Every (batch element, KV head) chooses for
+ * itself; of its src_len rows these `keep` stay:
+ *   the first n_first, the last n_recent, and of those between the keep - n_first - n_recent with the largest mass
+ *   (equal ones, -0 == +0: the lower row; NaN ranks below every number).
+ *   idx_out[b, hk, :] = the rows that stay, ascending
+ *   dst row j of (b, hk) = src row idx_out[b, hk, j] for K and V, bit copies;  mass_dst likewise
+ * A row of dst is not at its old position: attention over dst takes ctx_len = keep, and a model's position embedding goes on from
+ * the old length, as it does behind a pruned cache.
+ * mass: element (b, hk, n) at b * mass_stride_b + hk * mass_stride_h + n, fp32; only rows between are read for the choice.
+ * src and dst may be 8-bit caches (codes are copied; the per-head multipliers stay valid); they agree in batch, n_kv_heads,
+ * head_dim and dtype.  k_dst/v_dst may be NULL together (indices and mass only, k_src/v_src are then not read), mass_dst may be
+ * NULL.  Rows of dst and mass_dst from `keep` on are left as they were, so that a decoding loop appends behind them.
+ * src and dst must not overlap.  1 <= keep <= src_len <= 2^30, n_first + n_recent <= keep.  Deterministic.
+ * Errors: NULL_ARG, BAD_SHAPE (also dst on src), BAD_DTYPE, BAD_ALIGN, WORKSPACE_TOO_SMALL, HIP.
+ */
+size_t hippo_evict_kv_workspace_bytes(const hippo_kv_desc* src, int32_t src_len, int32_t keep);
+int hippo_evict_kv(const float* mass, int64_t mass_stride_b, int64_t mass_stride_h,
+                   int32_t keep, int32_t n_first, int32_t n_recent,
+                   const void* k_src, const void* v_src, const hippo_kv_desc* src, int32_t src_len,
+                   void* k_dst, void* v_dst, const hippo_kv_desc* dst,
+                   float* mass_dst, int64_t mass_dst_stride_b, int64_t mass_dst_stride_h,
+                   int32_t* idx_out, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Target verification attention (Preliminaries, "Speculative Decoding": the target model takes the

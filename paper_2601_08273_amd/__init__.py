@@ -22,7 +22,7 @@ SCORE_ATTN, SCORE_TEMP, SCORE_SPA, SCORE_ALL, SCORE_ACCUMULATE_ONLY = 1, 2, 4, 7
 
 EXPORTS = ("hippo_status_string", "hippo_workspace_bytes", "hippo_score_tokens",
            "hippo_score_layers_workspace_bytes", "hippo_score_tokens_layers",
-           "hippo_select_gather_kv", "hippo_verify_attention", "hippo_draft_attention",
+           "hippo_select_gather_kv", "hippo_evict_kv_workspace_bytes", "hippo_evict_kv", "hippo_verify_attention", "hippo_draft_attention",
            "hippo_static_scratch_bytes", "hippo_static_scratch_init", "hippo_verify_attention_static",
            "hippo_verify_attention_append", "hippo_draft_attention_append",
            "hippo_verify_attention_paged", "hippo_draft_attention_paged",
@@ -104,6 +104,10 @@ def load():
     lib.hippo_score_tokens_layers.restype = C.c_int
     lib.hippo_select_gather_kv.argtypes = [vp, i32, vp, vp, kvp, i32, vdp, vp, vp, kvp, vp, vp, sz, vp]
     lib.hippo_select_gather_kv.restype = C.c_int
+    lib.hippo_evict_kv_workspace_bytes.argtypes = [kvp, i32, i32]
+    lib.hippo_evict_kv_workspace_bytes.restype = sz
+    lib.hippo_evict_kv.argtypes = [vp, i64, i64, i32, i32, i32, vp, vp, kvp, i32, vp, vp, kvp, vp, i64, i64, vp, vp, sz, vp]
+    lib.hippo_evict_kv.restype = C.c_int
     for fn in (lib.hippo_verify_attention, lib.hippo_draft_attention):
         fn.argtypes = [vp, i32, vp, vp, kvp, i32, f32, i32, vp, vp, vp, sz, vp]
         fn.restype = C.c_int
@@ -270,6 +274,17 @@ def hippo_select_gather_kv(scores, k: int, k_src, v_src, vid: VideoDesc, n_q_hea
     idx_out / k_dst / v_dst: optional preallocated outputs (k_dst, v_dst may be strided views)."""
     return _call(stream, (_native or _bound()).select_gather, scores, k, k_src, v_src, vid, n_q_heads, gather, idx_out,
                  k_dst, v_dst, workspace)
+
+
+def hippo_evict_kv(mass, keep: int, k_src, v_src, n_rows: Optional[int] = None, n_first: int = 0, n_recent: int = 0,
+                   idx_out=None, k_dst=None, v_dst=None, mass_dst=None, workspace=None, stream=None):
+    """mass [B,Hkv,>=n_rows] fp32, caches [B,Hkv,>=n_rows,d] (any cache type; None, None for the indices and mass only) ->
+    (idx [B,Hkv,keep] int32, k_dst, v_dst [B,Hkv,keep,d], mass_dst [B,Hkv,keep]): of each KV head the first n_first and last
+    n_recent of its n_rows rows (default: all of the cache's, or of mass's) and the rows between with the largest mass.
+    k_dst / v_dst / mass_dst: optional preallocated outputs of at least `keep` rows (strided views may be given); the rows behind
+    stay as they were."""
+    return _call(stream, (_native or _bound()).evict, mass, keep, k_src, v_src, n_rows, n_first, n_recent, idx_out, k_dst, v_dst,
+                 mass_dst, workspace)
 
 
 def hippo_verify_attention(q, k_cache, v_cache, ctx_len: int, softmax_scale: float = 0.0, num_splits: int = 0,

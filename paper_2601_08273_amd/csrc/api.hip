@@ -529,6 +529,55 @@ int hippo_select_gather_kv(const float* scores, int32_t k, const void* k_src, co
   return e == hipSuccess ? HIPPO_OK : HIPPO_ERR_HIP;
 }
 
+size_t hippo_evict_kv_workspace_bytes(const hippo_kv_desc* src, int32_t src_len, int32_t keep) {
+  if (check_kv(src, true) != HIPPO_OK || src_len < 1 || src_len > (1 << 30) || keep < 1 || keep > src_len) return 0;
+  return 256;   // the selection keeps its state in LDS; a token amount keeps the contract uniform
+}
+
+int hippo_evict_kv(const float* mass, int64_t mass_stride_b, int64_t mass_stride_h, int32_t keep, int32_t n_first,
+                   int32_t n_recent, const void* k_src, const void* v_src, const hippo_kv_desc* src, int32_t src_len,
+                   void* k_dst, void* v_dst, const hippo_kv_desc* dst, float* mass_dst, int64_t mass_dst_stride_b,
+                   int64_t mass_dst_stride_h, int32_t* idx_out, void* workspace, size_t workspace_bytes, void* stream) {
+  if (mass == nullptr || idx_out == nullptr || workspace == nullptr || src == nullptr) return HIPPO_ERR_NULL_ARG;
+  int rc = check_kv(src, true);
+  if (rc != HIPPO_OK) return rc;
+  if (src_len < 1 || src_len > (1 << 30) || n_first < 0 || n_recent < 0 || keep < 1 || keep > src_len) return HIPPO_ERR_BAD_SHAPE;
+  if ((long long)n_first + n_recent > keep) return HIPPO_ERR_BAD_SHAPE;
+  if (mass_stride_b < 0 || mass_stride_h < 0) return HIPPO_ERR_BAD_SHAPE;
+  if ((reinterpret_cast<uintptr_t>(mass) & 3u) || (reinterpret_cast<uintptr_t>(idx_out) & 3u) ||
+      (reinterpret_cast<uintptr_t>(workspace) & 255u))
+    return HIPPO_ERR_BAD_ALIGN;
+  EvictParams p;
+  p.mass = mass; p.mass_sb = mass_stride_b; p.mass_sh = mass_stride_h;
+  p.n_src = src_len; p.n_first = n_first; p.n_between = src_len - n_first - n_recent;
+  p.k = keep - n_first - n_recent; p.keep = keep;
+  p.idx_out = idx_out;
+  p.k_src = k_src; p.v_src = v_src; p.k_dst = nullptr; p.v_dst = nullptr;
+  p.mass_dst = mass_dst; p.mass_dsb = mass_dst_stride_b; p.mass_dsh = mass_dst_stride_h;
+  p.B = src->batch; p.Hkv = src->n_kv_heads; p.D = src->head_dim; p.elem_bytes = elem_bytes(src->dtype);
+  p.ssb = src->stride_b; p.ssh = src->stride_h; p.ssn = src->stride_n;
+  p.dsb = p.dsh = p.dsn = 0;
+  // every (batch element, KV head) writes rows of its own: those of different heads must not meet
+  if (mass_dst != nullptr) {
+    if (mass_dst == mass) return HIPPO_ERR_BAD_SHAPE;
+    if (reinterpret_cast<uintptr_t>(mass_dst) & 3u) return HIPPO_ERR_BAD_ALIGN;
+    if ((p.Hkv > 1 && mass_dst_stride_h < keep) || (p.B > 1 && mass_dst_stride_b < keep)) return HIPPO_ERR_BAD_SHAPE;
+  }
+  if (k_dst != nullptr || v_dst != nullptr) {
+    if (k_dst == nullptr || v_dst == nullptr || k_src == nullptr || v_src == nullptr || dst == nullptr) return HIPPO_ERR_NULL_ARG;
+    if ((rc = check_kv(dst, true)) != HIPPO_OK) return rc;
+    if (dst->batch != src->batch || dst->n_kv_heads != src->n_kv_heads || dst->head_dim != src->head_dim ||
+        dst->dtype != src->dtype || k_dst == k_src || v_dst == v_src || k_dst == v_src || v_dst == k_src || k_dst == v_dst)
+      return HIPPO_ERR_BAD_SHAPE;
+    if (!aligned16(k_src) || !aligned16(v_src) || !aligned16(k_dst) || !aligned16(v_dst)) return HIPPO_ERR_BAD_ALIGN;
+    p.k_dst = k_dst; p.v_dst = v_dst;
+    p.dsb = dst->stride_b; p.dsh = dst->stride_h; p.dsn = dst->stride_n;
+  }
+  if (workspace_bytes < 256) return HIPPO_ERR_WORKSPACE_TOO_SMALL;
+  const hipError_t e = launch_evict(p, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? HIPPO_OK : HIPPO_ERR_HIP;
+}
+
 int hippo_verify_attention(const void* q, int32_t q_len, const void* k_cache, const void* v_cache,
                            const hippo_kv_desc* kv, int32_t ctx_len, float softmax_scale, int32_t num_splits,
                            void* out, float* lse_out, void* workspace, size_t workspace_bytes, void* stream) {

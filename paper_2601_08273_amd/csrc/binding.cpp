@@ -17,6 +17,7 @@
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
 #include <ATen/ops/zeros.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -35,7 +36,8 @@ namespace {
   X(hippo_draft_attention_append) X(hippo_verify_attention_paged) X(hippo_draft_attention_paged)                        \
   X(hippo_verify_attention_fp8kv) X(hippo_draft_attention_fp8kv) X(hippo_quantize_kv_workspace_bytes)                   \
   X(hippo_quantize_kv_e4m3) X(hippo_spec_verify_workspace_bytes) X(hippo_spec_verify)                   \
-  X(hippo_token_logprobs_workspace_bytes) X(hippo_token_logprobs)
+  X(hippo_token_logprobs_workspace_bytes) X(hippo_token_logprobs)                 \
+  X(hippo_evict_kv_workspace_bytes) X(hippo_evict_kv)
 struct Library {
 #define X(name) decltype(&::name) name;
   HIPPO_LIBRARY(X)
@@ -276,6 +278,79 @@ PyObject* select_gather(PyObject* const* a) {
   return tuple({wrap(idx), wrap(k_dst), wrap(v_dst)});
 }
 
+// an output of this type and shape: `given`, or a new one
+Tensor output(PyObject* given, at::IntArrayRef sizes, at::ScalarType type, const Tensor& like) {
+  if (given == Py_None) return empty(sizes, type, like);
+  const Tensor t = tensor(given);
+  REQUIRE(t.sizes() == sizes && t.is_contiguous() && t.scalar_type() == type && t.device() == like.device());
+  return t;
+}
+
+// A kernel on the current stream reads and writes these: memory of the current device, not the host's or another GPU's.
+void require_here(std::initializer_list<const Tensor*> tensors) {
+  for (const Tensor* t : tensors)
+    if (t->defined()) require(t->is_cuda() && t->get_device() == c10::hip::current_device(), "tensors lie on the current device");
+}
+
+// [B, H_kv, at least n] fp32, any strides with unit stride on the rows
+void require_mass(const Tensor& mass, long long B, long long Hkv, long long n) {
+  REQUIRE(mass.dim() == 3 && mass.scalar_type() == at::kFloat && mass.size(0) == B && mass.size(1) == Hkv && mass.size(2) >= n);
+  REQUIRE(mass.stride(2) == 1 || mass.size(2) == 1);
+}
+
+// mass, keep, k_src, v_src, n_rows, n_first, n_recent, idx_out, k_dst, v_dst, mass_dst, workspace
+PyObject* evict(PyObject* const* a) {
+  const Tensor& mass = tensor(a[0]);
+  const long long keep = integer(a[1]), first = integer(a[5]), recent = integer(a[6]);
+  const Tensor k_src = tensor_or_none(a[2]), v_src = tensor_or_none(a[3]);
+  REQUIRE(mass.dim() == 3 && k_src.defined() == v_src.defined());
+  const long long B = mass.size(0), Hkv = mass.size(1);
+  const bool caches = k_src.defined();
+  long long n = caches && k_src.dim() == 4 ? k_src.size(2) : mass.size(2);
+  hippo_kv_desc src{}, dst{};
+  if (caches) {
+    src = describe(k_src, k_src.dim() == 4 ? k_src.size(1) : 0);
+    REQUIRE(same_layout(v_src, k_src) && v_src.scalar_type() == k_src.scalar_type());
+    REQUIRE(k_src.size(0) == B && k_src.size(1) == Hkv);
+  } else {                                                     // no rows to copy: any cache of these heads
+    src.batch = (int32_t)B;
+    src.n_q_heads = src.n_kv_heads = (int32_t)Hkv;
+    src.head_dim = 64;
+    src.dtype = HIPPO_DTYPE_F32;
+    src.stride_n = 64;
+    REQUIRE(a[8] == Py_None && a[9] == Py_None);
+  }
+  if (a[4] != Py_None) {
+    REQUIRE(integer(a[4]) >= 1 && integer(a[4]) <= n);
+    n = integer(a[4]);
+  }
+  require_mass(mass, B, Hkv, n);
+  REQUIRE(n <= 0x7fffffff && keep >= 1 && keep <= n && first >= 0 && first <= n && recent >= 0 && recent <= n);
+  const Tensor idx = output(a[7], {B, Hkv, keep}, at::kInt, mass);
+  Tensor k_dst = tensor_or_none(a[8]), v_dst = tensor_or_none(a[9]), mass_dst = tensor_or_none(a[10]);
+  if (caches) {
+    if (!k_dst.defined()) {
+      REQUIRE(!v_dst.defined());
+      k_dst = empty({B, Hkv, keep, k_src.size(3)}, k_src.scalar_type(), k_src);
+      v_dst = at::empty_like(k_dst);
+    }
+    REQUIRE(k_dst.dim() == 4 && k_dst.size(0) == B && k_dst.size(1) == Hkv && k_dst.size(2) >= keep && k_dst.size(3) == k_src.size(3));
+    REQUIRE(v_dst.defined() && same_layout(v_dst, k_dst));
+    REQUIRE(k_dst.scalar_type() == k_src.scalar_type() && v_dst.scalar_type() == k_src.scalar_type());
+    dst = describe(k_dst, Hkv);
+  }
+  if (!mass_dst.defined()) mass_dst = empty({B, Hkv, keep}, at::kFloat, mass);
+  require_mass(mass_dst, B, Hkv, keep);
+  const Tensor ws = workspace(a[11], mass, [&] { return lib.hippo_evict_kv_workspace_bytes(&src, (int32_t)n, (int32_t)keep); });
+  require_here({&mass, &k_src, &v_src, &idx, &k_dst, &v_dst, &mass_dst, &ws});
+  check(unlocked(lib.hippo_evict_kv, ptr<const float>(mass), (int64_t)mass.stride(0), (int64_t)mass.stride(1), (int32_t)keep,
+                 (int32_t)first, (int32_t)recent, ptr<const void>(k_src), ptr<const void>(v_src), &src, (int32_t)n, ptr(k_dst),
+                 ptr(v_dst), caches ? &dst : nullptr, ptr<float>(mass_dst), (int64_t)mass_dst.stride(0),
+                 (int64_t)mass_dst.stride(1), ptr<int32_t>(idx), ptr(ws), (size_t)ws.numel(), stream()),
+        "hippo_evict_kv");
+  return tuple({wrap(idx), wrap(k_dst), wrap(v_dst), wrap(mass_dst)});
+}
+
 // what the attention calls have in common: q, the rows' statistics, the output, the workspace
 struct AttentionCall {
   const Tensor& q;
@@ -446,14 +521,6 @@ PyObject* spec_verify(PyObject* const* a) {
   return want ? tuple({wrap(n_acc), wrap(next), wrap(alpha)}) : tuple({wrap(n_acc), wrap(next)});
 }
 
-// an output of this type and shape: `given`, or a new one
-Tensor output(PyObject* given, at::IntArrayRef sizes, at::ScalarType type, const Tensor& like) {
-  if (given == Py_None) return empty(sizes, type, like);
-  const Tensor t = tensor(given);
-  REQUIRE(t.sizes() == sizes && t.is_contiguous() && t.scalar_type() == type && t.device() == like.device());
-  return t;
-}
-
 // logits, tokens, temperature, n_top, logprob_out, entropy_out, top_ids_out, top_logprobs_out, workspace
 PyObject* token_logprobs(PyObject* const* a) {
   const Tensor &x = tensor(a[0]), &tokens = tensor(a[1]);
@@ -487,6 +554,7 @@ PyObject* token_logprobs(PyObject* const* a) {
   const Tensor ws = workspace(a[8], x, [&] {
     return lib.hippo_token_logprobs_workspace_bytes((int32_t)rows, (int32_t)V, code, (int32_t)n_top);
   });
+  require_here({&x, &tokens, &logprob, &entropy, &ids, &top, &ws});
   check(unlocked(lib.hippo_token_logprobs, ptr<const void>(x), code, (int64_t)stride, ptr<const int32_t>(tokens), (int32_t)rows,
                  (int32_t)V, temperature, (int32_t)n_top, ptr<float>(logprob), ptr<float>(entropy), ptr<int32_t>(ids),
                  ptr<float>(top), ptr(ws), (size_t)ws.numel(), stream()),
@@ -538,7 +606,7 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #define ENTRY(name, n) {#name, (PyCFunction)(void (*)(void))entry<name, n>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     ENTRY(bind, 3), ENTRY(score_tokens, 9), ENTRY(score_tokens_layers, 10), ENTRY(select_gather, 11), ENTRY(attention, 12),
-    ENTRY(attention_fp8kv, 12), ENTRY(attention_paged, 11), ENTRY(quantize, 6), ENTRY(spec_verify, 10), ENTRY(token_logprobs, 9),
+    ENTRY(attention_fp8kv, 12), ENTRY(attention_paged, 11), ENTRY(quantize, 6), ENTRY(spec_verify, 10), ENTRY(token_logprobs, 9), ENTRY(evict, 12),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -360,6 +360,23 @@ struct SelectParams {
 };
 hipError_t launch_select_gather(const SelectParams& p, hipStream_t st);
 
+// Eviction: of every (batch element, KV head) the first rows, the k of the rows between with the largest mass, the recent rows.
+struct EvictParams {
+  const float* mass;                        // row n of (b, hk) at b * mass_sb + hk * mass_sh + n
+  long long mass_sb, mass_sh;
+  int n_src, n_first, n_between, k, keep;   // n_between = n_src - n_first - recent rows, keep = n_first + k + recent rows
+  int32_t* idx_out;                         // [B, Hkv, keep]
+  const void* k_src;
+  const void* v_src;
+  void* k_dst;                              // null: indices (and mass) only
+  void* v_dst;
+  float* mass_dst;                          // may be null
+  long long mass_dsb, mass_dsh;
+  int B, Hkv, D, elem_bytes;
+  long long ssb, ssh, ssn, dsb, dsh, dsn;   // element strides
+};
+hipError_t launch_evict(const EvictParams& p, hipStream_t st);
+
 // ---- writer of the 8-bit cache format -----------------------------------------------------------
 struct QuantParams {
   const void* k_src;

@@ -105,7 +105,8 @@ __device__ __forceinline__ long long gather_offset(long long row, const SelectPa
   return row * p.elem_bytes + (e & ((1 << vpr_shift) - 1)) * 16;
 }
 
-// One block per sequence.  NC > 0: every thread keeps NC keys in registers, so the scores are read
+// The k largest of Nv scores, by one block; emit(place among the kept, index) for each of them.  NC > 0: every thread keeps NC keys
+// in registers, so the scores are read
 // from memory once and every loop over them is unrolled to the sequence's size class.  A wave owns
 // 64 NC consecutive scores, dealt to its lanes VW at a time (slot c of lane l is score
 // wave*64*NC + ((c / VW)*64 + l)*VW + c % VW), so that each load instruction of a wave reads one
@@ -117,27 +118,18 @@ __device__ __forceinline__ long long gather_offset(long long row, const SelectPa
 // third histogram are built from that list instead of from another sweep over every thread's keys.
 // The compaction is index-ordered: when the keys are cached, one wave scan per group of VW slots plus
 // one scan of the wave totals, per-(chunk, wave) ballots with running totals otherwise.
-//
-// GATHER: the launch builds the draft cache too.  Grid (H_kv * parts, B): every block selects for itself -- the same
-// integers, while all compute units but one would idle -- keeps the indices in LDS and copies its part of one KV head's
-// rows.  Saves a launch on the host and its start on the GPU (16384 tokens x 4 heads, 10 %: 9.2 + 4.3 us of kernels -> 12.1,
-// the eager call 17.7 -> 15.0; 1568 x 2 heads 4.1 + 2.6 -> 6.3).
-template <int NC, bool GATHER>
-__global__ __launch_bounds__(kSelThreads) void topk_select(SelectParams p, int vpr_shift) {
+// hist: kHistWords of LDS, one histogram per radix pass (12, 12, 8 bits); bin i lives at i + i/64, so that the 64 lanes of
+// the scanning wave, which own runs of 64 consecutive bins, hit different LDS banks.  Nothing reads it once a key is emitted.
+template <int NC, typename Emit>
+__device__ __forceinline__ void select_top(const float* sc, const int Nv, const int k, unsigned* const hist, Emit emit) {
   constexpr bool CACHED = NC > 0;
-  static_assert(CACHED || !GATHER, "the indices are in LDS only where the keys are in registers");
-  // one histogram per radix pass (12, 12, 8 bits); bin i lives at i + i/64, so that the 64 lanes of
-  // the scanning wave, which own runs of 64 consecutive bins, hit different LDS banks
   constexpr int kListCap = kBins;            // candidate list: the first histogram's memory, once its digit is known
-  __shared__ unsigned hist[kHistWords];
   __shared__ unsigned wave_tot[2][kSelWaves];
   __shared__ unsigned sh_prefix, sh_need, sh_bin_count, sh_list_n;
 
-  const int b = GATHER ? blockIdx.y : blockIdx.x, tid = threadIdx.x;
+  const int tid = threadIdx.x;
   const int lane = tid & 63, wave = tid >> 6;
-  const float* sc = p.scores + (long long)b * p.Nv;
-  int32_t* out = p.idx_out + (long long)b * p.k;
-  const int n_chunks = (p.Nv + kSelThreads - 1) / kSelThreads;
+  const int n_chunks = (Nv + kSelThreads - 1) / kSelThreads;
   // CACHED: every load goes out before anything waits for one: 16-byte loads where the row allows,
   // addresses past the end pulled back inside (those slots are then set to 0), and the histograms are
   // cleared under the loads.
@@ -147,27 +139,26 @@ __global__ __launch_bounds__(kSelThreads) void topk_select(SelectParams p, int v
   const int wave_first = wave * 64 * NC;     // CACHED only
   auto slot_index = [&](int c) { return wave_first + ((c / VW) * 64 + lane) * VW + c % VW; };
   if (CACHED) {
-    const bool vec_ok = (VW == 4) && (p.Nv % 4 == 0) && ((((long long)b * p.Nv) & 3) == 0) &&
-                        ((reinterpret_cast<uintptr_t>(p.scores) & 15u) == 0);      // block-uniform
+    const bool vec_ok = (VW == 4) && (Nv % 4 == 0) && ((reinterpret_cast<uintptr_t>(sc) & 15u) == 0);   // block-uniform
     if (vec_ok) {
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        const u32x4 x = *(const u32x4*)(sc + min(slot_index(v * VW), p.Nv - 4));
+        const u32x4 x = *(const u32x4*)(sc + min(slot_index(v * VW), Nv - 4));
         keys[v * VW] = x.x; keys[v * VW + 1 % VW] = x.y; keys[v * VW + 2 % VW] = x.z; keys[v * VW + 3 % VW] = x.w;
       }
     } else {
 #pragma unroll
-      for (int c = 0; c < NC; ++c) keys[c] = __float_as_uint(sc[min(slot_index(c), p.Nv - 1)]);
+      for (int c = 0; c < NC; ++c) keys[c] = __float_as_uint(sc[min(slot_index(c), Nv - 1)]);
     }
   }
   for (int i = tid; i < kHistWords; i += kSelThreads) hist[i] = 0;
   if (tid == 0) sh_list_n = 0;
   if (CACHED) {
 #pragma unroll
-    for (int c = 0; c < NC; ++c) keys[c] = (slot_index(c) < p.Nv) ? score_key(__uint_as_float(keys[c])) : 0u;
+    for (int c = 0; c < NC; ++c) keys[c] = (slot_index(c) < Nv) ? score_key(__uint_as_float(keys[c])) : 0u;
   }
   // ---- radix select of the k-th largest key ----
-  unsigned prefix = 0, need = (unsigned)p.k;   // `need` keys still wanted among those matching prefix
+  unsigned prefix = 0, need = (unsigned)k;   // `need` keys still wanted among those matching prefix
   const int shifts[3] = {20, 8, 0};
   const unsigned masks[3] = {0u, 0xfff00000u, 0xffffff00u};   // bits already decided
   const unsigned dmask[3] = {0xfffu, 0xfffu, 0xffu};
@@ -192,10 +183,10 @@ __global__ __launch_bounds__(kSelThreads) void topk_select(SelectParams p, int v
       for (int c0 = 0; c0 < n_chunks; c0 += 8) {         // eight scores in flight per thread
         float v[8];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = sc[min((c0 + q) * kSelThreads + tid, p.Nv - 1)];
+        for (int q = 0; q < 8; ++q) v[q] = sc[min((c0 + q) * kSelThreads + tid, Nv - 1)];
 #pragma unroll
         for (int q = 0; q < 8; ++q)
-          if ((c0 + q) * kSelThreads + tid < p.Nv) {
+          if ((c0 + q) * kSelThreads + tid < Nv) {
             const unsigned key = score_key(v[q]);
             if ((key & masks[pass]) == prefix) atomicAdd(&h[hist_slot((key >> shifts[pass]) & dmask[pass])], 1u);
           }
@@ -283,7 +274,6 @@ __global__ __launch_bounds__(kSelThreads) void topk_select(SelectParams p, int v
       gt_front = waves_in_front(run >> 16, wave_tot[0], lane, wave);
       eq_front = waves_in_front(run & 0xffffu, wave_tot[1], lane, wave);
     }
-    const bool writes = !GATHER || blockIdx.x == 0;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       unsigned gt_before = gt_front + (excl[v] >> 16), eq_before = eq_front + (excl[v] & 0xffffu);
@@ -292,38 +282,10 @@ __global__ __launch_bounds__(kSelThreads) void topk_select(SelectParams p, int v
         const unsigned key = keys[v * VW + e];
         const bool gt = key > thr, eq = key == thr;
         if (gt || (eq && eq_before < need_eq)) {
-          const unsigned at = gt_before + min(eq_before, need_eq);
-          if (writes) out[at] = slot_index(v * VW + e);
-          if (GATHER) hist[at] = (unsigned)slot_index(v * VW + e);
+          emit(gt_before + min(eq_before, need_eq), slot_index(v * VW + e));
         }
         gt_before += gt ? 1u : 0u;
         eq_before += eq ? 1u : 0u;
-      }
-    }
-    if constexpr (GATHER) {
-      __syncthreads();
-      const int hk = blockIdx.x % p.Hkv, part = blockIdx.x / p.Hkv, parts = gridDim.x / p.Hkv;
-      const int per_head = p.dst_len << vpr_shift;
-      constexpr int U = 4;                       // vectors of K and of V in flight per thread
-      for (int e0 = part * kSelThreads + tid; e0 < per_head; e0 += U * parts * kSelThreads) {
-        u32x4 kv[U], vv[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int e = min(e0 + u * parts * kSelThreads, per_head - 1);     // past the end: a repeat, not stored
-          const int n = e >> vpr_shift, kept = min(max(n - p.vis_off, 0), p.k - 1);
-          const int from = n < p.vis_off ? n : n < p.vis_off + p.k ? p.vis_off + (int)hist[kept] : n - p.k + p.Nv;
-          const long long so = gather_offset(b * p.ssb + hk * p.ssh + from * p.ssn, p, e, vpr_shift);
-          kv[u] = *(const u32x4*)((const char*)p.k_src + so);
-          vv[u] = *(const u32x4*)((const char*)p.v_src + so);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int e = e0 + u * parts * kSelThreads;
-          if (e >= per_head) break;
-          const long long dof = gather_offset(b * p.dsb + hk * p.dsh + (e >> vpr_shift) * p.dsn, p, e, vpr_shift);
-          *(u32x4*)((char*)p.k_dst + dof) = kv[u];
-          *(u32x4*)((char*)p.v_dst + dof) = vv[u];
-        }
       }
     }
   } else {
@@ -332,12 +294,12 @@ __global__ __launch_bounds__(kSelThreads) void topk_select(SelectParams p, int v
     if (tid == 0) { run_gt = 0; run_eq = 0; }
     __syncthreads();
     const unsigned long long below = (1ull << lane) - 1ull;
-    float ahead = sc[min(tid, p.Nv - 1)];                // the next chunk's score travels under this chunk's barriers
+    float ahead = sc[min(tid, Nv - 1)];                // the next chunk's score travels under this chunk's barriers
     for (int c = 0; c < n_chunks; ++c) {
       const float mine = ahead;
-      if (c + 1 < n_chunks) ahead = sc[min((c + 1) * kSelThreads + tid, p.Nv - 1)];
+      if (c + 1 < n_chunks) ahead = sc[min((c + 1) * kSelThreads + tid, Nv - 1)];
       bool gt = false, eq = false;
-      if (c * kSelThreads + tid < p.Nv) {
+      if (c * kSelThreads + tid < Nv) {
         const unsigned key = score_key(mine);
         gt = key > thr;
         eq = key == thr;
@@ -349,13 +311,58 @@ __global__ __launch_bounds__(kSelThreads) void topk_select(SelectParams p, int v
       unsigned off_gt = run_gt, off_eq = run_eq;
       for (int w = 0; w < wave; ++w) { off_gt += wg[w]; off_eq += we[w]; }
       const unsigned gt_before = off_gt + my_gt, eq_before = off_eq + my_eq;
-      if (gt || (eq && eq_before < need_eq)) out[gt_before + min(eq_before, need_eq)] = c * kSelThreads + tid;
+      if (gt || (eq && eq_before < need_eq)) emit(gt_before + min(eq_before, need_eq), c * kSelThreads + tid);
       __syncthreads();
       if (tid == kSelThreads - 1) {
         run_gt = off_gt + my_gt + (gt ? 1u : 0u);
         run_eq = off_eq + my_eq + (eq ? 1u : 0u);
       }
       __syncthreads();
+    }
+  }
+}
+
+// One block per sequence.
+//
+// GATHER: the launch builds the draft cache too.  Grid (H_kv * parts, B): every block selects for itself -- the same
+// integers, while all compute units but one would idle -- keeps the indices in LDS and copies its part of one KV head's
+// rows.  Saves a launch on the host and its start on the GPU (16384 tokens x 4 heads, 10 %: 9.2 + 4.3 us of kernels -> 12.1,
+// the eager call 17.7 -> 15.0; 1568 x 2 heads 4.1 + 2.6 -> 6.3).
+template <int NC, bool GATHER>
+__global__ __launch_bounds__(kSelThreads) void topk_select(SelectParams p, int vpr_shift) {
+  static_assert(NC > 0 || !GATHER, "the indices are in LDS only where the keys are in registers");
+  __shared__ unsigned hist[kHistWords];
+  const int b = GATHER ? blockIdx.y : blockIdx.x, tid = threadIdx.x;
+  int32_t* out = p.idx_out + (long long)b * p.k;
+  const bool writes = !GATHER || blockIdx.x == 0;
+  select_top<NC>(p.scores + (long long)b * p.Nv, p.Nv, p.k, hist, [&](unsigned at, int index) {
+    if (writes) out[at] = index;
+    if (GATHER) hist[at] = (unsigned)index;
+  });
+  if constexpr (GATHER) {
+    __syncthreads();
+    const int hk = blockIdx.x % p.Hkv, part = blockIdx.x / p.Hkv, parts = gridDim.x / p.Hkv;
+    const int per_head = p.dst_len << vpr_shift;
+    constexpr int U = 4;                       // vectors of K and of V in flight per thread
+    for (int e0 = part * kSelThreads + tid; e0 < per_head; e0 += U * parts * kSelThreads) {
+      u32x4 kv[U], vv[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int e = min(e0 + u * parts * kSelThreads, per_head - 1);     // past the end: a repeat, not stored
+        const int n = e >> vpr_shift, kept = min(max(n - p.vis_off, 0), p.k - 1);
+        const int from = n < p.vis_off ? n : n < p.vis_off + p.k ? p.vis_off + (int)hist[kept] : n - p.k + p.Nv;
+        const long long so = gather_offset(b * p.ssb + hk * p.ssh + from * p.ssn, p, e, vpr_shift);
+        kv[u] = *(const u32x4*)((const char*)p.k_src + so);
+        vv[u] = *(const u32x4*)((const char*)p.v_src + so);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int e = e0 + u * parts * kSelThreads;
+        if (e >= per_head) break;
+        const long long dof = gather_offset(b * p.dsb + hk * p.dsh + (e >> vpr_shift) * p.dsn, p, e, vpr_shift);
+        *(u32x4*)((char*)p.k_dst + dof) = kv[u];
+        *(u32x4*)((char*)p.v_dst + dof) = vv[u];
+      }
     }
   }
 }
@@ -443,6 +450,66 @@ hipError_t launch_select_gather(const SelectParams& p, hipStream_t st) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || per_head == 0 || one_launch) return e;
   hipLaunchKernelGGL(gather_kv, dim3((unsigned)((per_head + 255) / 256), p.Hkv, p.B), dim3(256), 0, st, p, vpr_shift);
+  return hipGetLastError();
+}
+
+// =================================================================================================
+// Eviction: every KV head of every sequence keeps rows of its own
+// =================================================================================================
+// One block per (KV head, sequence): the indices of the rows that stay, ascending.
+template <int NC>
+__global__ __launch_bounds__(kSelThreads) void evict_select(EvictParams p) {
+  __shared__ unsigned hist[kHistWords];
+  const int hk = blockIdx.x, b = blockIdx.y;
+  int32_t* out = p.idx_out + ((long long)b * p.Hkv + hk) * p.keep;
+  const int recent = p.keep - p.n_first - p.k;
+  for (int i = threadIdx.x; i < p.n_first; i += kSelThreads) out[i] = i;
+  for (int i = threadIdx.x; i < recent; i += kSelThreads) out[p.n_first + p.k + i] = p.n_src - recent + i;
+  if (p.k > 0)
+    select_top<NC>(p.mass + b * p.mass_sb + hk * p.mass_sh + p.n_first, p.n_between, p.k, hist,
+                   [&](unsigned at, int index) { out[p.n_first + (int)at] = p.n_first + index; });
+}
+
+// A thread moves 16 bytes of K and of V of rows that lie `gridDim.x` blocks apart; the first of a row's threads its mass too.
+__global__ __launch_bounds__(256) void evict_gather(EvictParams p, int vpr_shift) {
+  const int hk = blockIdx.y, b = blockIdx.z;
+  const int32_t* idx = p.idx_out + ((long long)b * p.Hkv + hk) * p.keep;
+  const int rows_per_block = 256 >> vpr_shift, vec = threadIdx.x & ((1 << vpr_shift) - 1);
+  const int n = blockIdx.x * rows_per_block + (threadIdx.x >> vpr_shift);
+  if (n >= p.keep) return;
+  const int from = idx[n];
+  if (p.mass_dst != nullptr && vec == 0)
+    p.mass_dst[b * p.mass_dsb + hk * p.mass_dsh + n] = p.mass[b * p.mass_sb + hk * p.mass_sh + from];
+  if (p.k_dst == nullptr) return;
+  const long long so = (b * p.ssb + hk * p.ssh + (long long)from * p.ssn) * p.elem_bytes + vec * 16;
+  const long long dof = (b * p.dsb + hk * p.dsh + (long long)n * p.dsn) * p.elem_bytes + vec * 16;
+  const u32x4 kv = *(const u32x4*)((const char*)p.k_src + so);
+  const u32x4 vv = *(const u32x4*)((const char*)p.v_src + so);
+  *(u32x4*)((char*)p.k_dst + dof) = kv;
+  *(u32x4*)((char*)p.v_dst + dof) = vv;
+}
+
+hipError_t launch_evict(const EvictParams& p, hipStream_t st) {
+  const int n_chunks = (p.n_between + kSelThreads - 1) / kSelThreads;
+  const int vpr = p.D * p.elem_bytes / 16;                 // 16-byte vectors per row: 4, 8, 16 or 32
+  int vpr_shift = 0;
+  while ((1 << vpr_shift) < vpr) ++vpr_shift;
+  const dim3 heads(p.Hkv, p.B);
+#define HIPPO_EVICT(NC_) hipLaunchKernelGGL((evict_select<NC_>), heads, dim3(kSelThreads), 0, st, p)
+  if (n_chunks <= 2) { HIPPO_EVICT(2); }
+  else if (n_chunks <= 4) { HIPPO_EVICT(4); }
+  else if (n_chunks <= 8) { HIPPO_EVICT(8); }
+  else if (n_chunks <= 16) { HIPPO_EVICT(16); }
+  else if (n_chunks <= 24) { HIPPO_EVICT(24); }
+  else if (n_chunks <= 40) { HIPPO_EVICT(40); }
+  else if (n_chunks <= kKeysPerThread) { HIPPO_EVICT(kKeysPerThread); }
+  else { HIPPO_EVICT(0); }
+#undef HIPPO_EVICT
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || (p.k_dst == nullptr && p.mass_dst == nullptr)) return e;
+  const int rows_per_block = 256 >> vpr_shift;
+  hipLaunchKernelGGL(evict_gather, dim3((unsigned)((p.keep + rows_per_block - 1) / rows_per_block), p.Hkv, p.B), dim3(256), 0, st,
+                     p, vpr_shift);
   return hipGetLastError();
 }
 

@@ -1,0 +1,75 @@
+"""Refusals of hippo_evict_kv, without a GPU: the library answers before it launches anything."""
+import ctypes as C
+
+import pytest
+import torch
+
+import paper_2601_08273_amd as h
+
+FAKE = 0x10000
+
+
+def desc(rows=20000, **more):
+    d = dict(batch=2, n_q_heads=28, n_kv_heads=4, head_dim=128, dtype=h.DTYPE_BF16)
+    d.update(more)
+    d.setdefault("stride_n", d["head_dim"])
+    d.setdefault("stride_h", rows * d["head_dim"])
+    d.setdefault("stride_b", d["n_kv_heads"] * rows * d["head_dim"])
+    return h.KvDesc(**d)
+
+
+def call(mass=FAKE, msb=80000, msh=20000, keep=8000, first=4, recent=256, k=FAKE, v=2 * FAKE, src=None, n=16657, kd=3 * FAKE,
+         vd=4 * FAKE, dst=None, md=5 * FAKE, mdb=80000, mdh=20000, idx=FAKE, ws=FAKE, ws_bytes=256, no_src=False, no_dst=False):
+    src = None if no_src else C.byref(src or desc())
+    dst = None if no_dst else C.byref(dst or desc(8192))
+    return h.load().hippo_evict_kv(mass, msb, msh, keep, first, recent, k, v, src, n, kd, vd, dst, md, mdb, mdh, idx, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("bad,status", [
+    (dict(mass=None), h.ERR_NULL_ARG), (dict(idx=None), h.ERR_NULL_ARG), (dict(ws=None), h.ERR_NULL_ARG),
+    (dict(no_src=True), h.ERR_NULL_ARG), (dict(no_dst=True), h.ERR_NULL_ARG), (dict(k=None), h.ERR_NULL_ARG),
+    (dict(vd=None), h.ERR_NULL_ARG), (dict(kd=None), h.ERR_NULL_ARG),
+    (dict(keep=0), h.ERR_BAD_SHAPE), (dict(keep=16658), h.ERR_BAD_SHAPE), (dict(keep=259), h.ERR_BAD_SHAPE),
+    (dict(first=-1), h.ERR_BAD_SHAPE), (dict(recent=-1), h.ERR_BAD_SHAPE), (dict(first=8000), h.ERR_BAD_SHAPE),
+    (dict(first=0x7fffffff, recent=0x7fffffff), h.ERR_BAD_SHAPE),
+    (dict(n=0), h.ERR_BAD_SHAPE), (dict(n=(1 << 30) + 1), h.ERR_BAD_SHAPE),
+    (dict(msh=-1), h.ERR_BAD_SHAPE), (dict(mdh=7999), h.ERR_BAD_SHAPE), (dict(mdb=0), h.ERR_BAD_SHAPE),
+    (dict(md=FAKE), h.ERR_BAD_SHAPE), (dict(kd=FAKE), h.ERR_BAD_SHAPE), (dict(vd=3 * FAKE), h.ERR_BAD_SHAPE),
+    (dict(vd=FAKE), h.ERR_BAD_SHAPE),
+    (dict(dst=desc(8192, batch=1)), h.ERR_BAD_SHAPE), (dict(dst=desc(8192, n_kv_heads=2)), h.ERR_BAD_SHAPE),
+    (dict(dst=desc(8192, head_dim=64)), h.ERR_BAD_SHAPE), (dict(dst=desc(8192, dtype=h.DTYPE_F32)), h.ERR_BAD_SHAPE),
+    (dict(src=desc(dtype=5)), h.ERR_BAD_DTYPE), (dict(src=desc(head_dim=96)), h.ERR_BAD_SHAPE),
+    (dict(k=FAKE + 8), h.ERR_BAD_ALIGN), (dict(vd=4 * FAKE + 4), h.ERR_BAD_ALIGN), (dict(mass=FAKE + 2), h.ERR_BAD_ALIGN),
+    (dict(md=5 * FAKE + 1), h.ERR_BAD_ALIGN), (dict(idx=FAKE + 2), h.ERR_BAD_ALIGN), (dict(ws=FAKE + 64), h.ERR_BAD_ALIGN),
+    (dict(dst=desc(8192, stride_n=132)), h.ERR_BAD_ALIGN),
+    (dict(ws_bytes=255), h.ERR_WORKSPACE_TOO_SMALL),
+])
+def test_arguments_are_checked(bad, status):
+    assert call(**bad) == status
+
+
+def test_workspace_sizes():
+    need = h.load().hippo_evict_kv_workspace_bytes
+    assert need(C.byref(desc()), 16657, 8000) > 0 and need(C.byref(desc(dtype=h.DTYPE_FP8_E4M3)), 16657, 8000) > 0
+    assert need(C.byref(desc()), 16657, 16658) == 0 and need(C.byref(desc()), 0, 1) == 0 and need(None, 10, 1) == 0
+
+
+def test_the_binding_refuses_tensors_it_would_misread():
+    m, k = torch.zeros(2, 3, 50), torch.zeros(2, 3, 50, 64)
+    v = k.clone()
+    for args, more in (
+            ((m.double(), 20, k, v), {}), ((m[0], 20, k, v), {}), ((m[:1], 20, k, v), {}), ((m[:, :, :40], 20, k, v), {}),
+            ((m.transpose(1, 2).contiguous().transpose(1, 2), 20, k, v), {}),                    # rows of mass not side by side
+            ((m, 20, k, v.transpose(1, 2).contiguous().transpose(1, 2)), {}), ((m, 20, k, v.bfloat16()), {}), ((m, 20, k, None), {}),
+            ((m, 0, k, v), {}), ((m, 51, k, v), {}), ((m, 20, k, v), dict(n_first=-1)), ((m, 20, k, v), dict(n_rows=51)),
+            ((m, 20, k, v), dict(n_rows=0)),
+            ((m, 20, k, v), dict(idx_out=torch.zeros(2, 3, 21, dtype=torch.int32))),
+            ((m, 20, k, v), dict(idx_out=torch.zeros(2, 3, 20))),
+            ((m, 20, k, v), dict(k_dst=torch.zeros(2, 3, 19, 64), v_dst=torch.zeros(2, 3, 19, 64))),
+            ((m, 20, k, v), dict(k_dst=torch.zeros(2, 3, 20, 64))), ((m, 20, k, v), dict(v_dst=torch.zeros(2, 3, 20, 64))),
+            ((m, 20, k, v), dict(k_dst=torch.zeros(2, 3, 20, 64).bfloat16(), v_dst=torch.zeros(2, 3, 20, 64).bfloat16())),
+            ((m, 20, k, v), dict(mass_dst=torch.zeros(2, 3, 19))), ((m, 20, None, None), dict(k_dst=k, v_dst=v))):
+        with pytest.raises(AssertionError):
+            h.hippo_evict_kv(*args, **more)
+    with pytest.raises(AssertionError):                           # host memory, which no kernel reads
+        h.hippo_evict_kv(m, 20, k, v)

@@ -51,5 +51,7 @@ def test_the_binding_refuses_tensors_it_would_misread():
             (x, t, dict(n_top=2, top_logprobs_out=torch.zeros(2, 4).t())), (x, t, dict(n_top=-1))):
         with pytest.raises(AssertionError):
             h.hippo_token_logprobs(logits, tokens, **more)
+    with pytest.raises(AssertionError):                           # host memory, which no kernel reads
+        h.hippo_token_logprobs(x, t)
     with pytest.raises(TypeError):
         h.hippo_token_logprobs(x.double(), t)
