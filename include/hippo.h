@@ -10,7 +10,7 @@
  *                        hippo_*_attention_append, hippo_*_attention_paged and
  *                        hippo_*_attention_fp8kv with hippo_quantize_kv_e4m3 (cache-format variants),
  *                        hippo_spec_verify (the speculative-sampling verdict of Eq. 1),
- *                        hippo_evict_kv (a draft cache that stays within a budget),
+ *                        hippo_*_attention_mass with hippo_evict_kv (a draft cache that stays within a budget),
  *                        hippo_token_logprobs (log probabilities of an answer's words),
  *                        hippo_vpsd_* (host-side control of the parallel decoding rounds).
  *
@@ -295,6 +295,39 @@ int hippo_draft_attention_append(const void* q, int32_t q_len, const void* k_new
                                  int32_t ctx_len, float softmax_scale, int32_t num_splits,
                                  void* out, float* lse_out,
                                  void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The same two attention calls with the weight that every cache row was given: what an eviction goes by (hippo_evict_kv).
+ *   mass_out[b, hk, n] = (n < ctx_len ? mass_in[b, hk, n] : 0)
+ *                        + sum over the new rows i and the query heads h of KV head hk of softmax_n(...)[b, i, h],
+ *   n in [0, ctx_len + q_len); a new row i gives nothing to rows behind ctx_len + i.
+ * out and lse_out as without mass, but that the slices' outputs reach the merge in fp32.  The weights are fp32 from fp32
+ * logits, of the probabilities before any rounding; sums run in a fixed order.  Rows that a verification rejects leave their share
+ * in older rows' mass; their own rows' mass is written anew with the rows.
+ * mass: `in` may be NULL (nothing accumulated yet) or `out` (in place, the same strides); element (b, hk, n) lies at
+ * b * stride_b + hk * stride_h + n.  Elements of `out` from ctx_len + q_len on are left as they were.
+ * k_new, v_new: both NULL (the caches hold the new rows), or the rows to append, as in the *_append calls.  Caches: F32 or BF16,
+ * contiguous.  Workspace: hippo_attention_mass_workspace_bytes, with seq_len = ctx_len + q_len; it grows with seq_len times the
+ * query rows.
+ * Errors: as the *_append calls, plus NULL_ARG for mass or its out, BAD_SHAPE for mass strides of rows that would meet.
+ */
+typedef struct hippo_mass_desc {
+  const float* in;
+  float* out;
+  int64_t in_stride_b, in_stride_h, out_stride_b, out_stride_h;   /* elements */
+} hippo_mass_desc;
+
+size_t hippo_attention_mass_workspace_bytes(const hippo_kv_desc* kv, int32_t q_len, int32_t seq_len, int32_t num_splits);
+int hippo_verify_attention_mass(const void* q, int32_t q_len, const void* k_new, const void* v_new,
+                                void* k_cache, void* v_cache, const hippo_kv_desc* kv,
+                                int32_t ctx_len, float softmax_scale, int32_t num_splits,
+                                void* out, float* lse_out, const hippo_mass_desc* mass,
+                                void* workspace, size_t workspace_bytes, void* stream);
+int hippo_draft_attention_mass(const void* q, int32_t q_len, const void* k_new, const void* v_new,
+                               void* k_cache, void* v_cache, const hippo_kv_desc* kv,
+                               int32_t ctx_len, float softmax_scale, int32_t num_splits,
+                               void* out, float* lse_out, const hippo_mass_desc* mass,
+                               void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * The same two attention calls over a cache stored in 8-bit floating point (a cache-format variant

@@ -25,6 +25,7 @@ EXPORTS = ("hippo_status_string", "hippo_workspace_bytes", "hippo_score_tokens",
            "hippo_select_gather_kv", "hippo_evict_kv_workspace_bytes", "hippo_evict_kv", "hippo_verify_attention", "hippo_draft_attention",
            "hippo_static_scratch_bytes", "hippo_static_scratch_init", "hippo_verify_attention_static",
            "hippo_verify_attention_append", "hippo_draft_attention_append",
+           "hippo_attention_mass_workspace_bytes", "hippo_verify_attention_mass", "hippo_draft_attention_mass",
            "hippo_verify_attention_paged", "hippo_draft_attention_paged",
            "hippo_verify_attention_fp8kv", "hippo_draft_attention_fp8kv",
            "hippo_quantize_kv_workspace_bytes", "hippo_quantize_kv_e4m3",
@@ -57,6 +58,11 @@ class PagedKvDesc(C.Structure):
                 ("head_dim", C.c_int32), ("dtype", C.c_int32), ("page_size", C.c_int32),
                 ("max_pages", C.c_int32), ("n_pool_pages", C.c_int32),
                 ("stride_page", C.c_int64), ("stride_n", C.c_int64), ("stride_h", C.c_int64)]
+
+
+class MassDesc(C.Structure):
+    _fields_ = [("in_", C.c_void_p), ("out", C.c_void_p), ("in_stride_b", C.c_int64), ("in_stride_h", C.c_int64),
+                ("out_stride_b", C.c_int64), ("out_stride_h", C.c_int64)]
 
 
 class KvDesc(C.Structure):
@@ -123,6 +129,11 @@ def load():
     for fn in (lib.hippo_verify_attention_append, lib.hippo_draft_attention_append,
                lib.hippo_verify_attention_fp8kv, lib.hippo_draft_attention_fp8kv):
         fn.argtypes = [vp, i32, vp, vp, vp, vp, kvp, i32, f32, i32, vp, vp, vp, sz, vp]
+        fn.restype = C.c_int
+    lib.hippo_attention_mass_workspace_bytes.argtypes = [kvp, i32, i32, i32]
+    lib.hippo_attention_mass_workspace_bytes.restype = sz
+    for fn in (lib.hippo_verify_attention_mass, lib.hippo_draft_attention_mass):
+        fn.argtypes = [vp, i32, vp, vp, vp, vp, kvp, i32, f32, i32, vp, vp, C.POINTER(MassDesc), vp, sz, vp]
         fn.restype = C.c_int
     lib.hippo_quantize_kv_workspace_bytes.argtypes = [kvp, i32]
     lib.hippo_quantize_kv_workspace_bytes.restype = C.c_size_t
@@ -300,6 +311,23 @@ def hippo_draft_attention(q, k_cache, v_cache, ctx_len: int, softmax_scale: floa
                           want_lse: bool = False, out=None, workspace=None, stream=None, k_new=None, v_new=None):
     return _call(stream, (_native or _bound()).attention, True, q, k_cache, v_cache, ctx_len, softmax_scale, num_splits,
                  want_lse, out, workspace, k_new, v_new)
+
+
+def hippo_verify_attention_mass(q, k_cache, v_cache, mass, ctx_len: int, softmax_scale: float = 0.0, num_splits: int = 0,
+                                want_lse: bool = False, out=None, mass_out=None, workspace=None, stream=None, k_new=None,
+                                v_new=None):
+    """hippo_verify_attention, and the weight that each cache row was given: mass [B,Hkv,>=ctx_len] fp32 or None (nothing
+    accumulated yet) -> (out, mass_out [B,Hkv,ctx_len+q_len][, lse]).  mass_out may be given with at least that many rows, `mass`
+    itself among them (in place); the rows behind stay as they were.  k_new / v_new [B,q_len,Hkv,d] are appended to the caches."""
+    return _call(stream, (_native or _bound()).attention_mass, False, q, k_cache, v_cache, mass, ctx_len, softmax_scale, num_splits,
+                 want_lse, out, mass_out, workspace, k_new, v_new)
+
+
+def hippo_draft_attention_mass(q, k_cache, v_cache, mass, ctx_len: int, softmax_scale: float = 0.0, num_splits: int = 0,
+                               want_lse: bool = False, out=None, mass_out=None, workspace=None, stream=None, k_new=None,
+                               v_new=None):
+    return _call(stream, (_native or _bound()).attention_mass, True, q, k_cache, v_cache, mass, ctx_len, softmax_scale, num_splits,
+                 want_lse, out, mass_out, workspace, k_new, v_new)
 
 
 def hippo_verify_attention_static(q, k_cache, v_cache, ctx_len: int, softmax_scale: float = 0.0, num_splits: int = 0,

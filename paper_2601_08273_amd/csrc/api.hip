@@ -52,8 +52,9 @@ struct AttnPlan {
   size_t off_m, off_l, off_e, bytes;
 };
 
+// mass: for a call that sums its weights
 int plan_attention(int call, const hippo_kv_desc* kv, int q_len, int n_total, int num_splits, AttnPlan* pl,
-                   bool may_be_wide = true) {
+                   bool may_be_wide = true, bool mass = false) {
   (void)call;   // draft and verify share one launch heuristic (they differ in wave priority only)
   if (q_len < 1 || n_total < q_len || num_splits < 0) return HIPPO_ERR_BAD_SHAPE;
   const int G = kv->n_q_heads / kv->n_kv_heads;
@@ -126,13 +127,31 @@ int plan_attention(int call, const hippo_kv_desc* kv, int q_len, int n_total, in
   if (S > 1024) S = 1024;
   pl->S = S;
   const size_t slots = (size_t)kv->batch * kv->n_kv_heads * S;
-  // the bf16 kernel hands its slices' outputs to the merge as bf16, the fp32 kernel as fp32
-  const size_t o_bytes = align_up(slots * pl->R * kv->head_dim * (f32 ? sizeof(float) : 2), 256);
+  // the bf16 kernel hands its slices' outputs to the merge as bf16, the fp32 kernel and the one for attention mass as fp32
+  const size_t o_bytes = align_up(slots * pl->R * kv->head_dim * (f32 || mass ? sizeof(float) : 2), 256);
   const size_t ml_bytes = align_up(slots * pl->R * sizeof(float), 256);
   pl->off_m = o_bytes;
   pl->off_l = o_bytes + ml_bytes;
   pl->off_e = o_bytes + 2 * ml_bytes;
   pl->bytes = pl->off_e + (wide ? align_up(slots * pl->R * 2 * sizeof(float), 256) : 0);
+  return HIPPO_OK;
+}
+
+// What a call that sums its weights needs beside that: the slices' second denominators, and the logits.
+struct MassPlan {
+  AttnPlan attn;
+  int logits_ld;
+  size_t off_f, off_logits, bytes;
+};
+
+int plan_mass(int call, const hippo_kv_desc* kv, int q_len, int n_total, int num_splits, MassPlan* pl) {
+  const int rc = plan_attention(call, kv, q_len, n_total, num_splits, &pl->attn, false, true);
+  if (rc != HIPPO_OK) return rc;
+  const size_t heads = (size_t)kv->batch * kv->n_kv_heads;
+  pl->logits_ld = (int)align_up((size_t)n_total, 64);
+  pl->off_f = pl->attn.bytes;
+  pl->off_logits = pl->off_f + align_up(heads * pl->attn.S * pl->attn.R * sizeof(float), 256);
+  pl->bytes = pl->off_logits + heads * pl->attn.R * pl->logits_ld * sizeof(float);
   return HIPPO_OK;
 }
 
@@ -147,6 +166,10 @@ struct AttnExtra {
   bool fp8 = false;                         // E4M3 cache with per-(b, hk) multipliers
   const float* k_scale = nullptr;
   const float* v_scale = nullptr;
+  bool mass = false;                        // sums of the weights
+  const float* mass_in = nullptr;
+  float* mass_out = nullptr;
+  long long mass_isb = 0, mass_ish = 0, mass_osb = 0, mass_osh = 0;
 };
 
 int attention_entry(int call, const void* q, int32_t q_len, const void* k_cache, const void* v_cache,
@@ -169,8 +192,14 @@ int attention_entry(int call, const void* q, int32_t q_len, const void* k_cache,
     return HIPPO_ERR_BAD_ALIGN;
   if (append && (!aligned16(k_new) || !aligned16(v_new))) return HIPPO_ERR_BAD_ALIGN;
   AttnPlan pl;
-  rc = plan_attention(call, kv, q_len, ctx_len + q_len, num_splits, &pl);
+  MassPlan mp;
+  rc = ex.mass ? plan_mass(call, kv, q_len, ctx_len + q_len, num_splits, &mp)
+               : plan_attention(call, kv, q_len, ctx_len + q_len, num_splits, &pl);
   if (rc != HIPPO_OK) return rc;
+  if (ex.mass) {
+    pl = mp.attn;
+    pl.bytes = mp.bytes;
+  }
   // One block for 65 to 96 rows needs twice the workspace of two chunks.  A loop that sized its own before the cache grew past
   // that line, or for more query rows, goes on in two chunks.
   if (workspace_bytes < pl.bytes && pl.wide) rc = plan_attention(call, kv, q_len, ctx_len + q_len, num_splits, &pl, false);
@@ -206,6 +235,19 @@ int attention_entry(int call, const void* q, int32_t q_len, const void* k_cache,
   p.block_table = ex.block_table; p.page_shift = page_shift; p.max_pages = ex.max_pages;
   p.n_pool_pages = ex.n_pool_pages; p.page_stride = ex.page_stride;
   p.k_scale = ex.fp8 ? ex.k_scale : nullptr; p.v_scale = ex.fp8 ? ex.v_scale : nullptr;
+  if (ex.mass) {
+    MassParams m;
+    static_cast<AttnParams&>(m) = p;
+    char* ws = static_cast<char*>(workspace);
+    // (fp32 probabilities are not rounded: one denominator serves both)
+    m.part_f = kv->dtype == HIPPO_DTYPE_F32 ? p.part_l : reinterpret_cast<float*>(ws + mp.off_f);
+    m.logits = reinterpret_cast<float*>(ws + mp.off_logits);
+    m.logits_ld = mp.logits_ld;
+    m.mass_in = ex.mass_in; m.mass_out = ex.mass_out;
+    m.mass_isb = ex.mass_isb; m.mass_ish = ex.mass_ish; m.mass_osb = ex.mass_osb; m.mass_osh = ex.mass_osh;
+    const hipError_t e = launch_attention_mass(m, kv->dtype, kv->head_dim, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? HIPPO_OK : HIPPO_ERR_HIP;
+  }
   // q and out of the 8-bit cache calls are bf16
   const int io_dtype = ex.fp8 ? (int)HIPPO_DTYPE_BF16 : kv->dtype;
   const hipError_t e = launch_attention(p, io_dtype, kv->head_dim, static_cast<hipStream_t>(stream));
@@ -717,6 +759,51 @@ int hippo_draft_attention_append(const void* q, int32_t q_len, const void* k_new
   ex.append = true; ex.k_new = k_new; ex.v_new = v_new;
   return attention_entry(HIPPO_CALL_DRAFT_ATTENTION, q, q_len, k_cache, v_cache, kv, ctx_len, softmax_scale,
                          num_splits, out, lse_out, workspace, workspace_bytes, stream, ex);
+}
+
+static int mass_entry(int call, const void* q, int32_t q_len, const void* k_new, const void* v_new, void* k_cache, void* v_cache,
+                      const hippo_kv_desc* kv, int32_t ctx_len, float softmax_scale, int32_t num_splits, void* out, float* lse_out,
+                      const hippo_mass_desc* mass, void* workspace, size_t workspace_bytes, void* stream) {
+  if (kv == nullptr || mass == nullptr || mass->out == nullptr) return HIPPO_ERR_NULL_ARG;
+  if ((k_new == nullptr) != (v_new == nullptr)) return HIPPO_ERR_NULL_ARG;
+  if (mass->in != nullptr && (mass->in_stride_b < 0 || mass->in_stride_h < 0)) return HIPPO_ERR_BAD_SHAPE;
+  // every (batch element, KV head) writes a row of its own
+  const long long n = (long long)ctx_len + q_len;
+  if ((kv->n_kv_heads > 1 && mass->out_stride_h < n) || (kv->batch > 1 && mass->out_stride_b < n)) return HIPPO_ERR_BAD_SHAPE;
+  // in place: where it stood
+  if (mass->in == mass->out && ((kv->n_kv_heads > 1 && mass->in_stride_h != mass->out_stride_h) ||
+                                (kv->batch > 1 && mass->in_stride_b != mass->out_stride_b)))
+    return HIPPO_ERR_BAD_SHAPE;
+  if ((reinterpret_cast<uintptr_t>(mass->in) & 3u) || (reinterpret_cast<uintptr_t>(mass->out) & 3u)) return HIPPO_ERR_BAD_ALIGN;
+  AttnExtra ex;
+  ex.append = k_new != nullptr; ex.k_new = k_new; ex.v_new = v_new;
+  ex.mass = true; ex.mass_in = mass->in; ex.mass_out = mass->out;
+  ex.mass_isb = mass->in_stride_b; ex.mass_ish = mass->in_stride_h;
+  ex.mass_osb = mass->out_stride_b; ex.mass_osh = mass->out_stride_h;
+  return attention_entry(call, q, q_len, k_cache, v_cache, kv, ctx_len, softmax_scale, num_splits, out, lse_out, workspace,
+                         workspace_bytes, stream, ex);
+}
+
+size_t hippo_attention_mass_workspace_bytes(const hippo_kv_desc* kv, int32_t q_len, int32_t seq_len, int32_t num_splits) {
+  MassPlan pl;
+  if (check_kv(kv) != HIPPO_OK || plan_mass(HIPPO_CALL_VERIFY_ATTENTION, kv, q_len, seq_len, num_splits, &pl) != HIPPO_OK) return 0;
+  return pl.bytes;
+}
+
+int hippo_verify_attention_mass(const void* q, int32_t q_len, const void* k_new, const void* v_new, void* k_cache, void* v_cache,
+                                const hippo_kv_desc* kv, int32_t ctx_len, float softmax_scale, int32_t num_splits, void* out,
+                                float* lse_out, const hippo_mass_desc* mass, void* workspace, size_t workspace_bytes,
+                                void* stream) {
+  return mass_entry(HIPPO_CALL_VERIFY_ATTENTION, q, q_len, k_new, v_new, k_cache, v_cache, kv, ctx_len, softmax_scale, num_splits,
+                    out, lse_out, mass, workspace, workspace_bytes, stream);
+}
+
+int hippo_draft_attention_mass(const void* q, int32_t q_len, const void* k_new, const void* v_new, void* k_cache, void* v_cache,
+                               const hippo_kv_desc* kv, int32_t ctx_len, float softmax_scale, int32_t num_splits, void* out,
+                               float* lse_out, const hippo_mass_desc* mass, void* workspace, size_t workspace_bytes,
+                               void* stream) {
+  return mass_entry(HIPPO_CALL_DRAFT_ATTENTION, q, q_len, k_new, v_new, k_cache, v_cache, kv, ctx_len, softmax_scale, num_splits,
+                    out, lse_out, mass, workspace, workspace_bytes, stream);
 }
 
 // paged caches: translate the pool descriptor into the per-row strides the kernels use

@@ -137,9 +137,11 @@ __device__ __forceinline__ bf16x8 e4m3x8_to_bf16(int lo, int hi) {
 // TT = tokens per tile (16 or 32), NST = ring stages (super-tiles resident in LDS)
 // MODE: 0 = contiguous cache, 1 = contiguous cache with appended-row fusion, 2 = paged cache
 // ONE = the slice is the whole cache: the block writes its rows' output
+// MASS = for attn_combine_mass: the denominators of the probabilities as they are, before their rounding to bf16, and the logits
 template <int D, int RB, int TG, int TT, int NST, int MODE, bool KV8 = false, bool NT = false, bool ROT = false,
-          bool ONE = false>
-__global__ __launch_bounds__(RB * TG * 64) void attn_partial_grid(AttnParams p) {
+          bool ONE = false, bool MASS = false>
+__global__ __launch_bounds__(RB * TG * 64) void attn_partial_grid(ParamsOf<MASS> p) {
+  static_assert(!MASS || (MODE < 2 && !KV8 && !ONE && RB <= 4), "weights are summed over contiguous bf16 caches");
   constexpr bool APPEND = MODE == 1, PAGED = MODE == 2;
   constexpr bool LONG32 = ROT && TT == 32;
   constexpr bool SCALED = RB > 4;                      // more than 64 rows in one block: see its stores
@@ -184,6 +186,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_partial_grid(AttnParams p) 
   const int chunk = p.n_chunks == 1 ? 0 : (int)(blockIdx.z % p.n_chunks);
   const int r0 = chunk * (RB * 16);
   const float inv_g = __builtin_amdgcn_rcpf((float)p.G);
+  float* stat_f = (float*)(smem + SM::total(RB));            // MASS: [TG][RB*16]
 
   // fp8 cache: the K multiplier scales the logits, the V multiplier the slice's output.  Fetched
   // first, through the scalar cache (a vector load here would sit behind every K/V transfer in the
@@ -304,7 +307,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_partial_grid(AttnParams p) 
 
   const int row = r0 + rb * 16 + j;                       // this lane's query row
   const int lim = (row < p.R) ? p.ctx_len + row_div_group(row, inv_g) : 0x7fffffff;
-  float m_run = -INFINITY, l_run = 0.f;
+  float m_run = -INFINITY, l_run = 0.f, fine = 0.f;
   f32x4 acc[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) acc[db] = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -400,6 +403,12 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_partial_grid(AttnParams p) 
         for (int e = 0; e < 4; ++e)
           if ((n0 + (KV8 ? 8 * g + 4 * tb : tb * 16 + 4 * g) + e) > lim) s[tb][e] = -INFINITY;
     }
+    if constexpr (MASS)
+      if (p.logits != nullptr && row < p.R) {
+        float* at = p.logits + (((long long)b * p.Hkv + hk) * p.R + row) * p.logits_ld + n0 + 4 * g;
+#pragma unroll
+        for (int tb = 0; tb < TB; ++tb) *(f32x4*)(at + tb * 16) = s[tb];
+      }
     float sv[TB * 4];
 #pragma unroll
     for (int e = 0; e < TB * 4; ++e) sv[e] = s[e >> 2][e & 3];
@@ -415,6 +424,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_partial_grid(AttnParams p) 
       const float a = up ? fast_exp2(m_run - mx) : 1.f;    // m_run = -inf -> 0
       if (up) m_run = mx;
       l_run *= a;
+      if constexpr (MASS) fine *= a;
 #pragma unroll
       for (int db = 0; db < DB; ++db) acc[db] *= a;
     }
@@ -430,6 +440,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_partial_grid(AttnParams p) 
                          fast_exp2(fmaf(s[h >> 1][(2 * h + 1) & 3], scale_log2, neg_m))};
       pk[h] = __builtin_bit_cast(unsigned, __builtin_convertvector(x, bf16x2_t));
       psum += __uint_as_float(pk[h] << 16) + __uint_as_float(pk[h] & 0xffff0000u);
+      if constexpr (MASS) fine += x[0] + x[1];
     }
     l_run += psum;                                         // per-lane share; groups g meet at the end
 
@@ -464,9 +475,11 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_partial_grid(AttnParams p) 
 
   // ---- merge the TG token groups of every row block ----
   l_run = rows4_sum(l_run);
+  if constexpr (MASS) fine = rows4_sum(fine);
   if (g == 0) {
     stat_m[tg * RB * 16 + rb * 16 + j] = m_run;
     stat_l[tg * RB * 16 + rb * 16 + j] = l_run;
+    if constexpr (MASS) stat_f[tg * RB * 16 + rb * 16 + j] = fine;
   }
   f32x4* xbuf = (f32x4*)ring;                              // [WAVES][DB][64 lanes]
   __syncthreads();   // (a) every wave is done reading the ring before anyone overwrites it
@@ -495,6 +508,12 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_partial_grid(AttnParams p) 
     for (int w = 0; w < TG; ++w) {
       f[w] = (mw[w] == -INFINITY) ? 0.f : fast_exp2(mw[w] - mm);
       ll = fmaf(f[w], stat_l[w * RB * 16 + rb * 16 + j], ll);
+    }
+    if constexpr (MASS) {
+      float lf = 0.f;
+#pragma unroll
+      for (int w = 0; w < TG; ++w) lf = fmaf(f[w], stat_f[w * RB * 16 + rb * 16 + j], lf);
+      if (TGC == 0 && g == 0 && row < p.R) p.part_f[(((long long)b * p.Hkv + hk) * p.S + split) * p.R + row] = lf;
     }
     if constexpr (KV8) {
 #pragma unroll
@@ -556,7 +575,10 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_partial_grid(AttnParams p) 
       }
       // the slice's output leaves as bf16 (the merge weighs and sums it in fp32): half the bytes to write
       // here and to fetch in the merge, and the rounding is one more of the size the output's own has
-      if (row < p.R) {
+      // (MASS: in fp32.  One rounding less brings the output's error from 2.7e-3 to 2.3e-3, and few rows cost few bytes.)
+      if constexpr (MASS) {
+        if (row < p.R) *(f32x4*)((float*)p.part_o + (slot * p.R + row) * D + db * 16 + 4 * g) = o;
+      } else if (row < p.R) {
         typedef __attribute__((ext_vector_type(2))) float f32x2_t;
         const f32x2_t lo = {o[0], o[1]}, hi = {o[2], o[3]};
         uint2 w;
@@ -631,8 +653,9 @@ struct F32Smem {
   }
 };
 
-template <int D, int RB, int TG, int NST, int MODE, bool ONE = false>
-__global__ __launch_bounds__(RB * TG * 64) void attn_partial_f32(AttnParams p) {
+template <int D, int RB, int TG, int NST, int MODE, bool ONE = false, bool MASS = false>
+__global__ __launch_bounds__(RB * TG * 64) void attn_partial_f32(ParamsOf<MASS> p) {
+  static_assert(!MASS || (MODE < 2 && !ONE), "weights are summed over contiguous caches");
   constexpr bool APPEND = MODE == 1, PAGED = MODE == 2;
   using SM = F32Smem<D, TG, NST>;
   constexpr int WAVES = RB * TG;
@@ -775,6 +798,9 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_partial_f32(AttnParams p) {
       for (int e = 0; e < 4; ++e)
         if (n0 + 4 * g + e > lim) sv[e] = -INFINITY;
     }
+    if constexpr (MASS)
+      if (row < p.R)
+        *(f32x4*)(p.logits + (((long long)b * p.Hkv + hk) * p.R + row) * p.logits_ld + n0 + 4 * g) = (f32x4){sv[0], sv[1], sv[2], sv[3]};
     const float mx = rows4_max(max_nan_of(sv)) * p.scale_log2;
     const bool up = mx > m_run + kRescaleGap;          // lazy reference, as in attn_partial_grid
     if (__any(up)) {
@@ -864,6 +890,96 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_partial_f32(AttnParams p) {
 }
 
 // =================================================================================================
+// Attention mass: mass_out[n] = (n < ctx_len ? mass_in[n] : 0) + sum over the KV head's rows of 2^(z - m*) / l*
+// A row's weights need its statistics over the whole cache, which are known once every slice is done: the launch that merges the
+// slices is the first that can sum them.  Its blocks in front take the tokens (kMassTile each), the others merge a row each.
+// l* sums the probabilities as they are: the output's denominator, of those rounded to bf16, is off by up to 2^-9 where one
+// token has most of the weight, and so would the weights be.
+// The logits z come either from memory, where the slices left them (8 bytes a row and token, written and read: fewer than a row
+// of K has, for few rows), or from K again.
+// =================================================================================================
+constexpr int kMassTile = 256;
+constexpr int kMassRows = 16;          // rows whose statistics are merged at a time
+
+// m* and 1 / l* of the KV head's rows r0 .. r0 + kMassRows - 1 into LDS, by all 256 threads: 16 rows x 16 groups of slices
+__device__ __forceinline__ void mass_stats(const MassParams& p, int b, int hk, int r0, float* row_m, float* row_inv) {
+  __shared__ float sm[16][kMassRows], sl[16][kMassRows];
+  const int tid = threadIdx.x, j = tid & 15, grp = tid >> 4;
+  const int r = min(r0 + j, p.R - 1);
+  const long long at = ((long long)b * p.Hkv + hk) * p.S * p.R + r;
+  float m = -INFINITY, l = 0.f;
+  for (int s = grp; s < p.S; s += 16) {
+    const float ms = p.part_m[at + (long long)s * p.R], ls = p.part_f[at + (long long)s * p.R];
+    const float mm = max_nan(m, ms);
+    // (a slice without a finite logit has nothing to add)
+    l = (m == -INFINITY ? 0.f : l * fast_exp2(m - mm)) + (ms == -INFINITY ? 0.f : ls * fast_exp2(ms - mm));
+    m = mm;
+  }
+  sm[grp][j] = m;
+  sl[grp][j] = l;
+  __syncthreads();
+  if (tid < kMassRows) {
+    float mm = sm[0][tid], ll = 0.f;
+#pragma unroll
+    for (int g = 1; g < 16; ++g) mm = max_nan(mm, sm[g][tid]);
+#pragma unroll
+    for (int g = 0; g < 16; ++g) ll += sm[g][tid] == -INFINITY ? 0.f : sl[g][tid] * fast_exp2(sm[g][tid] - mm);
+    row_m[tid] = mm;
+    row_inv[tid] = r0 + tid < p.R ? 1.f / ll : 0.f;
+  }
+  __syncthreads();
+}
+
+// the weight of a token from its logit; fp32 rounds product and sum one by one, as its slices do
+template <bool F32>
+__device__ __forceinline__ float weight_of(float z, float scale_log2, float m) {
+  if constexpr (F32) {
+#pragma clang fp contract(off)
+    return fast_exp2(z * scale_log2 - m);
+  } else {
+    return fast_exp2(fmaf(z, scale_log2, -m));
+  }
+}
+
+// kMassTile tokens from logits in memory: a wave takes every fourth row, four tokens a lane
+template <bool F32>
+__device__ __forceinline__ void mass_tile(const MassParams& p, int tile, int hk, int b) {
+  __shared__ float row_m[kMassRows], row_inv[kMassRows];
+  __shared__ f32x4 part[4][64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int n = tile * kMassTile + tid;
+  float* out = p.mass_out + b * p.mass_osb + hk * p.mass_osh;
+  float before = 0.f;
+  if (n < p.ctx_len && p.mass_in != nullptr) before = p.mass_in[b * p.mass_isb + hk * p.mass_ish + n];
+  const int n4 = min(tile * kMassTile + lane * 4, p.logits_ld - 4);       // (past the row's end: a repeat, not stored)
+  const float* z0 = p.logits + ((long long)b * p.Hkv + hk) * p.R * p.logits_ld + n4;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int r0 = 0; r0 < p.R; r0 += kMassRows) {
+    f32x4 z[kMassRows / 4];
+#pragma unroll
+    for (int u = 0; u < kMassRows / 4; ++u) z[u] = *(const f32x4*)(z0 + (long long)min(r0 + wave + 4 * u, p.R - 1) * p.logits_ld);
+    mass_stats(p, b, hk, r0, row_m, row_inv);
+#pragma unroll
+    for (int u = 0; u < kMassRows / 4; ++u) {
+      if (r0 + wave + 4 * u >= p.R) break;
+      const float m = row_m[wave + 4 * u], inv = row_inv[wave + 4 * u];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] = fmaf(weight_of<F32>(z[u][e], p.scale_log2, m), inv, sum[e]);
+    }
+    __syncthreads();               // before the next rows' statistics
+  }
+  part[wave][lane] = sum;
+  __syncthreads();
+  if (n < p.n_total) {
+    const float* at = (const float*)part + tid;
+    out[n] = before + ((at[0] + at[256]) + (at[512] + at[768]));
+  }
+}
+
+__device__ __forceinline__ int mass_tiles_of(const AttnParams&) { return 0; }
+__device__ __forceinline__ int mass_tiles_of(const MassParams& p) { return p.mass_tiles; }
+
+// =================================================================================================
 // Merge of the KV slices: out = sum_s 2^(m_s - m*) o_s / sum_s 2^(m_s - m*) l_s
 // The slices' outputs o_s are fp32 (the fp32 kernel's), bf16 (the bf16 kernel's) or, of its blocks of more than 64 rows, fp16
 // with a factor, or bf16 with -1 in its place.
@@ -903,15 +1019,20 @@ __device__ __forceinline__ f32x4 part_o_weighed(f32x4 raw, float weight, float f
   }
 }
 
-template <typename T, int D, int PO>
-__global__ __launch_bounds__(256) void attn_combine(AttnParams p) {
+template <typename T, int D, int PO, bool MASS = false>
+__global__ __launch_bounds__(256) void attn_combine(ParamsOf<MASS> p) {
+  if constexpr (MASS)
+    if ((int)blockIdx.x < p.mass_tiles) {
+      mass_tile<sizeof(T) == 4>(p, blockIdx.x, blockIdx.y, blockIdx.z);
+      return;
+    }
   constexpr int VPR = D / 4;           // four-element vectors per row
   constexpr int NSG = 256 / VPR;       // slice groups
   __shared__ float w_s[kMaxSplits];
   __shared__ float red[8];
   __shared__ f32x4 acc_s[NSG][VPR];
 
-  const int r = blockIdx.x, hk = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
+  const int r = MASS ? blockIdx.x - mass_tiles_of(p) : blockIdx.x, hk = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
   const long long slot0 = ((long long)b * p.Hkv + hk) * p.S;
   const int vec = tid % VPR, sg = tid / VPR;
 
@@ -1021,7 +1142,7 @@ __global__ __launch_bounds__(256) void attn_combine(AttnParams p) {
 // =================================================================================================
 // Lets KERNEL use `smem` bytes of dynamic LDS.  The attribute belongs to a (kernel, device) pair: it is set once for
 // each device this process uses.
-template <void (*KERNEL)(AttnParams)>
+template <auto KERNEL>
 static hipError_t allow_dynamic_lds(int smem) {
   static std::atomic<unsigned long long> attr_set{0};
   int dev = 0;
@@ -1037,28 +1158,30 @@ static hipError_t allow_dynamic_lds(int smem) {
 }
 
 template <int D, int RB, int TG, int TT, int NST, int MODE, bool KV8 = false, bool NT = false, bool ROT = false,
-          bool ONE = false>
-static hipError_t launch_grid_mode(const AttnParams& p, hipStream_t st) {
-  // the paged variant keeps its slice of the page table behind the ring
-  constexpr int smem = GridSmem<D, TG, TT, NST, KV8 ? 1 : 2>::total(RB) + (MODE == 2 ? kMaxSlicePages * 4 : 0);
-  const hipError_t e = allow_dynamic_lds<attn_partial_grid<D, RB, TG, TT, NST, MODE, KV8, NT, ROT, ONE>>(smem);
+          bool ONE = false, bool MASS = false>
+static hipError_t launch_grid_mode(const ParamsOf<MASS>& p, hipStream_t st) {
+  // the paged variant keeps its slice of the page table behind the ring, the one for attention mass its denominators
+  constexpr int smem = GridSmem<D, TG, TT, NST, KV8 ? 1 : 2>::total(RB) + (MODE == 2 ? kMaxSlicePages * 4 : 0) +
+                       (MASS ? TG * RB * 16 * 4 : 0);
+  const hipError_t e = allow_dynamic_lds<attn_partial_grid<D, RB, TG, TT, NST, MODE, KV8, NT, ROT, ONE, MASS>>(smem);
   if (e != hipSuccess) return e;
   dim3 grid(p.S, p.Hkv, p.B * p.n_chunks);
-  AttnParams q = p;                               // the slices' tile counts for this kernel's tile size
+  ParamsOf<MASS> q = p;                           // the slices' tile counts for this kernel's tile size
   const int n_tiles = (p.n_total + TT - 1) / TT;
   q.tiles_q = n_tiles / p.S;
   q.tiles_r = n_tiles % p.S;
-  hipLaunchKernelGGL((attn_partial_grid<D, RB, TG, TT, NST, MODE, KV8, NT, ROT, ONE>), grid, dim3(RB * TG * 64), smem, st, q);
+  hipLaunchKernelGGL((attn_partial_grid<D, RB, TG, TT, NST, MODE, KV8, NT, ROT, ONE, MASS>), grid, dim3(RB * TG * 64), smem, st, q);
   return hipGetLastError();
 }
 
 // the appended-row and paged variants are separate instantiations, so the plain call carries none of
 // their address selects
-template <int D, int RB, int TG, int TT, int NST, bool NT = false, bool ROT = false, bool ONE = false>
-static hipError_t launch_grid(const AttnParams& p, hipStream_t st) {
-  if (p.block_table != nullptr) return launch_grid_mode<D, RB, TG, TT, NST, 2, false, NT, ROT, ONE>(p, st);
-  if (p.k_new != nullptr) return launch_grid_mode<D, RB, TG, TT, NST, 1, false, NT, ROT, ONE>(p, st);
-  return launch_grid_mode<D, RB, TG, TT, NST, 0, false, NT, ROT, ONE>(p, st);
+template <int D, int RB, int TG, int TT, int NST, bool NT = false, bool ROT = false, bool ONE = false, bool MASS = false>
+static hipError_t launch_grid(const ParamsOf<MASS>& p, hipStream_t st) {
+  if constexpr (!MASS)
+    if (p.block_table != nullptr) return launch_grid_mode<D, RB, TG, TT, NST, 2, false, NT, ROT, ONE>(p, st);
+  if (p.k_new != nullptr) return launch_grid_mode<D, RB, TG, TT, NST, 1, false, NT, ROT, ONE, MASS>(p, st);
+  return launch_grid_mode<D, RB, TG, TT, NST, 0, false, NT, ROT, ONE, MASS>(p, st);
 }
 
 // Up to 16 query rows and one slice of a short cache (the library's choice up to 256 rows, 128 in fp32): the block
@@ -1076,8 +1199,8 @@ static bool stream_exceeds_caches(const AttnParams& p, int head_dim, int elem_by
 
 // Short slices (a block owns only a handful of tiles, as at 16K context on 256 compute units) use
 // 16-token tiles and a deeper ring; long slices use 32-token tiles, which halve the barrier count.
-template <int D, int RB>
-static hipError_t launch_grid_rb(const AttnParams& p, hipStream_t st) {
+template <int D, int RB, bool MASS = false>
+static hipError_t launch_grid_rb(const ParamsOf<MASS>& p, hipStream_t st) {
   const int tiles32_per_block = ((p.n_total + 31) / 32) / (p.S > 0 ? p.S : 1);
   const bool small_tiles = tiles32_per_block < 24;
   if (!small_tiles) {
@@ -1095,8 +1218,8 @@ static hipError_t launch_grid_rb(const AttnParams& p, hipStream_t st) {
     // layers (2 x 8 x 128 x 20K, 72 rows 53.1 -> 46.9; 33K x 4 heads from 24.5 to 23.7), and cost as much when it does, as in
     // calls over one layer (34.9 -> 42.2; 20.4 -> 22.4; 64 channels x 20K, 104 rows 28.7 -> 32.8): there the 32-token tiles stay.
     if constexpr (RB == 3 || (RB == 4 && D == 64))
-      if (nt && (D == 64 ? RB == 3 || p.n_chunks == 1 : p.n_chunks > 1)) return launch_grid<D, RB, 4, 16, 4, true, true>(p, st);
-    return nt ? launch_grid<D, RB, 4, 32, 2, true, true>(p, st) : launch_grid<D, RB, 4, 32, 2, false, true>(p, st);
+      if (nt && (D == 64 ? RB == 3 || p.n_chunks == 1 : p.n_chunks > 1)) return launch_grid<D, RB, 4, 16, 4, true, true, false, MASS>(p, st);
+    return nt ? launch_grid<D, RB, 4, 32, 2, true, true, false, MASS>(p, st) : launch_grid<D, RB, 4, 32, 2, false, true, false, MASS>(p, st);
   }
   // measured at the 16K configuration: with 3-4 row blocks, two token groups and a four-stage ring
   // (the whole slice in flight at once) beat four groups by ~8 %; the block merge moves half the data
@@ -1105,11 +1228,12 @@ static hipError_t launch_grid_rb(const AttnParams& p, hipStream_t st) {
   // rows, us a call: 33K 19.6 -> 18.9, 40K 21.2 -> 20.9; at 26K, 12 tiles, 16.2 against 16.4; two chunks of 48, 84 rows at 16K
   // 17.6 -> 16.1, so two chunks take them from 12 tiles on as well, caches not in the last-level cache: 91 rows, 16000 tokens
   // 18.6 -> 17.0, chunks of 64 and a rest 18.4; 12500 tokens, 12 tiles, 15.7 against 16.7; 2 x 7000 16.1 against 17.4)
-  if (RB >= 3 && tiles32_per_block >= (RB == 4 || p.n_chunks > 1 ? 12 : 16)) return launch_grid<D, RB, 2, 32, 3>(p, st);
-  if (RB >= 3) return launch_grid<D, RB, 2, 16, 4>(p, st);
-  if constexpr (RB == 1)
+  if (RB >= 3 && tiles32_per_block >= (RB == 4 || p.n_chunks > 1 ? 12 : 16))
+    return launch_grid<D, RB, 2, 32, 3, false, false, false, MASS>(p, st);
+  if (RB >= 3) return launch_grid<D, RB, 2, 16, 4, false, false, false, MASS>(p, st);
+  if constexpr (RB == 1 && !MASS)
     if (one_slice_call(p)) return launch_grid<D, RB, 4, 16, 3, false, false, true>(p, st);
-  return launch_grid<D, RB, 4, 16, 3>(p, st);
+  return launch_grid<D, RB, 4, 16, 3, false, false, false, MASS>(p, st);
 }
 
 // 65 to 96 rows in one block (plan_attention says when; the cache exceeds the last-level cache): twelve waves in two token
@@ -1143,51 +1267,56 @@ static hipError_t launch_kv8_d(const AttnParams& p, hipStream_t st) {
   }
 }
 
-template <int D>
-static hipError_t launch_mfma_d(const AttnParams& p, hipStream_t st) {
+template <int D, bool MASS = false>
+static hipError_t launch_mfma_d(const ParamsOf<MASS>& p, hipStream_t st) {
   switch (p.row_chunk / 16) {
-    case 1: return launch_grid_rb<D, 1>(p, st);
-    case 2: return launch_grid_rb<D, 2>(p, st);
-    case 3: return launch_grid_rb<D, 3>(p, st);
-    case 4: return launch_grid_rb<D, 4>(p, st);
-    case 6: return launch_grid_wide<D>(p, st);
+    case 1: return launch_grid_rb<D, 1, MASS>(p, st);
+    case 2: return launch_grid_rb<D, 2, MASS>(p, st);
+    case 3: return launch_grid_rb<D, 3, MASS>(p, st);
+    case 4: return launch_grid_rb<D, 4, MASS>(p, st);
+    case 6:
+      if constexpr (!MASS) return launch_grid_wide<D>(p, st);
     default: return hipErrorInvalidValue;
   }
 }
 
-template <int D, int RB, int TG, int NST, int MODE, bool ONE>
-static hipError_t launch_f32_mode(const AttnParams& p, hipStream_t st) {
+template <int D, int RB, int TG, int NST, int MODE, bool ONE, bool MASS>
+static hipError_t launch_f32_mode(const ParamsOf<MASS>& p, hipStream_t st) {
   constexpr int smem = F32Smem<D, TG, NST>::total(RB) + (MODE == 2 ? kMaxSlicePages * 4 : 0);
-  const hipError_t e = allow_dynamic_lds<attn_partial_f32<D, RB, TG, NST, MODE, ONE>>(smem);
+  const hipError_t e = allow_dynamic_lds<attn_partial_f32<D, RB, TG, NST, MODE, ONE, MASS>>(smem);
   if (e != hipSuccess) return e;
-  AttnParams q = p;
+  ParamsOf<MASS> q = p;
   const int n_tiles = (p.n_total + 15) / 16;
   q.tiles_q = n_tiles / p.S;
   q.tiles_r = n_tiles % p.S;
-  hipLaunchKernelGGL((attn_partial_f32<D, RB, TG, NST, MODE, ONE>), dim3(p.S, p.Hkv, p.B * p.n_chunks), dim3(RB * TG * 64),
+  hipLaunchKernelGGL((attn_partial_f32<D, RB, TG, NST, MODE, ONE, MASS>), dim3(p.S, p.Hkv, p.B * p.n_chunks), dim3(RB * TG * 64),
                      smem, st, q);
   return hipGetLastError();
 }
 
-template <int D, int RB, int TG, int NST, bool ONE = false>
-static hipError_t launch_f32(const AttnParams& p, hipStream_t st) {
-  if (p.block_table != nullptr) return launch_f32_mode<D, RB, TG, NST, 2, ONE>(p, st);
-  if (p.k_new != nullptr) return launch_f32_mode<D, RB, TG, NST, 1, ONE>(p, st);
-  return launch_f32_mode<D, RB, TG, NST, 0, ONE>(p, st);
+template <int D, int RB, int TG, int NST, bool ONE = false, bool MASS = false>
+static hipError_t launch_f32(const ParamsOf<MASS>& p, hipStream_t st) {
+  if constexpr (!MASS)
+    if (p.block_table != nullptr) return launch_f32_mode<D, RB, TG, NST, 2, ONE, false>(p, st);
+  if (p.k_new != nullptr) return launch_f32_mode<D, RB, TG, NST, 1, ONE, MASS>(p, st);
+  return launch_f32_mode<D, RB, TG, NST, 0, ONE, MASS>(p, st);
 }
 
 // row blocks x token groups: four groups while LDS and sixteen waves allow them
-template <int D>
-static hipError_t launch_f32_d(const AttnParams& p, hipStream_t st) {
+template <int D, bool MASS = false>
+static hipError_t launch_f32_d(const ParamsOf<MASS>& p, hipStream_t st) {
   // ring stages: what 160 KB of LDS hold beside the queries
   constexpr bool W = D == 128;
   switch (p.row_chunk / 16) {
-    case 1: return one_slice_call(p) ? launch_f32<D, 1, 4, W ? 2 : 4, true>(p, st) : launch_f32<D, 1, 4, W ? 2 : 4>(p, st);
-    case 2: return launch_f32<D, 2, 4, W ? 2 : 4>(p, st);
-    case 3: return launch_f32<D, 3, 4, W ? 2 : 4>(p, st);
-    case 4: return launch_f32<D, 4, W ? 2 : 4, W ? 3 : 4>(p, st);
-    case 6: return launch_f32<D, 6, 2, W ? 3 : 4>(p, st);
-    case 8: return launch_f32<D, 8, 2, W ? 2 : 4>(p, st);
+    case 1:
+      if constexpr (!MASS)
+        if (one_slice_call(p)) return launch_f32<D, 1, 4, W ? 2 : 4, true>(p, st);
+      return launch_f32<D, 1, 4, W ? 2 : 4, false, MASS>(p, st);
+    case 2: return launch_f32<D, 2, 4, W ? 2 : 4, false, MASS>(p, st);
+    case 3: return launch_f32<D, 3, 4, W ? 2 : 4, false, MASS>(p, st);
+    case 4: return launch_f32<D, 4, W ? 2 : 4, W ? 3 : 4, false, MASS>(p, st);
+    case 6: return launch_f32<D, 6, 2, W ? 3 : 4, false, MASS>(p, st);
+    case 8: return launch_f32<D, 8, 2, W ? 2 : 4, false, MASS>(p, st);
     default: return hipErrorInvalidValue;
   }
 }
@@ -1211,6 +1340,27 @@ hipError_t launch_attention(const AttnParams& p, int dtype, int head_dim, hipStr
   e = (head_dim == 128) ? launch_f32_d<128>(p, st) : launch_f32_d<64>(p, st);
   if (e != hipSuccess || one_slice_call(p)) return e;
   return (head_dim == 128) ? launch_combine<float, 128, kPartF32>(p, st) : launch_combine<float, 64, kPartF32>(p, st);
+}
+
+template <typename T, int D, int PO>
+static hipError_t launch_combine_mass(const MassParams& p, hipStream_t st) {
+  MassParams q = p;
+  q.mass_tiles = (p.n_total + kMassTile - 1) / kMassTile;
+  hipLaunchKernelGGL((attn_combine<T, D, PO, true>), dim3(q.mass_tiles + p.R, p.Hkv, p.B), dim3(256), 0, st, q);
+  return hipGetLastError();
+}
+
+hipError_t launch_attention_mass(const MassParams& p, int dtype, int head_dim, hipStream_t st) {
+  hipError_t e;
+  if (dtype == HIPPO_DTYPE_BF16) {
+    e = (head_dim == 128) ? launch_mfma_d<128, true>(p, st) : launch_mfma_d<64, true>(p, st);
+    if (e != hipSuccess) return e;
+    return (head_dim == 128) ? launch_combine_mass<uint16_t, 128, kPartF32>(p, st)
+                             : launch_combine_mass<uint16_t, 64, kPartF32>(p, st);
+  }
+  e = (head_dim == 128) ? launch_f32_d<128, true>(p, st) : launch_f32_d<64, true>(p, st);
+  if (e != hipSuccess) return e;
+  return (head_dim == 128) ? launch_combine_mass<float, 128, kPartF32>(p, st) : launch_combine_mass<float, 64, kPartF32>(p, st);
 }
 
 }  // namespace hippo

@@ -37,7 +37,8 @@ namespace {
   X(hippo_verify_attention_fp8kv) X(hippo_draft_attention_fp8kv) X(hippo_quantize_kv_workspace_bytes)                   \
   X(hippo_quantize_kv_e4m3) X(hippo_spec_verify_workspace_bytes) X(hippo_spec_verify)                   \
   X(hippo_token_logprobs_workspace_bytes) X(hippo_token_logprobs)                 \
-  X(hippo_evict_kv_workspace_bytes) X(hippo_evict_kv)
+  X(hippo_evict_kv_workspace_bytes) X(hippo_evict_kv) X(hippo_attention_mass_workspace_bytes)                      \
+  X(hippo_verify_attention_mass) X(hippo_draft_attention_mass)
 struct Library {
 #define X(name) decltype(&::name) name;
   HIPPO_LIBRARY(X)
@@ -400,6 +401,45 @@ PyObject* attention(PyObject* const* a) {
   return c.result();
 }
 
+// draft, q, k_cache, v_cache, mass, ctx_len, softmax_scale, num_splits, want_lse, out, mass_out, workspace, k_new, v_new
+PyObject* attention_mass(PyObject* const* a) {
+  AttentionCall c(a[0], a[1], a[5], a[6], a[7]);
+  const Tensor &k = tensor(a[2]), &v = tensor(a[3]);
+  const Tensor mass = tensor_or_none(a[4]), k_new = tensor_or_none(a[12]), v_new = tensor_or_none(a[13]);
+  const hippo_kv_desc kv = describe(k, c.q.size(2));
+  const long long B = k.size(0), Hkv = k.size(1), n = c.ctx_len + c.q.size(1);
+  REQUIRE(same_layout(v, k) && v.scalar_type() == k.scalar_type() && c.q.scalar_type() == k.scalar_type());
+  REQUIRE(c.q.size(0) == B && c.q.size(3) == k.size(3) && c.ctx_len >= 0 && n <= k.size(2) && c.q.size(1) >= 1);
+  if (mass.defined()) require_mass(mass, B, Hkv, c.ctx_len);
+  Tensor mass_out = tensor_or_none(a[10]);
+  if (!mass_out.defined()) mass_out = empty({B, Hkv, n}, at::kFloat, c.q);
+  require_mass(mass_out, B, Hkv, n);
+  c.out = output(a[9], c.q.sizes(), c.q.scalar_type(), c.q);
+  if (truth(a[8])) c.lse = empty({B, c.q.size(2), c.q.size(1)}, at::kFloat, c.q);
+  c.ws = workspace(a[11], c.q, [&] {
+    return lib.hippo_attention_mass_workspace_bytes(&kv, c.q_len(), (int32_t)n, (int32_t)c.num_splits);
+  });
+  REQUIRE(k_new.defined() == v_new.defined());
+  if (k_new.defined())
+    for (const Tensor* t : {&k_new, &v_new})
+      REQUIRE(t->sizes() == at::IntArrayRef({B, c.q.size(1), Hkv, k.size(3)}) && t->is_contiguous() && t->scalar_type() == k.scalar_type());
+  hippo_mass_desc m{};
+  m.in = ptr<const float>(mass);
+  m.out = ptr<float>(mass_out);
+  if (mass.defined()) {
+    m.in_stride_b = mass.stride(0);
+    m.in_stride_h = mass.stride(1);
+  }
+  m.out_stride_b = mass_out.stride(0);
+  m.out_stride_h = mass_out.stride(1);
+  require_here({&c.q, &k, &v, &mass, &mass_out, &c.out, &c.lse, &c.ws, &k_new, &v_new});
+  check(unlocked(c.draft() ? lib.hippo_draft_attention_mass : lib.hippo_verify_attention_mass, ptr<const void>(c.q), c.q_len(),
+                 ptr<const void>(k_new), ptr<const void>(v_new), ptr(k), ptr(v), &kv, (int32_t)c.ctx_len, c.scale,
+                 (int32_t)c.num_splits, ptr(c.out), ptr<float>(c.lse), &m, ptr(c.ws), (size_t)c.ws.numel(), stream()),
+        c.draft() ? "hippo_draft_attention_mass" : "hippo_verify_attention_mass");
+  return c.lse.defined() ? tuple({wrap(c.out), wrap(mass_out), wrap(c.lse)}) : tuple({wrap(c.out), wrap(mass_out)});
+}
+
 // draft, q, k_codes, v_codes, k_scale, v_scale, ctx_len, softmax_scale, num_splits, want_lse, out, workspace
 PyObject* attention_fp8kv(PyObject* const* a) {
   AttentionCall c(a[0], a[1], a[6], a[7], a[8]);
@@ -606,7 +646,7 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #define ENTRY(name, n) {#name, (PyCFunction)(void (*)(void))entry<name, n>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     ENTRY(bind, 3), ENTRY(score_tokens, 9), ENTRY(score_tokens_layers, 10), ENTRY(select_gather, 11), ENTRY(attention, 12),
-    ENTRY(attention_fp8kv, 12), ENTRY(attention_paged, 11), ENTRY(quantize, 6), ENTRY(spec_verify, 10), ENTRY(token_logprobs, 9), ENTRY(evict, 12),
+    ENTRY(attention_fp8kv, 12), ENTRY(attention_paged, 11), ENTRY(quantize, 6), ENTRY(spec_verify, 10), ENTRY(token_logprobs, 9), ENTRY(evict, 12), ENTRY(attention_mass, 14),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -286,8 +286,24 @@ struct AttnParams {
 };
 constexpr int kMaxSlicePages = 1024;   // page-table entries a block stages in LDS
 
+
+// The call that also sums its weights.  (Its arguments are its own: among AttnParams' every kernel would fetch them.)
+struct MassParams : AttnParams {
+  float* part_f;            // [B, Hkv, S, R] partial denominators of the unrounded probabilities
+  float* logits;            // [B, Hkv, R, logits_ld] q . k, -inf behind a row's last token; null: the merge works them out again
+  int logits_ld;
+  int mass_tiles;           // blocks of a KV head's tokens in the merge (set by its launcher)
+  const float* mass_in;     // may be null; element (b, hk, n) at b * mass_isb + hk * mass_ish + n
+  float* mass_out;
+  long long mass_isb, mass_ish, mass_osb, mass_osh;
+};
+template <bool MASS> struct ParamsChoice { using type = AttnParams; };
+template <> struct ParamsChoice<true> { using type = MassParams; };
+template <bool MASS> using ParamsOf = typename ParamsChoice<MASS>::type;
+
 // Launchers, one per translation unit.  All return a hipError_t from hipGetLastError().
 hipError_t launch_attention(const AttnParams& p, int dtype, int head_dim, hipStream_t st);
+hipError_t launch_attention_mass(const MassParams& p, int dtype, int head_dim, hipStream_t st);
 
 constexpr int kMaxScoreLayers = 64;   // layers whose s_attn sweeps can share one launch
 
