@@ -404,7 +404,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_partial_grid(ParamsOf<MASS>
           if ((n0 + (KV8 ? 8 * g + 4 * tb : tb * 16 + 4 * g) + e) > lim) s[tb][e] = -INFINITY;
     }
     if constexpr (MASS)
-      if (p.logits != nullptr && row < p.R) {
+      if (row < p.R) {
         float* at = p.logits + (((long long)b * p.Hkv + hk) * p.R + row) * p.logits_ld + n0 + 4 * g;
 #pragma unroll
         for (int tb = 0; tb < TB; ++tb) *(f32x4*)(at + tb * 16) = s[tb];
@@ -895,41 +895,15 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_partial_f32(ParamsOf<MASS> 
 // slices is the first that can sum them.  Its blocks in front take the tokens (kMassTile each), the others merge a row each.
 // l* sums the probabilities as they are: the output's denominator, of those rounded to bf16, is off by up to 2^-9 where one
 // token has most of the weight, and so would the weights be.
-// The logits z come either from memory, where the slices left them (8 bytes a row and token, written and read: fewer than a row
-// of K has, for few rows), or from K again.
+// The logits z are in memory, where the slices left them: 8 bytes a row and token, written and read, where K again would be 2 D and
+// another set of products.  us a call, logits -> K again: 16640 x 4 heads x 128, 21 rows 17.2 -> 19.6, 42 rows 21.5 -> 20.4, 63 rows
+// 23.2 -> 22.7, 4 x 8 x 37000, 48 rows 200 -> 195: not worth the second kernel.  What the stores cost the slices is not the bytes
+// alone: a stream that only reads runs at 6.7 TB/s here, one that writes a little at 5.4 (4 x 8 x 37120, 8 rows 90 -> 121 us, 113
+// with stores that stay in the L2, whatever the order of stores and transfers and the depth of the ring).
+// kMassTile tokens a block, ROWS rows' logits and statistics asked for together: 16640 x 4, 42 rows 10.1 -> 5.9 us against 16 rows
+// at a time, each after the one before.
 // =================================================================================================
 constexpr int kMassTile = 256;
-constexpr int kMassRows = 16;          // rows whose statistics are merged at a time
-
-// m* and 1 / l* of the KV head's rows r0 .. r0 + kMassRows - 1 into LDS, by all 256 threads: 16 rows x 16 groups of slices
-__device__ __forceinline__ void mass_stats(const MassParams& p, int b, int hk, int r0, float* row_m, float* row_inv) {
-  __shared__ float sm[16][kMassRows], sl[16][kMassRows];
-  const int tid = threadIdx.x, j = tid & 15, grp = tid >> 4;
-  const int r = min(r0 + j, p.R - 1);
-  const long long at = ((long long)b * p.Hkv + hk) * p.S * p.R + r;
-  float m = -INFINITY, l = 0.f;
-  for (int s = grp; s < p.S; s += 16) {
-    const float ms = p.part_m[at + (long long)s * p.R], ls = p.part_f[at + (long long)s * p.R];
-    const float mm = max_nan(m, ms);
-    // (a slice without a finite logit has nothing to add)
-    l = (m == -INFINITY ? 0.f : l * fast_exp2(m - mm)) + (ms == -INFINITY ? 0.f : ls * fast_exp2(ms - mm));
-    m = mm;
-  }
-  sm[grp][j] = m;
-  sl[grp][j] = l;
-  __syncthreads();
-  if (tid < kMassRows) {
-    float mm = sm[0][tid], ll = 0.f;
-#pragma unroll
-    for (int g = 1; g < 16; ++g) mm = max_nan(mm, sm[g][tid]);
-#pragma unroll
-    for (int g = 0; g < 16; ++g) ll += sm[g][tid] == -INFINITY ? 0.f : sl[g][tid] * fast_exp2(sm[g][tid] - mm);
-    row_m[tid] = mm;
-    row_inv[tid] = r0 + tid < p.R ? 1.f / ll : 0.f;
-  }
-  __syncthreads();
-}
-
 // the weight of a token from its logit; fp32 rounds product and sum one by one, as its slices do
 template <bool F32>
 __device__ __forceinline__ float weight_of(float z, float scale_log2, float m) {
@@ -941,10 +915,64 @@ __device__ __forceinline__ float weight_of(float z, float scale_log2, float m) {
   }
 }
 
-// kMassTile tokens from logits in memory: a wave takes every fourth row, four tokens a lane
-template <bool F32>
+// m* and 1 / l* of the KV head's rows r0 .. r0 + ROWS - 1 into LDS, by all 256 threads: ROWS rows x 256 / ROWS groups of slices.
+// fetch() asks for the first PF slices of every group, finish() merges.
+template <int ROWS>
+struct MassStats {
+  static constexpr int GROUPS = 256 / ROWS, PF = 64 / GROUPS;       // up to 64 slices are fetched at once
+  const float *m_at, *l_at;
+  int row;
+  float ms[PF], ls[PF];
+  __device__ __forceinline__ void fetch(const MassParams& p, int b, int hk, int r0) {
+    const long long at = ((long long)b * p.Hkv + hk) * p.S * p.R;   // (uniform: a lane adds 32 bits, as 1024 slices x 4096 rows need)
+    m_at = p.part_m + at;
+    l_at = p.part_f + at;
+    row = min(r0 + (int)threadIdx.x % ROWS, p.R - 1);
+    const int grp = threadIdx.x / ROWS;
+#pragma unroll
+    for (int u = 0; u < PF; ++u) {
+      const unsigned i = (unsigned)(min(grp + u * GROUPS, p.S - 1) * p.R + row);   // past the last slice: a repeat, not used
+      ms[u] = m_at[i];
+      ls[u] = l_at[i];
+    }
+  }
+  __device__ __forceinline__ void finish(const MassParams& p, int r0, float* row_m, float* row_inv) {
+    __shared__ float sm[GROUPS][ROWS], sl[GROUPS][ROWS];
+    const int tid = threadIdx.x, j = tid % ROWS, grp = tid / ROWS;
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int u = 0; u < PF; ++u)
+      if (grp + u * GROUPS < p.S) m = max_nan(m, ms[u]);
+    // (a slice without a finite logit has nothing to add)
+#pragma unroll
+    for (int u = 0; u < PF; ++u)
+      if (grp + u * GROUPS < p.S && ms[u] != -INFINITY) l = fmaf(ls[u], fast_exp2(ms[u] - m), l);
+    for (int s = grp + 64; s < p.S; s += GROUPS) {
+      const float m1 = m_at[(unsigned)(s * p.R + row)], l1 = l_at[(unsigned)(s * p.R + row)], mm = max_nan(m, m1);
+      l = (m == -INFINITY ? 0.f : l * fast_exp2(m - mm)) + (m1 == -INFINITY ? 0.f : l1 * fast_exp2(m1 - mm));
+      m = mm;
+    }
+    sm[grp][j] = m;
+    sl[grp][j] = l;
+    __syncthreads();
+    if (tid < ROWS) {
+      float mm = sm[0][tid], ll = 0.f;
+#pragma unroll
+      for (int g = 1; g < GROUPS; ++g) mm = max_nan(mm, sm[g][tid]);
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g) ll += sm[g][tid] == -INFINITY ? 0.f : sl[g][tid] * fast_exp2(sm[g][tid] - mm);
+      row_m[tid] = mm;
+      row_inv[tid] = r0 + tid < p.R ? 1.f / ll : 0.f;
+    }
+    __syncthreads();
+  }
+};
+
+// kMassTile tokens from logits in memory: a wave takes every fourth row, four tokens a lane.  ROWS rows at a time, whose logits and
+// statistics are asked for together.
+template <bool F32, int ROWS>
 __device__ __forceinline__ void mass_tile(const MassParams& p, int tile, int hk, int b) {
-  __shared__ float row_m[kMassRows], row_inv[kMassRows];
+  __shared__ float row_m[ROWS], row_inv[ROWS];
   __shared__ f32x4 part[4][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n = tile * kMassTile + tid;
@@ -954,19 +982,22 @@ __device__ __forceinline__ void mass_tile(const MassParams& p, int tile, int hk,
   const int n4 = min(tile * kMassTile + lane * 4, p.logits_ld - 4);       // (past the row's end: a repeat, not stored)
   const float* z0 = p.logits + ((long long)b * p.Hkv + hk) * p.R * p.logits_ld + n4;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int r0 = 0; r0 < p.R; r0 += kMassRows) {
-    f32x4 z[kMassRows / 4];
+  MassStats<ROWS> stats;
+  for (int r0 = 0; r0 < p.R; r0 += ROWS) {
+    stats.fetch(p, b, hk, r0);
+    f32x4 z[ROWS / 4];
 #pragma unroll
-    for (int u = 0; u < kMassRows / 4; ++u) z[u] = *(const f32x4*)(z0 + (long long)min(r0 + wave + 4 * u, p.R - 1) * p.logits_ld);
-    mass_stats(p, b, hk, r0, row_m, row_inv);
+    for (int u = 0; u < ROWS / 4; ++u)
+      if (r0 + wave + 4 * u < p.R) z[u] = *(const f32x4*)(z0 + (long long)(r0 + wave + 4 * u) * p.logits_ld);
+    stats.finish(p, r0, row_m, row_inv);
 #pragma unroll
-    for (int u = 0; u < kMassRows / 4; ++u) {
+    for (int u = 0; u < ROWS / 4; ++u) {
       if (r0 + wave + 4 * u >= p.R) break;
       const float m = row_m[wave + 4 * u], inv = row_inv[wave + 4 * u];
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum[e] = fmaf(weight_of<F32>(z[u][e], p.scale_log2, m), inv, sum[e]);
     }
-    __syncthreads();               // before the next rows' statistics
+    if (r0 + ROWS < p.R) __syncthreads();                                 // before the next rows' statistics
   }
   part[wave][lane] = sum;
   __syncthreads();
@@ -1019,11 +1050,12 @@ __device__ __forceinline__ f32x4 part_o_weighed(f32x4 raw, float weight, float f
   }
 }
 
-template <typename T, int D, int PO, bool MASS = false>
-__global__ __launch_bounds__(256) void attn_combine(ParamsOf<MASS> p) {
-  if constexpr (MASS)
+// MASS: rows whose weights a block in front sums at a time; 0: there is no such block
+template <typename T, int D, int PO, int MASS = 0>
+__global__ __launch_bounds__(256) void attn_combine(ParamsOf<(MASS > 0)> p) {
+  if constexpr (MASS > 0)
     if ((int)blockIdx.x < p.mass_tiles) {
-      mass_tile<sizeof(T) == 4>(p, blockIdx.x, blockIdx.y, blockIdx.z);
+      mass_tile<sizeof(T) == 4, MASS>(p, blockIdx.x, blockIdx.y, blockIdx.z);
       return;
     }
   constexpr int VPR = D / 4;           // four-element vectors per row
@@ -1032,7 +1064,7 @@ __global__ __launch_bounds__(256) void attn_combine(ParamsOf<MASS> p) {
   __shared__ float red[8];
   __shared__ f32x4 acc_s[NSG][VPR];
 
-  const int r = MASS ? blockIdx.x - mass_tiles_of(p) : blockIdx.x, hk = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
+  const int r = MASS > 0 ? blockIdx.x - mass_tiles_of(p) : blockIdx.x, hk = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
   const long long slot0 = ((long long)b * p.Hkv + hk) * p.S;
   const int vec = tid % VPR, sg = tid / VPR;
 
@@ -1346,7 +1378,9 @@ template <typename T, int D, int PO>
 static hipError_t launch_combine_mass(const MassParams& p, hipStream_t st) {
   MassParams q = p;
   q.mass_tiles = (p.n_total + kMassTile - 1) / kMassTile;
-  hipLaunchKernelGGL((attn_combine<T, D, PO, true>), dim3(q.mass_tiles + p.R, p.Hkv, p.B), dim3(256), 0, st, q);
+  const dim3 grid(q.mass_tiles + p.R, p.Hkv, p.B);
+  if (p.R <= 16) hipLaunchKernelGGL((attn_combine<T, D, PO, 16>), grid, dim3(256), 0, st, q);
+  else hipLaunchKernelGGL((attn_combine<T, D, PO, 64>), grid, dim3(256), 0, st, q);
   return hipGetLastError();
 }
 

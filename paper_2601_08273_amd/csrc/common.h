@@ -290,7 +290,7 @@ constexpr int kMaxSlicePages = 1024;   // page-table entries a block stages in L
 // The call that also sums its weights.  (Its arguments are its own: among AttnParams' every kernel would fetch them.)
 struct MassParams : AttnParams {
   float* part_f;            // [B, Hkv, S, R] partial denominators of the unrounded probabilities
-  float* logits;            // [B, Hkv, R, logits_ld] q . k, -inf behind a row's last token; null: the merge works them out again
+  float* logits;            // [B, Hkv, R, logits_ld] q . k, -inf behind a row's last token
   int logits_ld;
   int mass_tiles;           // blocks of a KV head's tokens in the merge (set by its launcher)
   const float* mass_in;     // may be null; element (b, hk, n) at b * mass_isb + hk * mass_ish + n
