@@ -120,7 +120,10 @@ __device__ __forceinline__ long long gather_offset(long long row, const SelectPa
 // one scan of the wave totals, per-(chunk, wave) ballots with running totals otherwise.
 // hist: kHistWords of LDS, one histogram per radix pass (12, 12, 8 bits); bin i lives at i + i/64, so that the 64 lanes of
 // the scanning wave, which own runs of 64 consecutive bins, hit different LDS banks.  Nothing reads it once a key is emitted.
-template <int NC, typename Emit>
+// ANY: the scores start anywhere and are any number, as between the first and the recent rows of a head's mass: 16-byte loads that
+// are 4-byte aligned, and the vector that the end cuts is taken from the last four scores (16400 scores a head x 4, 8192 kept: 14.3 ->
+// 12.4 us with them).
+template <int NC, bool ANY = false, typename Emit>
 __device__ __forceinline__ void select_top(const float* sc, const int Nv, const int k, unsigned* const hist, Emit emit) {
   constexpr bool CACHED = NC > 0;
   constexpr int kListCap = kBins;            // candidate list: the first histogram's memory, once its digit is known
@@ -140,7 +143,20 @@ __device__ __forceinline__ void select_top(const float* sc, const int Nv, const 
   auto slot_index = [&](int c) { return wave_first + ((c / VW) * 64 + lane) * VW + c % VW; };
   if (CACHED) {
     const bool vec_ok = (VW == 4) && (Nv % 4 == 0) && ((reinterpret_cast<uintptr_t>(sc) & 15u) == 0);   // block-uniform
-    if (vec_ok) {
+    if (ANY && VW == 4 && Nv >= 4) {
+      typedef __attribute__((aligned(4))) u32x4 u32x4_any;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int first = slot_index(v * VW), cut = first - (Nv - 4);
+        const u32x4 x = *(const u32x4_any*)(sc + min(first, Nv - 4));
+        keys[v * VW] = x.x; keys[v * VW + 1 % VW] = x.y; keys[v * VW + 2 % VW] = x.z; keys[v * VW + 3 % VW] = x.w;
+        if (cut > 0 && cut < 4) {                          // scores Nv - 4 .. Nv - 1 in the places of `first` ..
+          keys[v * VW] = cut == 1 ? x.y : cut == 2 ? x.z : x.w;
+          keys[v * VW + 1 % VW] = cut == 1 ? x.z : x.w;
+          keys[v * VW + 2 % VW] = x.w;
+        }
+      }
+    } else if (vec_ok) {
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         const u32x4 x = *(const u32x4*)(sc + min(slot_index(v * VW), Nv - 4));
@@ -456,18 +472,63 @@ hipError_t launch_select_gather(const SelectParams& p, hipStream_t st) {
 // =================================================================================================
 // Eviction: every KV head of every sequence keeps rows of its own
 // =================================================================================================
-// One block per (KV head, sequence): the indices of the rows that stay, ascending.
-template <int NC>
-__global__ __launch_bounds__(kSelThreads) void evict_select(EvictParams p) {
+// The indices of the rows that stay, ascending, by one block per (KV head, sequence).
+// GATHER: the launch copies the rows too, as topk_select's does.  Grid (H_kv * parts, B): every block of a head selects for itself,
+// keeps the indices in LDS and copies its part of the rows.
+template <int NC, bool GATHER>
+__global__ __launch_bounds__(kSelThreads) void evict_select(EvictParams p, int vpr_shift) {
+  static_assert(NC > 0 || !GATHER, "the indices are in LDS only where the keys are in registers");
   __shared__ unsigned hist[kHistWords];
-  const int hk = blockIdx.x, b = blockIdx.y;
+  const int hk = GATHER ? blockIdx.x % p.Hkv : blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+  const int part = GATHER ? blockIdx.x / p.Hkv : 0, parts = GATHER ? gridDim.x / p.Hkv : 1;
+  const bool writes = part == 0;
+  const float* mass = p.mass + b * p.mass_sb + hk * p.mass_sh;
   int32_t* out = p.idx_out + ((long long)b * p.Hkv + hk) * p.keep;
-  const int recent = p.keep - p.n_first - p.k;
-  for (int i = threadIdx.x; i < p.n_first; i += kSelThreads) out[i] = i;
-  for (int i = threadIdx.x; i < recent; i += kSelThreads) out[p.n_first + p.k + i] = p.n_src - recent + i;
+  const int recent = p.keep - p.n_first - p.k, last = p.n_src - p.keep;      // row j of the recent ones in dst is row last + j
+  if (writes) {
+    for (int i = tid; i < p.n_first; i += kSelThreads) out[i] = i;
+    for (int i = tid; i < recent; i += kSelThreads) out[p.n_first + p.k + i] = p.n_src - recent + i;
+  }
   if (p.k > 0)
-    select_top<NC>(p.mass + b * p.mass_sb + hk * p.mass_sh + p.n_first, p.n_between, p.k, hist,
-                   [&](unsigned at, int index) { out[p.n_first + (int)at] = p.n_first + index; });
+    select_top<NC, true>(mass + p.n_first, p.n_between, p.k, hist, [&](unsigned at, int index) {
+      if (writes) out[p.n_first + (int)at] = p.n_first + index;
+      if (GATHER) hist[at] = (unsigned)index;
+    });
+  if constexpr (GATHER) {
+    __syncthreads();
+    float* mass_dst = p.mass_dst == nullptr ? nullptr : p.mass_dst + b * p.mass_dsb + hk * p.mass_dsh;
+    const char* k_src = (const char*)p.k_src + (b * p.ssb + hk * p.ssh) * p.elem_bytes;
+    const char* v_src = (const char*)p.v_src + (b * p.ssb + hk * p.ssh) * p.elem_bytes;
+    char* k_dst = (char*)p.k_dst + (b * p.dsb + hk * p.dsh) * p.elem_bytes;
+    char* v_dst = (char*)p.v_dst + (b * p.dsb + hk * p.dsh) * p.elem_bytes;
+    const int per_head = p.keep << vpr_shift;
+    constexpr int U = 4;                       // vectors of K and of V in flight per thread
+    for (int e0 = part * kSelThreads + tid; e0 < per_head; e0 += U * parts * kSelThreads) {
+      u32x4 kv[U], vv[U];
+      float m[U] = {};
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int e = min(e0 + u * parts * kSelThreads, per_head - 1);     // past the end: a repeat, not stored
+        const int n = e >> vpr_shift, piece = (e & ((1 << vpr_shift) - 1)) * 16;
+        const int kept = min(max(n - p.n_first, 0), max(p.k - 1, 0));
+        const int from = n < p.n_first ? n : n < p.n_first + p.k ? p.n_first + (int)hist[kept] : n + last;
+        const long long so = (long long)from * p.ssn * p.elem_bytes + piece;
+        kv[u] = *(const u32x4*)(k_src + so);
+        vv[u] = *(const u32x4*)(v_src + so);
+        if (piece == 0 && mass_dst != nullptr) m[u] = mass[from];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int e = e0 + u * parts * kSelThreads;
+        if (e >= per_head) break;
+        const int n = e >> vpr_shift, piece = (e & ((1 << vpr_shift) - 1)) * 16;
+        const long long dof = (long long)n * p.dsn * p.elem_bytes + piece;
+        *(u32x4*)(k_dst + dof) = kv[u];
+        *(u32x4*)(v_dst + dof) = vv[u];
+        if (piece == 0 && mass_dst != nullptr) mass_dst[n] = m[u];
+      }
+    }
+  }
 }
 
 // A thread moves 16 bytes of K and of V of rows that lie `gridDim.x` blocks apart; the first of a row's threads its mass too.
@@ -494,8 +555,19 @@ hipError_t launch_evict(const EvictParams& p, hipStream_t st) {
   const int vpr = p.D * p.elem_bytes / 16;                 // 16-byte vectors per row: 4, 8, 16 or 32
   int vpr_shift = 0;
   while ((1 << vpr_shift) < vpr) ++vpr_shift;
-  const dim3 heads(p.Hkv, p.B);
-#define HIPPO_EVICT(NC_) hipLaunchKernelGGL((evict_select<NC_>), heads, dim3(kSelThreads), 0, st, p)
+  // One launch or two by the rules of launch_select_gather, whose kernels these are but for a selection a head.
+  const long long heads = (long long)p.B * p.Hkv, per_head = (long long)p.keep << vpr_shift;
+  const bool one_launch = p.k_dst != nullptr && n_chunks <= kGatherKeys && p.k <= kHistWords && per_head <= (1ll << 24) &&
+                          per_head * heads <= (128ll << 20) / 64 && heads <= (n_chunks <= kShortKeys ? 2 * kNumCU : kNumCU);
+  const long long parts = one_launch ? std::max<long long>(1, std::min<long long>((per_head + 2 * kSelThreads - 1) / (2 * kSelThreads),
+                                                                                  kNumCU / heads))
+                                     : 1;
+#define HIPPO_EVICT(NC_)                                                                                             \
+  if (one_launch)                                                                                                    \
+    hipLaunchKernelGGL((evict_select<NC_, (NC_ > 0 && NC_ <= kGatherKeys)>), dim3((unsigned)(p.Hkv * parts), p.B),    \
+                       dim3(kSelThreads), 0, st, p, vpr_shift);                                                      \
+  else                                                                                                               \
+    hipLaunchKernelGGL((evict_select<NC_, false>), dim3(p.Hkv, p.B), dim3(kSelThreads), 0, st, p, vpr_shift)
   if (n_chunks <= 2) { HIPPO_EVICT(2); }
   else if (n_chunks <= 4) { HIPPO_EVICT(4); }
   else if (n_chunks <= 8) { HIPPO_EVICT(8); }
@@ -506,7 +578,7 @@ hipError_t launch_evict(const EvictParams& p, hipStream_t st) {
   else { HIPPO_EVICT(0); }
 #undef HIPPO_EVICT
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || (p.k_dst == nullptr && p.mass_dst == nullptr)) return e;
+  if (e != hipSuccess || one_launch || (p.k_dst == nullptr && p.mass_dst == nullptr)) return e;
   const int rows_per_block = 256 >> vpr_shift;
   hipLaunchKernelGGL(evict_gather, dim3((unsigned)((p.keep + rows_per_block - 1) / rows_per_block), p.Hkv, p.B), dim3(256), 0, st,
                      p, vpr_shift);
