@@ -289,8 +289,13 @@ Tensor output(PyObject* given, at::IntArrayRef sizes, at::ScalarType type, const
 
 // A kernel on the current stream reads and writes these: memory of the current device, not the host's or another GPU's.
 void require_here(std::initializer_list<const Tensor*> tensors) {
-  for (const Tensor* t : tensors)
-    if (t->defined()) require(t->is_cuda() && t->get_device() == c10::hip::current_device(), "tensors lie on the current device");
+  int current = -1;
+  for (const Tensor* t : tensors) {
+    if (!t->defined()) continue;
+    require(t->is_cuda(), "tensors lie on the current device");
+    if (current < 0) current = c10::hip::current_device();
+    require(t->get_device() == current, "tensors lie on the current device");
+  }
 }
 
 // [B, H_kv, at least n] fp32, any strides with unit stride on the rows

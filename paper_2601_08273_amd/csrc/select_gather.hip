@@ -38,6 +38,7 @@ __device__ __forceinline__ uint32_t score_key(float x) {
   if ((u << 1) == 0u) u = 0u;
   return ((u & 0x80000000u) ? ~u : (u | 0x80000000u)) + 1u;      // at most 0xff800001 (+inf)
 }
+constexpr uint32_t kZeroKey = 0x80000001u;
 
 // One wave walks a histogram from the top bin down (no barriers inside): lane l owns the BPL bins
 // below nb - 1 - BPL*l, read BATCH at a time so the LDS reads pipeline; an inclusive wave scan of
@@ -122,7 +123,7 @@ __device__ __forceinline__ long long gather_offset(long long row, const SelectPa
 // the scanning wave, which own runs of 64 consecutive bins, hit different LDS banks.  Nothing reads it once a key is emitted.
 // ANY: the scores start anywhere and are any number, as between the first and the recent rows of a head's mass: 16-byte loads that
 // are 4-byte aligned, and the vector that the end cuts is taken from the last four scores (16400 scores a head x 4, 8192 kept: 14.3 ->
-// 12.4 us with them).
+// 12.4 us with them); and rows of mass 0 may be many (all of 33152 a head x 4: 99 -> 26 us).
 template <int NC, bool ANY = false, typename Emit>
 __device__ __forceinline__ void select_top(const float* sc, const int Nv, const int k, unsigned* const hist, Emit emit) {
   constexpr bool CACHED = NC > 0;
@@ -178,6 +179,10 @@ __device__ __forceinline__ void select_top(const float* sc, const int Nv, const 
   const int shifts[3] = {20, 8, 0};
   const unsigned masks[3] = {0u, 0xfff00000u, 0xffffff00u};   // bits already decided
   const unsigned dmask[3] = {0xfffu, 0xfffu, 0xffu};
+  bool many_zeros = false;                     // among three of the wave's rows of keys
+  if constexpr (CACHED && ANY)
+    many_zeros = __popcll(__ballot(keys[0] == kZeroKey)) + __popcll(__ballot(keys[NC / 2] == kZeroKey)) +
+                     __popcll(__ballot(keys[NC - 1] == kZeroKey)) >= 16;
   bool listed = false;                         // block-uniform: the candidates are in the LDS list
   unsigned list_n = 0;
   unsigned* const list = hist;                 // the first histogram's words
@@ -190,6 +195,16 @@ __device__ __forceinline__ void select_top(const float* sc, const int Nv, const 
         const unsigned key = list[i];
         if ((key & masks[pass]) == prefix) atomicAdd(&h[hist_slot((key >> shifts[pass]) & dmask[pass])], 1u);
       }
+    } else if (CACHED && ANY && many_zeros) {
+      // (rows without any weight are all of one bin, where an addition each takes turns with the others: counted by the wave)
+      int zeros = 0;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const bool in = (keys[c] & masks[pass]) == prefix && (pass > 0 || keys[c] != 0u), zero = keys[c] == kZeroKey;
+        zeros += __popcll(__ballot(in && zero));
+        if (in && !zero) atomicAdd(&h[hist_slot((keys[c] >> shifts[pass]) & dmask[pass])], 1u);
+      }
+      if (zeros != 0 && lane == 0) atomicAdd(&h[hist_slot((kZeroKey >> shifts[pass]) & dmask[pass])], (unsigned)zeros);
     } else if (CACHED) {
 #pragma unroll
       for (int c = 0; c < NC; ++c)        // (slots past the end would all hit bin 0: the first pass leaves them out)
