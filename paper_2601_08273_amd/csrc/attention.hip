@@ -42,6 +42,38 @@ __device__ __forceinline__ long long out_row(const AttnParams& p, int b, int hk,
   return (((long long)b * p.q_len + i) * p.H + h);
 }
 
+// the weight of a token from its logit; fp32 rounds product and sum one by one, as its slices do
+template <bool F32>
+__device__ __forceinline__ float weight_of(float z, float scale_log2, float m) {
+  if constexpr (F32) {
+#pragma clang fp contract(off)
+    return fast_exp2(z * scale_log2 - m);
+  } else {
+    return fast_exp2(fmaf(z, scale_log2, -m));
+  }
+}
+
+// Attention mass of a slice that is the whole cache, by the block that just took it: its waves' logits are in memory (each waited for
+// its own before the barriers that the caller's merge went through), the rows' statistics in LDS.  mass_tile sums the same in the
+// same order of rows, four at a time.  The launch of the merge costs more than one block's turn over its logits: 200 rows x 4 heads
+// x 128, 7 query rows 9.0 -> 7.2 us (without weights 5.9).
+template <bool F32>
+__device__ __forceinline__ void mass_of_block(const MassParams& p, int hk, int b, const float* row_m, const float* row_inv) {
+  const float* z = p.logits + ((long long)b * p.Hkv + hk) * p.R * p.logits_ld;
+  float* out = p.mass_out + b * p.mass_osb + hk * p.mass_osh;
+  for (int n = threadIdx.x; n < p.n_total; n += blockDim.x) {
+    float before = 0.f, sum[4] = {0.f, 0.f, 0.f, 0.f};
+    if (n < p.ctx_len && p.mass_in != nullptr) before = p.mass_in[b * p.mass_isb + hk * p.mass_ish + n];
+    float zr[16];                                            // a call of one slice has up to 16 rows
+#pragma unroll
+    for (int r = 0; r < 16; ++r) zr[r] = z[(long long)min(r, p.R - 1) * p.logits_ld + n];
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      if (r < p.R) sum[r % 4] = fmaf(weight_of<F32>(zr[r], p.scale_log2, row_m[r]), row_inv[r], sum[r % 4]);
+    out[n] = before + ((sum[0] + sum[1]) + (sum[2] + sum[3]));
+  }
+}
+
 // =================================================================================================
 // MFMA partial kernel (bf16): helpers
 // =================================================================================================
@@ -141,7 +173,7 @@ __device__ __forceinline__ bf16x8 e4m3x8_to_bf16(int lo, int hi) {
 template <int D, int RB, int TG, int TT, int NST, int MODE, bool KV8 = false, bool NT = false, bool ROT = false,
           bool ONE = false, bool MASS = false>
 __global__ __launch_bounds__(RB * TG * 64) void attn_partial_grid(ParamsOf<MASS> p) {
-  static_assert(!MASS || (MODE < 2 && !KV8 && !ONE && RB <= 4), "weights are summed over contiguous bf16 caches");
+  static_assert(!MASS || (MODE < 2 && !KV8 && RB <= 4), "weights are summed over contiguous bf16 caches");
   constexpr bool APPEND = MODE == 1, PAGED = MODE == 2;
   constexpr bool LONG32 = ROT && TT == 32;
   constexpr bool SCALED = RB > 4;                      // more than 64 rows in one block: see its stores
@@ -513,7 +545,14 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_partial_grid(ParamsOf<MASS>
       float lf = 0.f;
 #pragma unroll
       for (int w = 0; w < TG; ++w) lf = fmaf(f[w], stat_f[w * RB * 16 + rb * 16 + j], lf);
-      if (TGC == 0 && g == 0 && row < p.R) p.part_f[(((long long)b * p.Hkv + hk) * p.S + split) * p.R + row] = lf;
+      if constexpr (ONE) {
+        if (TGC == 0 && g == 0) {
+          stat_f[TG * RB * 16 + j] = mm;                   // behind what the waves still read
+          stat_f[TG * RB * 16 + 16 + j] = 1.f / lf;
+        }
+      } else if (TGC == 0 && g == 0 && row < p.R) {
+        p.part_f[(((long long)b * p.Hkv + hk) * p.S + split) * p.R + row] = lf;
+      }
     }
     if constexpr (KV8) {
 #pragma unroll
@@ -576,7 +615,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_partial_grid(ParamsOf<MASS>
       // the slice's output leaves as bf16 (the merge weighs and sums it in fp32): half the bytes to write
       // here and to fetch in the merge, and the rounding is one more of the size the output's own has
       // (MASS: in fp32.  One rounding less brings the output's error from 2.7e-3 to 2.3e-3, and few rows cost few bytes.)
-      if constexpr (MASS) {
+      if constexpr (MASS && !ONE) {
         if (row < p.R) *(f32x4*)((float*)p.part_o + (slot * p.R + row) * D + db * 16 + 4 * g) = o;
       } else if (row < p.R) {
         typedef __attribute__((ext_vector_type(2))) float f32x2_t;
@@ -606,6 +645,10 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_partial_grid(ParamsOf<MASS>
   else if (tg == 1) finish(std::integral_constant<int, 1>());
   else if (tg == 2) finish(std::integral_constant<int, 2 % TG>());
   else finish(std::integral_constant<int, 3 % TG>());
+  if constexpr (MASS && ONE) {
+    __syncthreads();
+    mass_of_block<false>(p, hk, b, stat_f + TG * RB * 16, stat_f + TG * RB * 16 + 16);
+  }
   if (APPEND && appends) {
     if (append_early) {
       if ((int)threadIdx.x < p.q_len * APR) {
@@ -655,7 +698,7 @@ struct F32Smem {
 
 template <int D, int RB, int TG, int NST, int MODE, bool ONE = false, bool MASS = false>
 __global__ __launch_bounds__(RB * TG * 64) void attn_partial_f32(ParamsOf<MASS> p) {
-  static_assert(!MASS || (MODE < 2 && !ONE), "weights are summed over contiguous caches");
+  static_assert(!MASS || MODE < 2, "weights are summed over contiguous caches");
   constexpr bool APPEND = MODE == 1, PAGED = MODE == 2;
   using SM = F32Smem<D, TG, NST>;
   constexpr int WAVES = RB * TG;
@@ -886,6 +929,15 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_partial_f32(ParamsOf<MASS> 
       }
     }
   }
+  if constexpr (MASS && ONE) {
+    float* row_m = (float*)(smem + SM::total(RB));
+    if (tg == 0 && g == 0) {
+      row_m[j] = mm;
+      row_m[16 + j] = 1.f / ll;
+    }
+    __syncthreads();
+    mass_of_block<true>(p, hk, b, row_m, row_m + 16);
+  }
   if (APPEND && split == 0 && chunk == 0) append_new_rows<float, D>(p, b, hk);
 }
 
@@ -904,17 +956,6 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_partial_f32(ParamsOf<MASS> 
 // at a time, each after the one before.
 // =================================================================================================
 constexpr int kMassTile = 256;
-// the weight of a token from its logit; fp32 rounds product and sum one by one, as its slices do
-template <bool F32>
-__device__ __forceinline__ float weight_of(float z, float scale_log2, float m) {
-  if constexpr (F32) {
-#pragma clang fp contract(off)
-    return fast_exp2(z * scale_log2 - m);
-  } else {
-    return fast_exp2(fmaf(z, scale_log2, -m));
-  }
-}
-
 // m* and 1 / l* of the KV head's rows r0 .. r0 + ROWS - 1 into LDS, by all 256 threads: ROWS rows x 256 / ROWS groups of slices.
 // fetch() asks for the first PF slices of every group, finish() merges.
 template <int ROWS>
@@ -1192,9 +1233,10 @@ static hipError_t allow_dynamic_lds(int smem) {
 template <int D, int RB, int TG, int TT, int NST, int MODE, bool KV8 = false, bool NT = false, bool ROT = false,
           bool ONE = false, bool MASS = false>
 static hipError_t launch_grid_mode(const ParamsOf<MASS>& p, hipStream_t st) {
-  // the paged variant keeps its slice of the page table behind the ring, the one for attention mass its denominators
+  // the paged variant keeps its slice of the page table behind the ring, the one for attention mass its denominators and,
+  // of one slice, the merged statistics
   constexpr int smem = GridSmem<D, TG, TT, NST, KV8 ? 1 : 2>::total(RB) + (MODE == 2 ? kMaxSlicePages * 4 : 0) +
-                       (MASS ? TG * RB * 16 * 4 : 0);
+                       (MASS ? (TG * RB * 16 + 32) * 4 : 0);
   const hipError_t e = allow_dynamic_lds<attn_partial_grid<D, RB, TG, TT, NST, MODE, KV8, NT, ROT, ONE, MASS>>(smem);
   if (e != hipSuccess) return e;
   dim3 grid(p.S, p.Hkv, p.B * p.n_chunks);
@@ -1263,8 +1305,8 @@ static hipError_t launch_grid_rb(const ParamsOf<MASS>& p, hipStream_t st) {
   if (RB >= 3 && tiles32_per_block >= (RB == 4 || p.n_chunks > 1 ? 12 : 16))
     return launch_grid<D, RB, 2, 32, 3, false, false, false, MASS>(p, st);
   if (RB >= 3) return launch_grid<D, RB, 2, 16, 4, false, false, false, MASS>(p, st);
-  if constexpr (RB == 1 && !MASS)
-    if (one_slice_call(p)) return launch_grid<D, RB, 4, 16, 3, false, false, true>(p, st);
+  if constexpr (RB == 1)
+    if (one_slice_call(p)) return launch_grid<D, RB, 4, 16, 3, false, false, true, MASS>(p, st);
   return launch_grid<D, RB, 4, 16, 3, false, false, false, MASS>(p, st);
 }
 
@@ -1314,7 +1356,7 @@ static hipError_t launch_mfma_d(const ParamsOf<MASS>& p, hipStream_t st) {
 
 template <int D, int RB, int TG, int NST, int MODE, bool ONE, bool MASS>
 static hipError_t launch_f32_mode(const ParamsOf<MASS>& p, hipStream_t st) {
-  constexpr int smem = F32Smem<D, TG, NST>::total(RB) + (MODE == 2 ? kMaxSlicePages * 4 : 0);
+  constexpr int smem = F32Smem<D, TG, NST>::total(RB) + (MODE == 2 ? kMaxSlicePages * 4 : 0) + (MASS && ONE ? 32 * 4 : 0);
   const hipError_t e = allow_dynamic_lds<attn_partial_f32<D, RB, TG, NST, MODE, ONE, MASS>>(smem);
   if (e != hipSuccess) return e;
   ParamsOf<MASS> q = p;
@@ -1341,8 +1383,7 @@ static hipError_t launch_f32_d(const ParamsOf<MASS>& p, hipStream_t st) {
   constexpr bool W = D == 128;
   switch (p.row_chunk / 16) {
     case 1:
-      if constexpr (!MASS)
-        if (one_slice_call(p)) return launch_f32<D, 1, 4, W ? 2 : 4, true>(p, st);
+      if (one_slice_call(p)) return launch_f32<D, 1, 4, W ? 2 : 4, true, MASS>(p, st);
       return launch_f32<D, 1, 4, W ? 2 : 4, false, MASS>(p, st);
     case 2: return launch_f32<D, 2, 4, W ? 2 : 4, false, MASS>(p, st);
     case 3: return launch_f32<D, 3, 4, W ? 2 : 4, false, MASS>(p, st);
@@ -1388,12 +1429,12 @@ hipError_t launch_attention_mass(const MassParams& p, int dtype, int head_dim, h
   hipError_t e;
   if (dtype == HIPPO_DTYPE_BF16) {
     e = (head_dim == 128) ? launch_mfma_d<128, true>(p, st) : launch_mfma_d<64, true>(p, st);
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess || one_slice_call(p)) return e;
     return (head_dim == 128) ? launch_combine_mass<uint16_t, 128, kPartF32>(p, st)
                              : launch_combine_mass<uint16_t, 64, kPartF32>(p, st);
   }
   e = (head_dim == 128) ? launch_f32_d<128, true>(p, st) : launch_f32_d<64, true>(p, st);
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || one_slice_call(p)) return e;
   return (head_dim == 128) ? launch_combine_mass<float, 128, kPartF32>(p, st) : launch_combine_mass<float, 64, kPartF32>(p, st);
 }
 

@@ -104,6 +104,27 @@ def test_slices(hippo, dtype, H, Hkv, d, ctx, q_len, splits):
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("B,H,Hkv,d,ctx,q_len", [
+    (1, 16, 1, 64, 735, 1), (2, 6, 3, 128, 735, 1), (1, 16, 2, 128, 600, 2), (2, 5, 1, 64, 253, 3), (3, 4, 4, 128, 256, 16),
+    (70, 8, 4, 64, 31, 2)])
+def test_one_slice_in_one_launch(hippo, dtype, B, H, Hkv, d, ctx, q_len):
+    """up to 16 rows over the whole cache in a block each, which sums the weights itself; in place, with appended rows"""
+    q, k, v, mass = make(B, H, Hkv, d, ctx, q_len, dtype, 21, 2.0)
+    got = hippo.hippo_verify_attention_mass(q, k, v, mass, ctx, want_lse=True, num_splits=1)
+    check(got, reference(q, k, v, ctx, mass, 1), dtype)
+    plain = hippo.hippo_verify_attention(q, k, v, ctx, want_lse=True, num_splits=1)
+    assert torch.equal(got[0], plain[0]) and torch.equal(got[2], plain[1])
+    k_new, v_new = (x[:, :, ctx:].transpose(1, 2).contiguous() for x in (k, v))
+    k2, v2 = k.clone(), v.clone()
+    k2[:, :, ctx:], v2[:, :, ctx:] = 3.0, float("nan")
+    room = torch.full((B, Hkv, ctx + q_len + 5), 50.0, device="cuda")
+    room[:, :, :ctx] = mass
+    again = hippo.hippo_verify_attention_mass(q, k2, v2, room, ctx, mass_out=room, k_new=k_new, v_new=v_new, num_splits=1)
+    assert torch.equal(again[0], got[0]) and torch.equal(room[:, :, :ctx + q_len], got[1])
+    assert (room[:, :, ctx + q_len:] == 50.0).all() and torch.equal(k2, k) and torch.equal(v2, v)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("B,H,Hkv,d,ctx,q_len", [
     (1, 4, 2, 64, 832, 1), (2, 28, 4, 128, 500, 6), (1, 28, 4, 128, 1895, 1), (3, 8, 4, 64, 40, 3), (1, 28, 4, 128, 16640, 6),
     (1, 8, 1, 128, 700, 25)])
 def test_appended_rows(hippo, dtype, B, H, Hkv, d, ctx, q_len):
