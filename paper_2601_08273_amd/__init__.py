@@ -22,7 +22,8 @@ SCORE_ATTN, SCORE_TEMP, SCORE_SPA, SCORE_ALL, SCORE_ACCUMULATE_ONLY = 1, 2, 4, 7
 
 EXPORTS = ("hippo_status_string", "hippo_workspace_bytes", "hippo_score_tokens",
            "hippo_score_layers_workspace_bytes", "hippo_score_tokens_layers",
-           "hippo_select_gather_kv", "hippo_evict_kv_workspace_bytes", "hippo_evict_kv", "hippo_verify_attention", "hippo_draft_attention",
+           "hippo_select_gather_kv", "hippo_evict_kv_workspace_bytes", "hippo_evict_kv",
+           "hippo_verify_attention", "hippo_draft_attention",
            "hippo_static_scratch_bytes", "hippo_static_scratch_init", "hippo_verify_attention_static",
            "hippo_verify_attention_append", "hippo_draft_attention_append",
            "hippo_attention_mass_workspace_bytes", "hippo_verify_attention_mass", "hippo_draft_attention_mass",

@@ -35,9 +35,9 @@ namespace {
   X(hippo_select_gather_kv) X(hippo_verify_attention) X(hippo_draft_attention) X(hippo_verify_attention_append)         \
   X(hippo_draft_attention_append) X(hippo_verify_attention_paged) X(hippo_draft_attention_paged)                        \
   X(hippo_verify_attention_fp8kv) X(hippo_draft_attention_fp8kv) X(hippo_quantize_kv_workspace_bytes)                   \
-  X(hippo_quantize_kv_e4m3) X(hippo_spec_verify_workspace_bytes) X(hippo_spec_verify)                   \
-  X(hippo_token_logprobs_workspace_bytes) X(hippo_token_logprobs)                 \
-  X(hippo_evict_kv_workspace_bytes) X(hippo_evict_kv) X(hippo_attention_mass_workspace_bytes)                      \
+  X(hippo_quantize_kv_e4m3) X(hippo_spec_verify_workspace_bytes) X(hippo_spec_verify)                                   \
+  X(hippo_token_logprobs_workspace_bytes) X(hippo_token_logprobs) X(hippo_evict_kv_workspace_bytes) X(hippo_evict_kv)   \
+  X(hippo_attention_mass_workspace_bytes)                                                                               \
   X(hippo_verify_attention_mass) X(hippo_draft_attention_mass)
 struct Library {
 #define X(name) decltype(&::name) name;
@@ -651,8 +651,8 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #define ENTRY(name, n) {#name, (PyCFunction)(void (*)(void))entry<name, n>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     ENTRY(bind, 3), ENTRY(score_tokens, 9), ENTRY(score_tokens_layers, 10), ENTRY(select_gather, 11), ENTRY(attention, 12),
-    ENTRY(attention_fp8kv, 12), ENTRY(attention_paged, 11), ENTRY(quantize, 6), ENTRY(spec_verify, 10), ENTRY(token_logprobs, 9), ENTRY(evict, 12), ENTRY(attention_mass, 14),
-    {nullptr, nullptr, 0, nullptr}};
+    ENTRY(attention_fp8kv, 12), ENTRY(attention_paged, 11), ENTRY(quantize, 6), ENTRY(spec_verify, 10),
+    ENTRY(token_logprobs, 9), ENTRY(evict, 12), ENTRY(attention_mass, 14), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

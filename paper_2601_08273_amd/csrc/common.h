@@ -286,7 +286,6 @@ struct AttnParams {
 };
 constexpr int kMaxSlicePages = 1024;   // page-table entries a block stages in LDS
 
-
 // The call that also sums its weights.  (Its arguments are its own: among AttnParams' every kernel would fetch them.)
 struct MassParams : AttnParams {
   float* part_f;            // [B, Hkv, S, R] partial denominators of the unrounded probabilities

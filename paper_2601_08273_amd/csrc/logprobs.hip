@@ -312,8 +312,8 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 ? 5 : 4) void lp_rows(Logpr
       for (int j = 0; j < NV; ++j) raw[j] = *reinterpret_cast<const u32x4*>(base + v0 + (j * THREADS + tid) * VEC);
       return;
     }
-    // The row's last chunk: -inf behind its end.  (Vectors behind it fetch the last whole one again; the one that the end cuts
-    // starts at v_hi rounded down, 16-byte aligned, and is fetched word by word.)
+    // The row's last chunk: -inf behind its end.  (The vector that the end cuts starts at v_hi rounded down and is fetched word by
+    // word.)
     const int whole = v_hi / VEC * VEC;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
