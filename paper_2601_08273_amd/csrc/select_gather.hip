@@ -43,10 +43,10 @@ constexpr uint32_t kZeroKey = 0x80000001u;
 // One wave walks a histogram from the top bin down (no barriers inside): lane l owns the BPL bins
 // below nb - 1 - BPL*l, read BATCH at a time so the LDS reads pipeline; an inclusive wave scan of
 // the lane sums counts the keys in all higher bins; the lane in which the running count reaches
-// `need` walks its bins again and publishes the digit and what is still needed inside it.
+// `need` walks its bins again and publishes the digit, what is still needed inside it and what it holds.
 template <int BPL, int BATCH>
 __device__ __forceinline__ void walk_histogram(const unsigned* h, int nb, int lane, unsigned prefix, unsigned need,
-                                               int shift, unsigned* out_prefix, unsigned* out_need) {
+                                               int shift, unsigned* out_prefix, unsigned* out_need, unsigned* out_count) {
   const int top = nb - 1 - BPL * lane;
   unsigned hsum = 0;
 #pragma unroll 1
@@ -61,6 +61,7 @@ __device__ __forceinline__ void walk_histogram(const unsigned* h, int nb, int la
   unsigned above = incl - hsum;                 // keys in bins above this lane's
   if (above < need && incl >= need) {           // exactly one lane
     int d = top;
+    unsigned in_bin = 0;
     bool found = false;
 #pragma unroll 1
     for (int q0 = 0; q0 < BPL; q0 += BATCH) {
@@ -70,13 +71,14 @@ __device__ __forceinline__ void walk_histogram(const unsigned* h, int nb, int la
 #pragma unroll
       for (int q = 0; q < BATCH; ++q) {
         if (!found) {
-          if (above + v[q] >= need) { found = true; d = top - q0 - q; }
+          if (above + v[q] >= need) { found = true; d = top - q0 - q; in_bin = v[q]; }
           else above += v[q];
         }
       }
     }
     *out_prefix = prefix | ((unsigned)d << shift);
     *out_need = need - above;
+    *out_count = in_bin;
   }
 }
 
@@ -225,7 +227,7 @@ __device__ __forceinline__ void select_top(const float* sc, const int Nv, const 
     }
     __syncthreads();
     if (pass == 2) {
-      if (wave == 0) walk_histogram<4, 4>(h, 256, lane, prefix, need, shifts[pass], &sh_prefix, &sh_need);
+      if (wave == 0) walk_histogram<4, 4>(h, 256, lane, prefix, need, shifts[pass], &sh_prefix, &sh_need, &sh_bin_count);
     } else {
       // all threads: thread t sums its 4 bins from the top down (thread 0 holds the highest), a block
       // scan counts the keys in all higher bins, and the one thread in which the running count reaches
@@ -279,9 +281,32 @@ __device__ __forceinline__ void select_top(const float* sc, const int Nv, const 
   const unsigned thr = prefix;      // the k-th largest key
   const unsigned need_eq = need;    // how many keys equal to it are kept (lowest indices first)
 
+  const bool keep_equal = sh_bin_count == need_eq;      // all of those (block-uniform)
+
   // ---- compaction in index order ----
   __syncthreads();
-  if (CACHED) {
+  if (CACHED && NC <= kPackedCounts && keep_equal) {
+    // The usual call: one count, of the keys that are kept.  (us a call in a graph, two counts -> one, indices only: 16384 scores,
+    // 1638 kept 10.2 -> 9.5, with 4 heads' rows 13.1 -> 12.7, 32768, 3276 kept 16.1 -> 14.4; not with more than 40 keys a thread, 26 to 70 more of which it spills.)
+    unsigned excl[NV], run = 0;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      unsigned mine = 0;
+#pragma unroll
+      for (int e = 0; e < VW; ++e) mine += keys[v * VW + e] >= thr ? 1u : 0u;
+      const unsigned incl = wave_scan_incl(mine);
+      excl[v] = run + incl - mine;
+      run += (unsigned)__builtin_amdgcn_readlane((int)incl, 63);
+    }
+    const unsigned in_front = waves_in_front(run, wave_tot[0], lane, wave);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      unsigned at = in_front + excl[v];
+#pragma unroll
+      for (int e = 0; e < VW; ++e)
+        if (keys[v * VW + e] >= thr) emit(at++, slot_index(v * VW + e));
+    }
+  } else if (CACHED) {
     // counts of keys above / equal to the threshold, packed (a wave's both fit 16 bits, a block's up to 40960 keys).
     // Index order inside a wave is (group of VW slots, lane, slot in the group): one wave scan per group, a running total
     // over the groups, then the totals of the waves in front; every thread then writes its own survivors.
@@ -473,6 +498,7 @@ hipError_t launch_select_gather(const SelectParams& p, hipStream_t st) {
   else if (n_chunks <= 16) { HIPPO_TOPK(16); }
   else if (n_chunks <= 24) { HIPPO_TOPK(24); }
   else if (n_chunks <= 32) { HIPPO_TOPK(32); }
+  else if (n_chunks <= 36) { HIPPO_TOPK(36); }
   else if (n_chunks <= 40) { HIPPO_TOPK(40); }
   else if (n_chunks <= 56) { HIPPO_TOPK(56); }
   else if (n_chunks <= kKeysPerThread) { HIPPO_TOPK(kKeysPerThread); }
@@ -546,7 +572,7 @@ __global__ __launch_bounds__(kSelThreads) void evict_select(EvictParams p, int v
   }
 }
 
-// A thread moves 16 bytes of K and of V of rows that lie `gridDim.x` blocks apart; the first of a row's threads its mass too.
+// A thread moves 16 bytes of K and of V, the first of a row's threads its mass too.
 __global__ __launch_bounds__(256) void evict_gather(EvictParams p, int vpr_shift) {
   const int hk = blockIdx.y, b = blockIdx.z;
   const int32_t* idx = p.idx_out + ((long long)b * p.Hkv + hk) * p.keep;
@@ -577,6 +603,8 @@ hipError_t launch_evict(const EvictParams& p, hipStream_t st) {
   const long long parts = one_launch ? std::max<long long>(1, std::min<long long>((per_head + 2 * kSelThreads - 1) / (2 * kSelThreads),
                                                                                   kNumCU / heads))
                                      : 1;
+  // (a class of 36 keys for long videos' caches: 33152 rows x 4 heads, 8000 kept, 23.7 us in one of 40, 20.5; 56 keys: 48000 rows
+  // 41.3 in one of 72, 33.3)
 #define HIPPO_EVICT(NC_)                                                                                             \
   if (one_launch)                                                                                                    \
     hipLaunchKernelGGL((evict_select<NC_, (NC_ > 0 && NC_ <= kGatherKeys)>), dim3((unsigned)(p.Hkv * parts), p.B),    \
@@ -588,12 +616,16 @@ hipError_t launch_evict(const EvictParams& p, hipStream_t st) {
   else if (n_chunks <= 8) { HIPPO_EVICT(8); }
   else if (n_chunks <= 16) { HIPPO_EVICT(16); }
   else if (n_chunks <= 24) { HIPPO_EVICT(24); }
+  else if (n_chunks <= 32) { HIPPO_EVICT(32); }
+  else if (n_chunks <= 36) { HIPPO_EVICT(36); }
   else if (n_chunks <= 40) { HIPPO_EVICT(40); }
+  else if (n_chunks <= 56) { HIPPO_EVICT(56); }
   else if (n_chunks <= kKeysPerThread) { HIPPO_EVICT(kKeysPerThread); }
   else { HIPPO_EVICT(0); }
 #undef HIPPO_EVICT
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || one_launch || (p.k_dst == nullptr && p.mass_dst == nullptr)) return e;
+  if (p.k_dst == nullptr) vpr_shift = 0;                   // the masses alone: a row a thread
   const int rows_per_block = 256 >> vpr_shift;
   hipLaunchKernelGGL(evict_gather, dim3((unsigned)((p.keep + rows_per_block - 1) / rows_per_block), p.Hkv, p.B), dim3(256), 0, st,
                      p, vpr_shift);
