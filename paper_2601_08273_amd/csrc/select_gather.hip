@@ -603,8 +603,9 @@ hipError_t launch_evict(const EvictParams& p, hipStream_t st) {
   const long long parts = one_launch ? std::max<long long>(1, std::min<long long>((per_head + 2 * kSelThreads - 1) / (2 * kSelThreads),
                                                                                   kNumCU / heads))
                                      : 1;
-  // (a class of 36 keys for long videos' caches: 33152 rows x 4 heads, 8000 kept, 23.7 us in one of 40, 20.5; 56 keys: 48000 rows
-  // 41.3 in one of 72, 33.3)
+  // (Finer classes of keys a thread than topk_select's, since every block of a head selects, in one launch.  us a call in a graph:
+  // 12000 rows x 4 heads x 128, 4000 kept in a class of 16 14.4, of 12 13.8; 20000, 9000 kept in 24 22.2, in 20 21.3; indices alone,
+  // 33152, 8000 kept in 40 23.7, in 36 20.5; 48000 in 72 41.3, in 56 33.3.)
 #define HIPPO_EVICT(NC_)                                                                                             \
   if (one_launch)                                                                                                    \
     hipLaunchKernelGGL((evict_select<NC_, (NC_ > 0 && NC_ <= kGatherKeys)>), dim3((unsigned)(p.Hkv * parts), p.B),    \
@@ -614,7 +615,9 @@ hipError_t launch_evict(const EvictParams& p, hipStream_t st) {
   if (n_chunks <= 2) { HIPPO_EVICT(2); }
   else if (n_chunks <= 4) { HIPPO_EVICT(4); }
   else if (n_chunks <= 8) { HIPPO_EVICT(8); }
+  else if (n_chunks <= 12) { HIPPO_EVICT(12); }
   else if (n_chunks <= 16) { HIPPO_EVICT(16); }
+  else if (n_chunks <= 20) { HIPPO_EVICT(20); }
   else if (n_chunks <= 24) { HIPPO_EVICT(24); }
   else if (n_chunks <= 32) { HIPPO_EVICT(32); }
   else if (n_chunks <= 36) { HIPPO_EVICT(36); }
