@@ -75,6 +75,19 @@ def test_rows_that_stay(hippo, dtype, d, B, Hkv, N, keep, first, recent):
         check(got, mass, k, v, keep, first, recent, (dtype, kind))
 
 
+@pytest.mark.parametrize("N", [8192 + 1, 12288, 12288 + 1, 20480, 20480 + 1, 32768, 32768 + 1, 36864, 36864 + 1, 57344, 57344 + 1])
+@pytest.mark.parametrize("kind", ["heavy", "ties", "odd"])
+def test_edges_of_the_classes(hippo, N, kind):
+    """rows between as many as a class of keys a thread holds, and one more; indices and mass alone and with rows"""
+    mass, k, v = make(1, 2, N + 3, 64, "fp8", N, kind)
+    for keep in (5 + N // 7, N - 1):
+        got = hippo.hippo_evict_kv(mass, keep, k, v, n_first=1, n_recent=2)
+        check(got, mass, k, v, keep, 1, 2, keep)
+        idx, none, none_too, md = hippo.hippo_evict_kv(mass, keep, None, None, n_first=1, n_recent=2)
+        assert none is None and none_too is None and torch.equal(idx, got[0])
+        assert torch.equal(md.view(torch.int32), got[3].view(torch.int32))
+
+
 @pytest.mark.parametrize("N", [16384, 16657, 24581, 33280, 40964, 73730, 80001])
 @pytest.mark.parametrize("kind", ["heavy", "ties", "equal", "odd"])
 def test_long_caches(hippo, N, kind):
