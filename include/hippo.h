@@ -203,8 +203,8 @@ int hippo_select_gather_kv(const float* scores, int32_t k,
  * src and dst may be 8-bit caches (codes are copied; the per-head multipliers stay valid); they agree in batch, n_kv_heads,
  * head_dim and dtype.  k_dst/v_dst may be NULL together (indices and mass only, k_src/v_src are then not read), mass_dst may be
  * NULL.  Rows of dst and mass_dst from `keep` on are left as they were, so that a decoding loop appends behind them.
- * src and dst must not overlap.  1 <= keep <= src_len <= 2^30, n_first + n_recent <= keep.  Deterministic.
- * Errors: NULL_ARG, BAD_SHAPE (also dst on src), BAD_DTYPE, BAD_ALIGN, WORKSPACE_TOO_SMALL, HIP.
+ * src and dst, and mass and mass_dst, must not overlap.  1 <= keep <= src_len <= 2^30, n_first + n_recent <= keep.  Deterministic.
+ * Errors: NULL_ARG, BAD_SHAPE (also dst on src, and strides by which rows of dst or of mass_dst would meet), BAD_DTYPE, BAD_ALIGN, WORKSPACE_TOO_SMALL, HIP.
  */
 size_t hippo_evict_kv_workspace_bytes(const hippo_kv_desc* src, int32_t src_len, int32_t keep);
 int hippo_evict_kv(const float* mass, int64_t mass_stride_b, int64_t mass_stride_h,
@@ -304,7 +304,7 @@ int hippo_draft_attention_append(const void* q, int32_t q_len, const void* k_new
  * out and lse_out as without mass, but that the slices' outputs reach the merge in fp32.  The weights are fp32 from fp32
  * logits, of the probabilities before any rounding; sums run in a fixed order.  Rows that a verification rejects leave their share
  * in older rows' mass; their own rows' mass is written anew with the rows.
- * mass: `in` may be NULL (nothing accumulated yet) or `out` (in place, the same strides); element (b, hk, n) lies at
+ * mass: `in` may be NULL (nothing accumulated yet) or `out` (in place, the same strides), and does not overlap it otherwise; element (b, hk, n) lies at
  * b * stride_b + hk * stride_h + n.  Elements of `out` from ctx_len + q_len on are left as they were.
  * k_new, v_new: both NULL (the caches hold the new rows), or the rows to append, as in the *_append calls.  Caches: F32 or BF16,
  * contiguous.  Workspace: hippo_attention_mass_workspace_bytes, with seq_len = ctx_len + q_len; it grows with seq_len times the

@@ -35,6 +35,34 @@ int check_kv(const hippo_kv_desc* kv, bool allow_fp8 = false) {
   return HIPPO_OK;
 }
 
+// Blocks of `len` elements at d[0].stride i + d[1].stride j + d[2].stride k, i < d[0].count and so on: whether two of them share an
+// element, that is, whether len exceeds the size of some sum of the strides, each up to count - 1 times and in either direction.
+// The wider strides come first: what the narrower ones reach leaves few multiples of a wider one to try, and none but 0 of the
+// layouts in which a dimension steps over the ones inside it.
+struct Spaced {
+  long long count, stride;
+};
+bool blocks_meet(const Spaced* d, int n, __int128 at, bool moved, long long len) {
+  if (n == 0) return moved && at < len && -at < len;
+  __int128 reach = len - 1;
+  for (int i = 1; i < n; ++i) reach += (__int128)(d[i].count - 1) * d[i].stride;
+  if (d->count <= 1) return blocks_meet(d + 1, n - 1, at, moved, len);
+  const __int128 most = d->count - 1, s = d->stride;             // s >= len > 0, see rows_meet
+  __int128 lo = -((reach + at) / s), hi = (reach - at) / s;
+  // (a distance and its opposite are of the same two blocks)
+  for (__int128 i = std::max(lo, moved ? -most : (__int128)0); i <= std::min(hi, most); ++i)
+    if (blocks_meet(d + 1, n - 1, at + i * s, moved || i != 0, len)) return true;
+  return false;
+}
+bool rows_meet(Spaced a, Spaced b, Spaced c, long long len) {
+  if (len < 1) return false;
+  Spaced d[3] = {a, b, c};
+  for (const Spaced& x : d)
+    if (x.count > 1 && x.stride < len) return true;
+  std::sort(d, d + 3, [](const Spaced& x, const Spaced& y) { return x.stride > y.stride; });
+  return blocks_meet(d, 3, 0, false, len);
+}
+
 int check_video(const hippo_video_desc* v) {
   if (v == nullptr) return HIPPO_ERR_NULL_ARG;
   if (v->n_frames < 1 || v->grid_h < 1 || v->grid_w < 1 || v->vis_offset < 0) return HIPPO_ERR_BAD_SHAPE;
@@ -603,7 +631,7 @@ int hippo_evict_kv(const float* mass, int64_t mass_stride_b, int64_t mass_stride
   if (mass_dst != nullptr) {
     if (mass_dst == mass) return HIPPO_ERR_BAD_SHAPE;
     if (reinterpret_cast<uintptr_t>(mass_dst) & 3u) return HIPPO_ERR_BAD_ALIGN;
-    if ((p.Hkv > 1 && mass_dst_stride_h < keep) || (p.B > 1 && mass_dst_stride_b < keep)) return HIPPO_ERR_BAD_SHAPE;
+    if (rows_meet({p.B, mass_dst_stride_b}, {p.Hkv, mass_dst_stride_h}, {1, 0}, keep)) return HIPPO_ERR_BAD_SHAPE;
   }
   if (k_dst != nullptr || v_dst != nullptr) {
     if (k_dst == nullptr || v_dst == nullptr || k_src == nullptr || v_src == nullptr || dst == nullptr) return HIPPO_ERR_NULL_ARG;
@@ -612,6 +640,7 @@ int hippo_evict_kv(const float* mass, int64_t mass_stride_b, int64_t mass_stride
         dst->dtype != src->dtype || k_dst == k_src || v_dst == v_src || k_dst == v_src || v_dst == k_src || k_dst == v_dst)
       return HIPPO_ERR_BAD_SHAPE;
     if (!aligned16(k_src) || !aligned16(v_src) || !aligned16(k_dst) || !aligned16(v_dst)) return HIPPO_ERR_BAD_ALIGN;
+    if (rows_meet({p.B, dst->stride_b}, {p.Hkv, dst->stride_h}, {keep, dst->stride_n}, p.D)) return HIPPO_ERR_BAD_SHAPE;
     p.k_dst = k_dst; p.v_dst = v_dst;
     p.dsb = dst->stride_b; p.dsh = dst->stride_h; p.dsn = dst->stride_n;
   }
@@ -766,10 +795,12 @@ static int mass_entry(int call, const void* q, int32_t q_len, const void* k_new,
                       const hippo_mass_desc* mass, void* workspace, size_t workspace_bytes, void* stream) {
   if (kv == nullptr || mass == nullptr || mass->out == nullptr) return HIPPO_ERR_NULL_ARG;
   if ((k_new == nullptr) != (v_new == nullptr)) return HIPPO_ERR_NULL_ARG;
+  const int rc = check_kv(kv);
+  if (rc != HIPPO_OK) return rc;
   if (mass->in != nullptr && (mass->in_stride_b < 0 || mass->in_stride_h < 0)) return HIPPO_ERR_BAD_SHAPE;
   // every (batch element, KV head) writes a row of its own
-  const long long n = (long long)ctx_len + q_len;
-  if ((kv->n_kv_heads > 1 && mass->out_stride_h < n) || (kv->batch > 1 && mass->out_stride_b < n)) return HIPPO_ERR_BAD_SHAPE;
+  if (rows_meet({kv->batch, mass->out_stride_b}, {kv->n_kv_heads, mass->out_stride_h}, {1, 0}, (long long)ctx_len + q_len))
+    return HIPPO_ERR_BAD_SHAPE;
   // in place: where it stood
   if (mass->in == mass->out && ((kv->n_kv_heads > 1 && mass->in_stride_h != mass->out_stride_h) ||
                                 (kv->batch > 1 && mass->in_stride_b != mass->out_stride_b)))

@@ -66,3 +66,17 @@ def test_the_binding_refuses_tensors_it_would_misread():
             ((q, k, v, m, 48), {})):                               # host memory, which no kernel reads
         with pytest.raises(AssertionError):
             h.hippo_verify_attention_mass(*args, **more)
+
+
+@pytest.mark.parametrize("strides,status", [
+    (dict(osb=20000, osh=20000), h.ERR_BAD_SHAPE),                 # head 1 of the first sequence on head 0 of the second
+    (dict(osb=76645, osh=20000), h.ERR_BAD_SHAPE), (dict(osb=76646, osh=20000), h.ERR_WORKSPACE_TOO_SMALL),
+    (dict(osb=16646, osh=33291), h.ERR_BAD_SHAPE), (dict(osb=16646, osh=33292), h.ERR_WORKSPACE_TOO_SMALL),
+    (dict(osb=40000, osh=20000), h.ERR_BAD_SHAPE), (dict(osb=17000, osh=50000), h.ERR_WORKSPACE_TOO_SMALL),
+    (dict(osb=0, osh=0), h.ERR_BAD_SHAPE), (dict(isb=0, ish=0), h.ERR_WORKSPACE_TOO_SMALL),          # `in` is only read
+    (dict(m_in=3 * FAKE, isb=20000, ish=20000, osb=20000, osh=20000), h.ERR_BAD_SHAPE),              # in place
+    (dict(kv=desc(batch=1), osb=0), h.ERR_WORKSPACE_TOO_SMALL), (dict(kv=desc(n_kv_heads=1), osh=0), h.ERR_WORKSPACE_TOO_SMALL),
+])
+def test_rows_of_mass_that_would_meet_are_refused(strides, status):
+    for fn in (h.load().hippo_verify_attention_mass, h.load().hippo_draft_attention_mass):
+        assert call(fn, ws_bytes=256, **strides) == status

@@ -1,5 +1,7 @@
 """Refusals of hippo_evict_kv, without a GPU: the library answers before it launches anything."""
 import ctypes as C
+import itertools
+import random
 
 import pytest
 import torch
@@ -73,3 +75,55 @@ def test_the_binding_refuses_tensors_it_would_misread():
             h.hippo_evict_kv(*args, **more)
     with pytest.raises(AssertionError):                           # host memory, which no kernel reads
         h.hippo_evict_kv(m, 20, k, v)
+
+
+def rows_meet(counts, strides, length):
+    """by writing the rows down"""
+    places = [sum(i * s for i, s in zip(at, strides)) for at in itertools.product(*map(range, counts))]
+    places.sort()
+    return any(b - a < length for a, b in zip(places, places[1:]))
+
+
+@pytest.mark.parametrize("bad", [
+    dict(mdb=8000, mdh=8000), dict(mdb=20000, mdh=20000),                    # head 1 of the first sequence on head 0 of the second
+    dict(mdb=67999, mdh=20000), dict(mdb=8000, mdh=15999), dict(mdb=40000, mdh=20000), dict(mdb=0, mdh=0),
+    dict(dst=desc(8192, stride_b=0)), dict(dst=desc(8192, stride_h=0)), dict(dst=desc(8192, stride_b=0, stride_h=0)),
+    dict(dst=desc(8192, stride_b=8192 * 128)), dict(dst=desc(8192, stride_b=4 * 8192 * 128 - 193 * 128)), dict(dst=desc(7999)),
+    dict(dst=desc(8192, stride_n=512, stride_h=64, stride_b=8192 * 512)),    # heads inside a row, of 64 of its 128 channels each
+    dict(dst=desc(8192, stride_n=512, stride_h=128, stride_b=512)),
+])
+def test_rows_of_dst_that_would_meet_are_refused(bad):
+    assert call(ws_bytes=255, **bad) == h.ERR_BAD_SHAPE
+
+
+@pytest.mark.parametrize("good", [
+    dict(mdb=68000, mdh=20000), dict(mdb=8000, mdh=16000), dict(mdb=20000, mdh=40000), dict(mdb=10000, mdh=20000),
+    dict(dst=desc(8000)), dict(dst=desc(8192, stride_b=4 * 8192 * 128 - 192 * 128)),
+    dict(dst=desc(8192, stride_n=512, stride_h=128, stride_b=8000 * 512)),   # [B, N, Hkv, d]
+    dict(dst=desc(8192, stride_n=1024, stride_h=128, stride_b=512)),         # [N, B, Hkv, d]
+    dict(dst=desc(8192, stride_n=1024, stride_h=256, stride_b=128)),         # [N, Hkv, B, d]
+    dict(dst=desc(8192, stride_h=2 * 8192 * 128, stride_b=8192 * 128)),      # [Hkv, B, N, d]
+    dict(src=desc(batch=1), dst=desc(8192, batch=1, stride_b=0)),            # nobody steps over the only sequence
+    dict(src=desc(stride_h=0), dst=desc(8192)), dict(src=desc(stride_b=0), dst=desc(8192)),       # src is only read
+    dict(msb=0, msh=0),
+])
+def test_rows_of_dst_that_do_not_meet_are_taken(good):
+    assert call(ws_bytes=255, **good) == h.ERR_WORKSPACE_TOO_SMALL           # the last of the checks
+
+
+def test_any_strides_of_dst():
+    rng = random.Random(5)
+    answers = set()
+    for _ in range(600):
+        B, Hkv, keep = rng.randint(1, 4), rng.randint(1, 4), rng.randint(1, 5)
+        mdb, mdh = rng.randint(0, 30), rng.randint(0, 30)
+        few = dict(keep=keep, first=0, recent=1, n=9, src=desc(9, batch=B, n_q_heads=12, n_kv_heads=Hkv), ws_bytes=255)
+        want = h.ERR_BAD_SHAPE if rows_meet((B, Hkv), (mdb, mdh), keep) else h.ERR_WORKSPACE_TOO_SMALL
+        assert call(kd=None, vd=None, mdb=mdb, mdh=mdh, **few) == want, (B, Hkv, keep, mdb, mdh)
+        sb, sh, sn = (64 * rng.randint(0, 14) + 8 * rng.choice([0, 0, 1]) for _ in range(3))
+        sn += 128
+        want = h.ERR_BAD_SHAPE if rows_meet((B, Hkv, keep), (sb, sh, sn), 128) else h.ERR_WORKSPACE_TOO_SMALL
+        dst = desc(9, batch=B, n_q_heads=12, n_kv_heads=Hkv, stride_b=sb, stride_h=sh, stride_n=sn)
+        assert call(dst=dst, md=None, **few) == want, (B, Hkv, keep, sb, sh, sn)
+        answers.add((want, B > 1 and Hkv > 1 and keep > 1))
+    assert len(answers) == 4
