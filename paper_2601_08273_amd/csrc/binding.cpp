@@ -585,7 +585,7 @@ PyObject* token_logprobs(PyObject* const* a) {
     if (inside == 1) stride = step = x.stride(i);
     else REQUIRE(x.stride(i) == inside * step);
   }
-  if (rows == 1) stride = std::max<long long>(stride, (V + 7) / 8 * 8);       // nobody steps over the only row
+  if (rows == 1) stride = (V + 7) / 8 * 8;                                    // nobody steps over the only row
   REQUIRE(rows <= 0x7fffffff && V <= 0x7fffffff && n_top >= 0 && n_top <= 0x7fffffff);
   REQUIRE(tokens.sizes() == at::IntArrayRef(shape) && tokens.is_contiguous() && tokens.scalar_type() == at::kInt);
   const float temperature = (float)number(a[2]);

@@ -212,6 +212,18 @@ def test_leading_dimensions_strides_and_given_buffers(hippo, dtype):
         assert torch.equal(a[0], b[1, 2])
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_the_stride_of_the_only_row_is_nobodys(hippo, dtype):
+    g = torch.Generator(device="cuda").manual_seed(12)
+    tokens = torch.tensor([4999], dtype=torch.int32, device="cuda")
+    wide = (2.0 * torch.randn((3, 6001), generator=g, device="cuda")).to(TYPES[dtype])       # rows of no multiple of 16 bytes
+    chain = (2.0 * torch.randn((1, 7, 32004), generator=g, device="cuda")).to(TYPES[dtype])
+    for x in (wide[0:1, :5000], wide[0:1], chain[:, -1], chain[:, -1:], chain[0, -1:, :5000]):
+        t = tokens.view(x.shape[:-1])
+        got = hippo.hippo_token_logprobs(x, t, 0.8, n_top=5)
+        check(got, reference(x.reshape(1, -1).float().cpu().numpy(), [4999], 0.8, 5), x.shape)
+
+
 @pytest.mark.parametrize("R,V", [(2, 152064), (1100, 9000), (4, 30000)])
 def test_streams_graphs_and_repeats(hippo, R, V):
     g = torch.Generator(device="cuda").manual_seed(R)
