@@ -1,5 +1,6 @@
 """Refusals of hippo_*_attention_mass, without a GPU: the library answers before it launches anything."""
 import ctypes as C
+import re
 
 import pytest
 import torch
@@ -80,3 +81,37 @@ def test_the_binding_refuses_tensors_it_would_misread():
 def test_rows_of_mass_that_would_meet_are_refused(strides, status):
     for fn in (h.load().hippo_verify_attention_mass, h.load().hippo_draft_attention_mass):
         assert call(fn, ws_bytes=256, **strides) == status
+
+
+@pytest.mark.parametrize("case,part", [
+    (dict(mass=lambda m: m.double()), "mass.scalar_type() == at::kFloat"), (dict(mass=lambda m: m[0]), "mass.dim() == 3"),
+    (dict(mass=lambda m: m[:1]), "mass.size(0) == B"), (dict(mass=lambda m: m[:, :2]), "mass.size(1) == Hkv"),
+    (dict(mass=lambda m: m[:, :, :47]), "mass.size(2) >= n"),
+    (dict(mass=lambda m: m.transpose(1, 2).contiguous().transpose(1, 2)), "mass.stride(2) == 1"),
+    (dict(ctx=49), "n <= k.size(2)"), (dict(ctx=-1), "c.ctx_len >= 0"),
+    (dict(q=lambda q: q.bfloat16()), "c.q.scalar_type() == k.scalar_type()"), (dict(q=lambda q: q[:1]), "c.q.size(0) == B"),
+    (dict(q=lambda q: q[:, :0]), "c.q.size(1) >= 1"), (dict(q=lambda q: q[..., :32].contiguous()), "c.q.size(3) == k.size(3)"),
+    (dict(q=lambda q: q.transpose(0, 1)), "q.is_contiguous()"), (dict(q=lambda q: q[0]), "q.dim() == 4"),
+    (dict(k=lambda k: k[..., ::2]), "cache.stride(3) == 1"), (dict(k=lambda k: k[0]), "cache.dim() == 4"),
+    (dict(v=lambda v: v.bfloat16()), "v.scalar_type() == k.scalar_type()"),
+    (dict(v=lambda v: v.transpose(1, 2).contiguous().transpose(1, 2)), "same_layout(v, k)"), (dict(v=lambda v: v[:, :, :49]), "same_layout(v, k)"),
+    (dict(mass_out=torch.zeros(2, 3, 49)), "mass.size(2) >= n"), (dict(mass_out=torch.zeros(2, 3, 50).double()), "mass.scalar_type() == at::kFloat"),
+    (dict(mass_out=torch.zeros(2, 50, 3).transpose(1, 2)), "mass.stride(2) == 1"),
+    (dict(out=torch.zeros(2, 2, 6, 32)), "t.sizes() == sizes"), (dict(out=torch.zeros(2, 2, 6, 64).bfloat16()), "t.scalar_type() == type"),
+    (dict(out=torch.zeros(2, 6, 2, 64).transpose(1, 2)), "t.is_contiguous()"),
+    (dict(k_new=torch.zeros(2, 2, 3, 64)), "k_new.defined() == v_new.defined()"),
+    (dict(v_new=torch.zeros(2, 2, 3, 64)), "k_new.defined() == v_new.defined()"),
+    (dict(k_new=torch.zeros(2, 1, 3, 64), v_new=torch.zeros(2, 2, 3, 64)), "t->sizes()"),
+    (dict(k_new=torch.zeros(2, 2, 3, 64), v_new=torch.zeros(2, 2, 2, 64)), "t->sizes()"),
+    (dict(k_new=torch.zeros(2, 2, 3, 64), v_new=torch.zeros(2, 3, 2, 64).transpose(1, 2)), "t->is_contiguous()"),
+    (dict(k_new=torch.zeros(2, 2, 3, 64), v_new=torch.zeros(2, 2, 3, 64).bfloat16()), "t->scalar_type() == k.scalar_type()"),
+    (dict(), "tensors lie on the current device"),                # nothing else: host memory, which no kernel reads
+])
+@pytest.mark.parametrize("fn", [h.hippo_draft_attention_mass, h.hippo_verify_attention_mass])
+def test_the_binding_names_what_it_refuses(fn, case, part):
+    """(all of these tensors lie in host memory, which the last check refuses: each case has to fail at its own check, before it)"""
+    case = dict(case)
+    q, k, v, m = torch.zeros(2, 2, 6, 64), torch.zeros(2, 3, 50, 64), torch.zeros(2, 3, 50, 64), torch.zeros(2, 3, 48)
+    q, k, v, m = (case.pop(name, lambda x: x)(x) for name, x in (("q", q), ("k", k), ("v", v), ("mass", m)))
+    with pytest.raises(AssertionError, match=re.escape(part)):
+        fn(q, k, v, m, case.pop("ctx", 48), **case)

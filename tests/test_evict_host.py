@@ -2,6 +2,7 @@
 import ctypes as C
 import itertools
 import random
+import re
 
 import pytest
 import torch
@@ -127,3 +128,41 @@ def test_any_strides_of_dst():
         assert call(dst=dst, md=None, **few) == want, (B, Hkv, keep, sb, sh, sn)
         answers.add((want, B > 1 and Hkv > 1 and keep > 1))
     assert len(answers) == 4
+
+
+@pytest.mark.parametrize("case,part", [
+    (dict(mass=lambda m: m.double()), "mass.scalar_type() == at::kFloat"),
+    (dict(mass=lambda m: m[0]), "mass.dim() == 3"),
+    (dict(mass=lambda m: m[:1]), "k_src.size(0) == B"), (dict(mass=lambda m: m[:, :2]), "k_src.size(1) == Hkv"),
+    (dict(mass=lambda m: m[:, :, :40]), "mass.size(2) >= n"),
+    (dict(mass=lambda m: m.transpose(1, 2).contiguous().transpose(1, 2)), "mass.stride(2) == 1"),
+    (dict(v=lambda v: v.transpose(1, 2).contiguous().transpose(1, 2)), "same_layout(v_src, k_src)"),
+    (dict(v=lambda v: v[:, :, :49]), "same_layout(v_src, k_src)"),
+    (dict(v=lambda v: v.bfloat16()), "v_src.scalar_type() == k_src.scalar_type()"),
+    (dict(v=lambda v: None), "k_src.defined() == v_src.defined()"),
+    (dict(keep=0), "keep >= 1"), (dict(keep=51), "keep <= n"), (dict(n_first=-1), "first >= 0"), (dict(n_first=51), "first <= n"),
+    (dict(n_recent=-1), "recent >= 0"), (dict(n_recent=51), "recent <= n"),
+    (dict(n_rows=51), "integer(a[4]) <= n"), (dict(n_rows=0), "integer(a[4]) >= 1"),
+    (dict(idx_out=torch.zeros(2, 3, 21, dtype=torch.int32)), "t.sizes() == sizes"),
+    (dict(idx_out=torch.zeros(2, 3, 20)), "t.scalar_type() == type"),
+    (dict(idx_out=torch.zeros(3, 2, 20, dtype=torch.int32).transpose(0, 1)), "t.is_contiguous()"),
+    (dict(k_dst=torch.zeros(2, 3, 19, 64), v_dst=torch.zeros(2, 3, 19, 64)), "k_dst.size(2) >= keep"),
+    (dict(k_dst=torch.zeros(2, 3, 20, 32), v_dst=torch.zeros(2, 3, 20, 32)), "k_dst.size(3) == k_src.size(3)"),
+    (dict(k_dst=torch.zeros(2, 2, 20, 64), v_dst=torch.zeros(2, 2, 20, 64)), "k_dst.size(1) == Hkv"),
+    (dict(k_dst=torch.zeros(1, 3, 20, 64), v_dst=torch.zeros(1, 3, 20, 64)), "k_dst.size(0) == B"),
+    (dict(k_dst=torch.zeros(2, 3, 20, 64)), "v_dst.defined()"), (dict(v_dst=torch.zeros(2, 3, 20, 64)), "!v_dst.defined()"),
+    (dict(k_dst=torch.zeros(2, 3, 20, 64), v_dst=torch.zeros(2, 3, 21, 64)), "same_layout(v_dst, k_dst)"),
+    (dict(k_dst=torch.zeros(2, 3, 20, 64).bfloat16(), v_dst=torch.zeros(2, 3, 20, 64).bfloat16()),
+     "k_dst.scalar_type() == k_src.scalar_type()"),
+    (dict(mass_dst=torch.zeros(2, 3, 19)), "mass.size(2) >= n"),
+    (dict(mass_dst=torch.zeros(2, 3, 20).double()), "mass.scalar_type() == at::kFloat"),
+    (dict(k=lambda k: None, v=lambda v: None, k_dst=torch.zeros(2, 3, 20, 64), v_dst=torch.zeros(2, 3, 20, 64)), "a[8] == Py_None"),
+    (dict(), "tensors lie on the current device"),                # nothing else: host memory, which no kernel reads
+])
+def test_the_binding_names_what_it_refuses(case, part):
+    """(all of these tensors lie in host memory, which the last check refuses: each case has to fail at its own check, before it)"""
+    case = dict(case)
+    m, k, v = torch.zeros(2, 3, 50), torch.zeros(2, 3, 50, 64), torch.zeros(2, 3, 50, 64)
+    m, k, v = (case.pop(name, lambda x: x)(x) for name, x in (("mass", m), ("k", k), ("v", v)))
+    with pytest.raises(AssertionError, match=re.escape(part)):
+        h.hippo_evict_kv(m, case.pop("keep", 20), k, v, **case)

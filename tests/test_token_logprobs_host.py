@@ -1,5 +1,6 @@
 """Refusals of hippo_token_logprobs, without a GPU: the library answers before it launches anything."""
 import ctypes as C
+import re
 
 import pytest
 import torch
@@ -55,3 +56,24 @@ def test_the_binding_refuses_tensors_it_would_misread():
         h.hippo_token_logprobs(x, t)
     with pytest.raises(TypeError):
         h.hippo_token_logprobs(x.double(), t)
+
+
+@pytest.mark.parametrize("case,part", [
+    (dict(x=torch.zeros(64, 4).t()), "x.stride(-1) == 1"), (dict(x=torch.zeros(64)), "x.dim() >= 2"),
+    (dict(x=torch.zeros(2, 3, 64)[:, ::2], tokens=torch.zeros(2, 2, dtype=torch.int32)), "x.stride(i) == inside * step"),
+    (dict(x=torch.zeros(3, 2, 64).transpose(0, 1), tokens=torch.zeros(2, 3, dtype=torch.int32)), "x.stride(i) == inside * step"),
+    (dict(tokens=torch.zeros(4, dtype=torch.int64)), "tokens.scalar_type() == at::kInt"),
+    (dict(tokens=torch.zeros(3, dtype=torch.int32)), "tokens.sizes() =="), (dict(tokens=torch.zeros(2, 2, dtype=torch.int32)), "tokens.sizes() =="),
+    (dict(tokens=torch.zeros(8, dtype=torch.int32)[::2]), "tokens.is_contiguous()"),
+    (dict(logprob_out=torch.zeros(3)), "t.sizes() == sizes"), (dict(logprob_out=torch.zeros(8)[::2]), "t.is_contiguous()"),
+    (dict(entropy_out=torch.zeros(4, dtype=torch.float64)), "t.scalar_type() == type"), (dict(entropy_out=torch.zeros(4, 1)), "t.sizes() == sizes"),
+    (dict(n_top=2, top_ids_out=torch.zeros(4, 2)), "t.scalar_type() == type"),
+    (dict(n_top=2, top_ids_out=torch.zeros(4, 3, dtype=torch.int32)), "t.sizes() == sizes"),
+    (dict(n_top=2, top_logprobs_out=torch.zeros(2, 4).t()), "t.is_contiguous()"), (dict(n_top=-1), "n_top >= 0"),
+    (dict(), "tensors lie on the current device"),                # nothing else: host memory, which no kernel reads
+])
+def test_the_binding_names_what_it_refuses(case, part):
+    """(all of these tensors lie in host memory, which the last check refuses: each case has to fail at its own check, before it)"""
+    case = dict(case)
+    with pytest.raises(AssertionError, match=re.escape(part)):
+        h.hippo_token_logprobs(case.pop("x", torch.zeros(4, 64)), case.pop("tokens", torch.zeros(4, dtype=torch.int32)), **case)
