@@ -165,6 +165,40 @@ def test_strides_scale_and_given_buffers(hippo, dtype):
         hippo.hippo_verify_attention_mass(q, *views, m_in, ctx, workspace=ws[:-256])
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("H,d,ctx,q_len,splits", [
+    (8, 64, 200, 1, 0), (8, 128, 200, 3, 1), (8, 128, 1895, 1, 0), (28, 64, 900, 6, 7), (64, 128, 3001, 4, 0), (8, 64, 4097, 1, 64)])
+def test_infinite_and_nan_logits(hippo, dtype, H, d, ctx, q_len, splits):
+    """as a softmax has them, each in its KV head: logits of -inf give no weight (what lies at their rows is added to nothing),
+    one of +inf or NaN makes the head's weights and outputs NaN, and so do rows of -inf alone"""
+    q, k, v, mass = make(2, H, 4, d, ctx, q_len, dtype, 17)
+    q[..., 0] = q[..., 0].abs() + 0.5                            # so that a channel of -inf gives a logit of -inf
+    call = lambda k: hippo.hippo_verify_attention_mass(q, k, v, mass, ctx, want_lse=True, num_splits=splits)
+    clean, odd = call(k), k.clone()
+    gone = torch.zeros(ctx + q_len, dtype=torch.bool, device="cuda")
+    gone[:70], gone[ctx - 3:ctx] = True, True                     # whole tiles, and a piece of the last
+    odd[0, 1, gone, 0] = -math.inf
+    odd[0, 2, 5, 3] = math.nan
+    odd[0, 3, ctx // 2, 0] = math.inf
+    odd[1, 0, :, 0] = -math.inf
+    odd[1, 2, 0, 0] = -math.inf
+    out, total, lse = call(odd)
+    of_head = lambda x, b, h: x[b, :, h * (H // 4):(h + 1) * (H // 4)]
+    for b, h in ((0, 2), (0, 3), (1, 0)):
+        assert bool(of_head(out, b, h).isnan().all()) and bool(total[b, h].isnan().all())
+    for b, h in ((0, 0), (1, 1), (1, 3)):                         # the heads beside them
+        assert torch.equal(of_head(out, b, h), of_head(clean[0], b, h)) and torch.equal(total[b, h], clean[1][b, h])
+        assert torch.equal(lse[b, h * (H // 4):(h + 1) * (H // 4)], clean[2][b, h * (H // 4):(h + 1) * (H // 4)])
+    assert torch.equal(total[0, 1, gone], mass[0, 1, gone[:ctx]]) and torch.equal(total[1, 2, :1], mass[1, 2, :1])
+    # the others' weights are those of a cache without these rows, whose terms go through up to as many additions more
+    for b, h, rows in ((0, 1, gone), (1, 2, torch.arange(ctx + q_len, device="cuda") == 0)):
+        left, n = ~rows, int(rows.sum())
+        ref = reference(of_head(q, b, h)[None].contiguous(), k[b:b + 1, h:h + 1, left].contiguous(), v[b:b + 1, h:h + 1, left].contiguous(),
+                        ctx - n, mass[b:b + 1, h:h + 1, left[:ctx]].contiguous(), splits)
+        more = U * n * (ref[1] - torch.nn.functional.pad(mass[b:b + 1, h:h + 1, left[:ctx]].double(), (0, q_len))).abs()
+        check((of_head(out, b, h)[None], total[b:b + 1, h:h + 1, left]), (ref[0], ref[1], ref[2] + more), dtype, (b, h))
+
+
 def test_heads_far_apart(hippo):
     # the second KV head lies more than 2^32 bytes, and 2^31 elements, behind the first
     H, d, ctx = 4, 64, 200
