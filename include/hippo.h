@@ -301,11 +301,14 @@ int hippo_draft_attention_append(const void* q, int32_t q_len, const void* k_new
  *   mass_out[b, hk, n] = (n < ctx_len ? mass_in[b, hk, n] : 0)
  *                        + sum over the new rows i and the query heads h of KV head hk of softmax_n(...)[b, i, h],
  *   n in [0, ctx_len + q_len); a new row i gives nothing to rows behind ctx_len + i.
- * out and lse_out as without mass, but that the slices' outputs reach the merge in fp32.  The weights are fp32 from fp32
- * logits, of the probabilities before any rounding; sums run in a fixed order.  Rows that a verification rejects leave their share
- * in older rows' mass; their own rows' mass is written anew with the rows.
- * mass: `in` may be NULL (nothing accumulated yet) or `out` (in place, the same strides), and does not overlap it otherwise; element (b, hk, n) lies at
- * b * stride_b + hk * stride_h + n.  Elements of `out` from ctx_len + q_len on are left as they were.
+ * out and lse_out as without mass (over bf16 caches, of probabilities rounded to bf16: lse_out is within 2^-8 of the unrounded
+ * one's), but that the slices' outputs reach the merge in fp32.  The weights are fp32 from fp32 logits, of the probabilities before
+ * any rounding; sums run in a fixed order.
+ * Several new rows are those that a draft model takes in at once, such as the words that a verification accepted.  Every row's
+ * weights are added: there is no call that takes back the share of rows that are dropped afterwards (their own rows' mass is written
+ * anew with the rows), so a chain that may still be rejected is best attended to without mass.
+ * mass: `in` may be NULL (nothing accumulated yet) or `out` (in place, the same strides), and does not overlap it otherwise; element
+ * (b, hk, n) lies at b * stride_b + hk * stride_h + n.  Elements of `out` from ctx_len + q_len on are left as they were.
  * k_new, v_new: both NULL (the caches hold the new rows), or the rows to append, as in the *_append calls.  Caches: F32 or BF16,
  * contiguous.  Workspace: hippo_attention_mass_workspace_bytes, with seq_len = ctx_len + q_len; it grows with seq_len times the
  * query rows.

@@ -401,8 +401,9 @@ def hippo_spec_verify(p_logits, q_logits, draft_tokens, u_accept, u_sample, temp
 
 def hippo_token_logprobs(logits, tokens, temperature: float = 1.0, n_top: int = 0, logprob_out=None, entropy_out=None,
                          top_ids_out=None, top_logprobs_out=None, workspace=None, stream=None):
-    """logits [..., V] (rows may be padded, and lie evenly spaced), tokens [...] int32 -> (logprob [...], entropy [...]) fp32,
-    with n_top > 0 also (top_ids [..., n_top] int32, top_logprobs [..., n_top] fp32), the most likely word first."""
+    """logits [..., V] (rows may be padded, lie evenly spaced and start at multiples of 16 bytes), tokens [...] int32 ->
+    (logprob [...], entropy [...]) fp32, with n_top > 0 also (top_ids [..., n_top] int32, top_logprobs [..., n_top] fp32), the most
+    likely word first."""
     return _call(stream, (_native or _bound()).token_logprobs, logits, tokens, temperature, n_top, logprob_out, entropy_out,
                  top_ids_out, top_logprobs_out, workspace)
 

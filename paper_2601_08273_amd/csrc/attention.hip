@@ -169,7 +169,8 @@ __device__ __forceinline__ bf16x8 e4m3x8_to_bf16(int lo, int hi) {
 // TT = tokens per tile (16 or 32), NST = ring stages (super-tiles resident in LDS)
 // MODE: 0 = contiguous cache, 1 = contiguous cache with appended-row fusion, 2 = paged cache
 // ONE = the slice is the whole cache: the block writes its rows' output
-// MASS = for attn_combine_mass: the denominators of the probabilities as they are, before their rounding to bf16, and the logits
+// MASS = the call sums its weights: the denominators of the probabilities as they are, before their rounding to bf16, and the logits go
+// to the merge as well (of one slice, to mass_of_block)
 template <int D, int RB, int TG, int TT, int NST, int MODE, bool KV8 = false, bool NT = false, bool ROT = false,
           bool ONE = false, bool MASS = false>
 __global__ __launch_bounds__(RB * TG * 64) void attn_partial_grid(ParamsOf<MASS> p) {
@@ -463,6 +464,9 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_partial_grid(ParamsOf<MASS>
     const float neg_m = (m_run == -INFINITY) ? 0.f : -m_run;
     // the PV product sees P rounded to bf16; the denominator sums the same rounded values.  Two
     // probabilities are rounded by one packed conversion and read back with a shift and a mask.
+    // (The matrix unit takes V's type for both operands.  Numerator and denominator rounded alike, a token that has nearly all the
+    // weight keeps its row of V; many tokens' roundings average out: the output's error is 2.3e-3 where one of P in fp32 has 1.7e-3,
+    // its own rounding.  The row statistic that a caller may ask for goes with the output: it is of the rounded ones, within 2^-8.)
     unsigned pk[TB * 2];
     float psum = 0.f;
 #pragma unroll
@@ -945,7 +949,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_partial_f32(ParamsOf<MASS> 
 // Attention mass: mass_out[n] = (n < ctx_len ? mass_in[n] : 0) + sum over the KV head's rows of 2^(z - m*) / l*
 // A row's weights need its statistics over the whole cache, which are known once every slice is done: the launch that merges the
 // slices is the first that can sum them.  Its blocks in front take the tokens (kMassTile each), the others merge a row each.
-// l* sums the probabilities as they are: the output's denominator, of those rounded to bf16, is off by up to 2^-9 where one
+// l* sums the probabilities as they are: the output's denominator, of those rounded to bf16, is off by up to 2^-8 where one
 // token has most of the weight, and so would the weights be.
 // The logits z are in memory, where the slices left them: 8 bytes a row and token, written and read, where K again would be 2 D and
 // another set of products.  us a call, logits -> K again: 16640 x 4 heads x 128, 21 rows 17.2 -> 19.6, 42 rows 21.5 -> 20.4, 63 rows

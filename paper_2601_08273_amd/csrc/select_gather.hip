@@ -125,7 +125,9 @@ __device__ __forceinline__ long long gather_offset(long long row, const SelectPa
 // the scanning wave, which own runs of 64 consecutive bins, hit different LDS banks.  Nothing reads it once a key is emitted.
 // ANY: the scores start anywhere and are any number, as between the first and the recent rows of a head's mass: 16-byte loads that
 // are 4-byte aligned, and the vector that the end cuts is taken from the last four scores (16400 scores a head x 4, 8192 kept: 14.3 ->
-// 12.4 us with them); and rows of mass 0 may be many (all of 33152 a head x 4: 99 -> 26 us).
+// 12.4 us with them); and rows of mass 0 may be many (all of 33152 a head x 4: 99 -> 25 us).  That count is of zeros, in waves where
+// three probes see them, of keys in registers: other equal masses still take turns (all of 33152 alike 98 us), and so do all of them
+// where the scores are read anew in every pass (80001 a head x 4: any 112, all 0 or all alike 276).
 template <int NC, bool ANY = false, typename Emit>
 __device__ __forceinline__ void select_top(const float* sc, const int Nv, const int k, unsigned* const hist, Emit emit) {
   constexpr bool CACHED = NC > 0;
@@ -596,7 +598,10 @@ hipError_t launch_evict(const EvictParams& p, hipStream_t st) {
   const int vpr = p.D * p.elem_bytes / 16;                 // 16-byte vectors per row: 4, 8, 16 or 32
   int vpr_shift = 0;
   while ((1 << vpr_shift) < vpr) ++vpr_shift;
-  // One launch or two by the rules of launch_select_gather, whose kernels these are but for a selection a head.
+  // One launch or two by the rules of launch_select_gather, whose kernels these are but for a selection a head.  Its rule for
+  // streams that are being captured is left out: beyond 16384 rows two launches save a little where few rows stay, and lose more where
+  // many do (us a call in a graph, one launch -> two, 4 heads: 20000 rows, 1000 kept 14.8 -> 14.5; 24000, 1000 kept 16.6 -> 15.8, 8000
+  // kept 19.2 -> 21.8).
   const long long heads = (long long)p.B * p.Hkv, per_head = (long long)p.keep << vpr_shift;
   const bool one_launch = p.k_dst != nullptr && n_chunks <= kGatherKeys && p.k <= kHistWords && per_head <= (1ll << 24) &&
                           per_head * heads <= (128ll << 20) / 64 && heads <= (n_chunks <= kShortKeys ? 2 * kNumCU : kNumCU);
