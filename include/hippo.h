@@ -461,7 +461,8 @@ int hippo_spec_verify(const void* p_logits, const void* q_logits, int32_t dtype,
  * logits [rows, stride_row], dtype F32 or BF16, rows 16-byte aligned, stride_row >= vocab; the first `vocab` entries of a row
  * are read.  tokens [rows] int32; outputs fp32 [rows], int32 and fp32 [rows, n_top].  1 <= rows <= 2^22, vocab <= 2^20,
  * 0 <= n_top <= 32 and <= vocab, temperature > 0 and finite (at least 1e-38).  Sums are fp32, of the words other than
- * the largest, so that a row whose best word has nearly all the weight keeps its entropy.  Deterministic.
+ * the largest, so that a row whose best word has nearly all the weight keeps its entropy (words below 2^-126 of the best one's weight
+ * add nothing to the sums).  Deterministic.
  * Errors: NULL_ARG, BAD_SHAPE, BAD_DTYPE, BAD_ALIGN, WORKSPACE_TOO_SMALL, HIP.
  */
 size_t hippo_token_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t dtype, int32_t n_top);
