@@ -12,6 +12,8 @@
  *                        hippo_spec_verify (the speculative-sampling verdict of Eq. 1),
  *                        hippo_*_attention_mass with hippo_evict_kv (a draft cache that stays within a budget),
  *                        hippo_token_logprobs (log probabilities of an answer's words),
+ *                        hippo_prefill_attention* (prompts, packed or over pages), hippo_tree_attention* (trees of drafted
+ *                        tokens), hippo_plan_pages and hippo_write_kv_paged (what fills a paged cache),
  *                        hippo_vpsd_* (host-side control of the parallel decoding rounds).
  *
  * Conventions common to every entry point
@@ -470,6 +472,114 @@ int hippo_token_logprobs(const void* logits, int32_t dtype, int64_t stride_row, 
                          int32_t vocab, float temperature, int32_t n_top,
                          float* logprob_out, float* entropy_out, int32_t* top_ids_out, float* top_logprobs_out,
                          void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Attention of whole prompts, or of their next pieces: what fills a model's hidden states behind the rows that verification and draft
+ * decoding start from.  The sequences' rows lie one behind the other, without padding.
+ *   sequence b: query rows cu_q[b] .. cu_q[b+1] - 1 and key rows cu_k[b] .. cu_k[b+1] - 1 (len_q and len_k of them), the last ones
+ *   of both being the same tokens
+ *   out[cu_q[b] + i, h, :] = sum_n softmax_n(softmax_scale * q[cu_q[b] + i, h, :] . K[cu_k[b] + n, h/G, :]) V[cu_k[b] + n, h/G, :],
+ *   n in [0, len_k - len_q + i]
+ * cu_q, cu_k [n_seqs + 1] int32 on the DEVICE, ascending, within [0, total_q] and [0, total_k]; cu_k = cu_q for whole prompts.
+ * Sequences may be empty.  Rows of q that belong to no sequence are not read, and their rows of out and lse_out are left as
+ * they were.  (Offsets outside the buffers are cut off at their ends, and of a descending pair no row is taken: the
+ * result is then meaningless, but no access leaves the buffers.)
+ * A row that sees nothing (len_q > len_k), or whose logits are all -inf, gives zeros and lse -inf.  What K and V hold at rows that a
+ * query row does not see, infinities and NaN included, does not reach that row.
+ * q [total_q, H, d], k and v [total_k, H_kv, d], with the strides of desc: slices of one fused projection's output will do.  out
+ * [total_q, H, d] contiguous, dtype desc->dtype (F32 or BF16); lse_out optional [H, total_q] fp32.  softmax_scale <= 0 means
+ * 1/sqrt(d).  num_splits: blocks that share a tile of query rows (up to 64), 0 = library's choice; the result does not depend on it beyond
+ * rounding.  fp32 throughout, but that over bf16 the probabilities are rounded to bf16 before their product with V (and summed as
+ * rounded).  total_q = 0 does nothing.  Workspace: hippo_prefill_workspace_bytes.
+ * Errors: NULL_ARG, BAD_SHAPE (also more than 65535 sequences, 2^30 query rows times heads), BAD_DTYPE, BAD_ALIGN,
+ *         WORKSPACE_TOO_SMALL, HIP.
+ */
+typedef struct hippo_packed_desc {
+  int32_t n_q_heads, n_kv_heads, head_dim, dtype;
+  int64_t q_stride_n, q_stride_h;     /* elements, from token to token and from head to head */
+  int64_t kv_stride_n, kv_stride_h;   /* of k and v alike */
+} hippo_packed_desc;
+
+size_t hippo_prefill_workspace_bytes(const hippo_packed_desc* desc, int32_t total_q, int32_t total_k, int32_t n_seqs, int32_t num_splits);
+int hippo_prefill_attention(const void* q, int32_t total_q, const void* k, const void* v, int32_t total_k,
+                            const hippo_packed_desc* desc, const int32_t* cu_q, const int32_t* cu_k, int32_t n_seqs,
+                            float softmax_scale, int32_t num_splits, void* out, float* lse_out,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The same over a paged cache (hippo_paged_kv_desc, with batch = n_seqs) that already holds the new rows: sequence b's key row n lies
+ * where block_table says, and len_k = kv_lens[b] (int32 on the device, cut off at max_pages * page_size).  Workspace:
+ * hippo_prefill_workspace_bytes with total_k = max_pages * page_size.
+ */
+int hippo_prefill_attention_paged(const void* q, int32_t total_q, int64_t q_stride_n, int64_t q_stride_h,
+                                  const void* k_pool, const void* v_pool, const int32_t* block_table,
+                                  const hippo_paged_kv_desc* kv, const int32_t* cu_q, const int32_t* kv_lens,
+                                  float softmax_scale, int32_t num_splits, void* out, float* lse_out,
+                                  void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Verification of a tree of drafted tokens: where a chain's node sees everything before it, a tree's sees the context, its ancestors
+ * and itself.
+ *   out[b, i, h, :] as hippo_verify_attention's, over n in [0, ctx) and ctx + j for every node j on the way from node i to the root
+ *   parents[b, i]: the parent of node i, a node before it; -1: the context's last token.  Anything else (-2, say): there is no
+ *   such node (a batch's smaller trees are padded with them), nor its descendants: its row of out is zeros, its lse -inf, and no
+ *   node sees it, whatever its rows of K and V hold.
+ * n_nodes 1 .. 64.  The cache holds node j's own K and V at row ctx + j, at ctx + n_nodes rows in all.  ctx is ctx_lens[b] (int32
+ * [B] on the DEVICE: every sequence has its own length, and a captured graph follows them; cut off at seq_len - n_nodes), or ctx_len where
+ * ctx_lens is NULL.  seq_len: rows that the cache has room for.  parents [B, n_nodes] int32 on the device, parents_stride_b
+ * elements from one batch element to the next (0: one tree for all).  q, out [B, n_nodes, H, d] contiguous; lse_out optional [B, H, n_nodes].
+ * softmax_scale, num_splits, rounding, unseen rows as hippo_prefill_attention.  Workspace: hippo_tree_workspace_bytes.
+ * The accepted path's rows are afterwards moved to ctx, ctx + 1, ...: over pages by hippo_plan_pages (which gives the tree's
+ * rows back) and hippo_write_kv_paged (which picks rows).
+ * Errors: NULL_ARG, BAD_SHAPE, BAD_DTYPE, BAD_ALIGN, WORKSPACE_TOO_SMALL, HIP.
+ */
+size_t hippo_tree_workspace_bytes(const hippo_kv_desc* kv, int32_t n_nodes, int32_t seq_len, int32_t num_splits);
+int hippo_tree_attention(const void* q, int32_t n_nodes, const void* k_cache, const void* v_cache, const hippo_kv_desc* kv,
+                         int32_t seq_len, const int32_t* parents, int64_t parents_stride_b,
+                         const int32_t* ctx_lens, int32_t ctx_len, float softmax_scale, int32_t num_splits,
+                         void* out, float* lse_out, void* workspace, size_t workspace_bytes, void* stream);
+/* over pages: seq_len = max_pages * page_size (in hippo_tree_workspace_bytes too, whose kv's strides are then not used) */
+int hippo_tree_attention_paged(const void* q, int32_t n_nodes, const void* k_pool, const void* v_pool, const int32_t* block_table,
+                               const hippo_paged_kv_desc* kv, const int32_t* parents, int64_t parents_stride_b,
+                               const int32_t* ctx_lens, int32_t ctx_len, float softmax_scale, int32_t num_splits,
+                               void* out, float* lse_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The pages of a step, from the requests' lengths, without the host: request b has ctx_lens[b] rows in the cache and gets new_lens[b]
+ * more, or gives its last -new_lens[b] back (rejected drafts; all of them: the request is done).  All pointers are device int32.
+ *   1. given back: the pages behind ceil((ctx + new) / page_size) of every request with new < 0 go on the stack of free pages
+ *      (free_pages[0 .. n_free[0]) are free, the last is on top), request by request, each in the order of its table row
+ *   2. admitted: request b with new >= 0 if its rows fit its row of the table and, where it needs pages or slots at all, the pages
+ *      that the requests with new >= 0 up to and with b need are free and their new rows at most max_tokens
+ *   3. the admitted requests take their new pages off the stack, top first, in their order, into the next entries of their row
+ * kv_lens_out[b] = the rows that b has then: ctx where it was not admitted.
+ * cu_q_out [batch + 1]: offsets of the admitted new rows, 0 for the requests that bring none (hippo_prefill_attention_paged's cu_q)
+ * slots_out [max_tokens]: new row t's place in the pool, page * page_size + row in the page; positions_out: its row of the request.
+ *   Both are -1 from cu_q_out[batch] on, and a slot is where its page is none of the pool's.
+ * n_free_out [1]: how many pages are free then.  free_pages [n_pool_pages] and block_table [batch, max_pages] are written in place:
+ * new entries only, those given back stay where they stood.  (So a call may be repeated: as long as n_free and the lengths are
+ * the old ones it finds the same.)  ctx_lens, new_lens and n_free may not be outputs at the same time.
+ * Negative ctx_lens count as 0, n_free as at most n_pool_pages.  page_size a power of two, 16..256; batch <= 4096; max_tokens,
+ * n_pool_pages and max_pages <= 2^22, batch * max_pages <= 2^30.  Deterministic.
+ * Errors: NULL_ARG, BAD_SHAPE, BAD_ALIGN, HIP.
+ */
+int hippo_plan_pages(const int32_t* ctx_lens, const int32_t* new_lens, int32_t batch,
+                     int32_t* block_table, int32_t max_pages, int32_t* free_pages, int32_t n_pool_pages, const int32_t* n_free,
+                     int32_t page_size, int32_t max_tokens, int32_t* slots_out, int32_t* positions_out, int32_t* cu_q_out,
+                     int32_t* kv_lens_out, int32_t* n_free_out, void* stream);
+
+/*
+ * K and V rows into the pages: row rows[t] (t where rows is NULL) of k_new and v_new goes to slot slots[t], t < n_tokens, for every KV
+ * head, bit copies.  Tokens whose slot is outside the pool or whose row is outside [0, n_rows) are skipped, so that a step padded
+ * to a fixed size needs no count.  A slot that is named twice holds pieces of either row.
+ * k_new, v_new: element (row, hk, c) at row * stride_n + hk * stride_h + c, dtype kv->dtype (F32 or BF16); kv's batch, n_q_heads and
+ * max_pages are not looked at.  slots, rows: int32 [n_tokens] on the device.  The pools must not overlap k_new, v_new or each
+ * other.  n_tokens = 0 does nothing.
+ * Errors: NULL_ARG, BAD_SHAPE (also a pool whose rows would meet), BAD_DTYPE, BAD_ALIGN, HIP.
+ */
+int hippo_write_kv_paged(const void* k_new, const void* v_new, int32_t n_rows, int64_t stride_n, int64_t stride_h,
+                         const int32_t* slots, const int32_t* rows, int32_t n_tokens,
+                         void* k_pool, void* v_pool, const hippo_paged_kv_desc* kv, void* stream);
 
 /* ------------------------------------------------------------------------------------------
  * Host-side control of video parallel speculative decoding (Method, "Video Parallel Speculative

@@ -31,7 +31,10 @@ EXPORTS = ("hippo_status_string", "hippo_workspace_bytes", "hippo_score_tokens",
            "hippo_verify_attention_fp8kv", "hippo_draft_attention_fp8kv",
            "hippo_quantize_kv_workspace_bytes", "hippo_quantize_kv_e4m3",
            "hippo_spec_verify_workspace_bytes", "hippo_spec_verify",
-           "hippo_token_logprobs_workspace_bytes", "hippo_token_logprobs", "hippo_vpsd_prefill_buffer",
+           "hippo_token_logprobs_workspace_bytes", "hippo_token_logprobs",
+           "hippo_prefill_workspace_bytes", "hippo_prefill_attention", "hippo_prefill_attention_paged",
+           "hippo_tree_workspace_bytes", "hippo_tree_attention", "hippo_tree_attention_paged",
+           "hippo_plan_pages", "hippo_write_kv_paged", "hippo_vpsd_prefill_buffer",
            "hippo_vpsd_init", "hippo_vpsd_plan", "hippo_vpsd_commit", "hippo_vpsd_simulate")
 VPSD_CONSERVATIVE, VPSD_OPTIMISTIC = 0, 1
 POLICY_AUTOREGRESSIVE, POLICY_SERIAL_SD, POLICY_VPSD = 0, 1, 2
@@ -59,6 +62,11 @@ class PagedKvDesc(C.Structure):
                 ("head_dim", C.c_int32), ("dtype", C.c_int32), ("page_size", C.c_int32),
                 ("max_pages", C.c_int32), ("n_pool_pages", C.c_int32),
                 ("stride_page", C.c_int64), ("stride_n", C.c_int64), ("stride_h", C.c_int64)]
+
+
+class PackedDesc(C.Structure):
+    _fields_ = [("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+                ("q_stride_n", C.c_int64), ("q_stride_h", C.c_int64), ("kv_stride_n", C.c_int64), ("kv_stride_h", C.c_int64)]
 
 
 class MassDesc(C.Structure):
@@ -157,6 +165,19 @@ def load():
     lib.hippo_token_logprobs_workspace_bytes.restype = C.c_size_t
     lib.hippo_token_logprobs.argtypes = [vp, i32, i64, vp, i32, i32, f32, i32, vp, vp, vp, vp, vp, sz, vp]
     lib.hippo_token_logprobs.restype = C.c_int
+    pkp, pgp = C.POINTER(PackedDesc), C.POINTER(PagedKvDesc)
+    lib.hippo_prefill_workspace_bytes.argtypes = [pkp, i32, i32, i32, i32]
+    lib.hippo_tree_workspace_bytes.argtypes = [kvp, i32, i32, i32]
+    lib.hippo_prefill_workspace_bytes.restype = lib.hippo_tree_workspace_bytes.restype = sz
+    lib.hippo_prefill_attention.argtypes = [vp, i32, vp, vp, i32, pkp, vp, vp, i32, f32, i32, vp, vp, vp, sz, vp]
+    lib.hippo_prefill_attention_paged.argtypes = [vp, i32, i64, i64, vp, vp, vp, pgp, vp, vp, f32, i32, vp, vp, vp, sz, vp]
+    lib.hippo_tree_attention.argtypes = [vp, i32, vp, vp, kvp, i32, vp, i64, vp, i32, f32, i32, vp, vp, vp, sz, vp]
+    lib.hippo_tree_attention_paged.argtypes = [vp, i32, vp, vp, vp, pgp, vp, i64, vp, i32, f32, i32, vp, vp, vp, sz, vp]
+    lib.hippo_plan_pages.argtypes = [vp, vp, i32, vp, i32, vp, i32, vp, i32, i32, vp, vp, vp, vp, vp, vp]
+    lib.hippo_write_kv_paged.argtypes = [vp, vp, i32, i64, i64, vp, vp, i32, vp, vp, pgp, vp]
+    for fn in (lib.hippo_prefill_attention, lib.hippo_prefill_attention_paged, lib.hippo_tree_attention,
+               lib.hippo_tree_attention_paged, lib.hippo_plan_pages, lib.hippo_write_kv_paged):
+        fn.restype = C.c_int
     _lib = lib
     return lib
 
@@ -406,6 +427,54 @@ def hippo_token_logprobs(logits, tokens, temperature: float = 1.0, n_top: int = 
     likely word first."""
     return _call(stream, (_native or _bound()).token_logprobs, logits, tokens, temperature, n_top, logprob_out, entropy_out,
                  top_ids_out, top_logprobs_out, workspace)
+
+
+def hippo_prefill_attention(q, k, v, cu_q, cu_k=None, softmax_scale: float = 0.0, num_splits: int = 0, want_lse: bool = False,
+                            out=None, workspace=None, stream=None):
+    """Causal attention of packed prompts: q [T,H,d], k / v [T,Hkv,d] (slices of one fused projection's output will do), cu_q
+    [n_seqs+1] int32 on the device, the sequences' offsets -> out [T,H,d] (and lse [H,T] fp32).  cu_k: offsets of longer key
+    sequences (k / v [Tk,Hkv,d]) whose last rows the queries are.  Rows of `out` that belong to no sequence stay as they were."""
+    return _call(stream, (_native or _bound()).prefill, q, k, v, cu_q, cu_k, softmax_scale, num_splits, want_lse, out, workspace)
+
+
+def hippo_prefill_attention_paged(q, k_pool, v_pool, block_table, cu_q, kv_lens, softmax_scale: float = 0.0, num_splits: int = 0,
+                                  want_lse: bool = False, out=None, workspace=None, stream=None):
+    """The same over pools [n_pages, page_size, Hkv, d] that hold the new rows already: block_table [n_seqs, max_pages], cu_q
+    [n_seqs+1], kv_lens [n_seqs] (rows of each sequence, the new ones included), all int32 on the device."""
+    return _call(stream, (_native or _bound()).prefill_paged, q, k_pool, v_pool, block_table, cu_q, kv_lens, softmax_scale, num_splits,
+                 want_lse, out, workspace)
+
+
+def hippo_tree_attention(q, k_cache, v_cache, parents, ctx_lens, softmax_scale: float = 0.0, num_splits: int = 0,
+                         want_lse: bool = False, out=None, workspace=None, stream=None):
+    """Verification of a tree of drafted tokens: q [B,n_nodes,H,d], caches [B,Hkv,N,d] with node j's K / V at row ctx + j, parents
+    [B,n_nodes] (or [n_nodes], one tree for all) int32 on the device: a node before it, -1 for the context's last token, -2 where
+    there is no such node.  ctx_lens: [B] int32 on the device, or one number -> out [B,n_nodes,H,d] (and lse [B,H,n_nodes])."""
+    return _call(stream, (_native or _bound()).tree, q, k_cache, v_cache, parents, ctx_lens, softmax_scale, num_splits, want_lse, out,
+                 workspace)
+
+
+def hippo_tree_attention_paged(q, k_pool, v_pool, block_table, parents, ctx_lens, softmax_scale: float = 0.0, num_splits: int = 0,
+                               want_lse: bool = False, out=None, workspace=None, stream=None):
+    """The same over pools [n_pages, page_size, Hkv, d]; block_table [B, max_pages] int32 on the device."""
+    return _call(stream, (_native or _bound()).tree_paged, q, k_pool, v_pool, block_table, parents, ctx_lens, softmax_scale, num_splits,
+                 want_lse, out, workspace)
+
+
+def hippo_plan_pages(ctx_lens, new_lens, block_table, free_pages, n_free, page_size: int, max_tokens: int, slots_out=None,
+                     positions_out=None, cu_q_out=None, kv_lens_out=None, n_free_out=None, stream=None):
+    """The pages of a step, from lengths on the device: ctx_lens, new_lens [B] int32 (new < 0: rows given back), block_table
+    [B,max_pages] and the stack free_pages [n_pool] with n_free [1] of them free -> (slots [max_tokens], positions [max_tokens],
+    cu_q [B+1], kv_lens [B], n_free [1]) int32.  block_table and free_pages are written in place; requests whose pages or slots do
+    not suffice are not admitted (their kv_lens stay)."""
+    return _call(stream, (_native or _bound()).plan_pages, ctx_lens, new_lens, block_table, free_pages, n_free, page_size, max_tokens,
+                 slots_out, positions_out, cu_q_out, kv_lens_out, n_free_out)
+
+
+def hippo_write_kv_paged(k_new, v_new, slots, k_pool, v_pool, rows=None, stream=None) -> None:
+    """k_new / v_new [T,Hkv,d] into the pools [n_pages, page_size, Hkv, d]: row t (rows[t] where `rows` is given) to slot slots[t];
+    tokens with a slot or row of -1 are skipped."""
+    return _call(stream, (_native or _bound()).write_pages, k_new, v_new, slots, k_pool, v_pool, rows)
 
 
 # ---------------------------------------------------------------------------------------------

@@ -18,7 +18,8 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libhippo.so")
 BINDING = os.path.join(HERE, "_binding.so")
-SOURCES = ["api.hip", "attention.hip", "logprobs.hip", "quantize.hip", "score.hip", "select_gather.hip", "spec_verify.hip", "vpsd.cpp"]
+SOURCES = ["api.hip", "attention.hip", "logprobs.hip", "pages.hip", "prefill.hip", "quantize.hip", "score.hip", "select_gather.hip", "spec_verify.hip",
+           "tree.hip", "vpsd.cpp"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",   # no packed-fp32 instruction forms
@@ -56,7 +57,7 @@ def _build_binding() -> None:
 
 def build(extra_flags=(), verbose: bool = True) -> str:
     os.makedirs(OBJ, exist_ok=True)
-    with ThreadPoolExecutor(max_workers=4) as ex:
+    with ThreadPoolExecutor(max_workers=6) as ex:
         binding = ex.submit(_build_binding)
         objs = list(ex.map(lambda s: _compile(s, list(extra_flags)), SOURCES))
         binding.result()

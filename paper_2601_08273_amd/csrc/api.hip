@@ -6,7 +6,7 @@
 #include <algorithm>
 #include <atomic>
 
-#include "common.h"
+#include "rows_attention.h"
 
 using namespace hippo;
 
@@ -360,6 +360,98 @@ int plan_spec(int batch, int gamma, int vocab, int dtype, SpecPlan* pl) {
   pl->off_arrived = stats + cells;
   pl->bytes = stats + cells + align_up((size_t)batch * sizeof(int), 256);
   return HIPPO_OK;
+}
+
+// ---- attention of many rows: planning -------------------------------------------------------------
+constexpr int kMaxRowSplits = 64;   // the merge keeps a split's statistics in a lane
+
+// rows: query rows of a KV head, over all sequences; ragged: sequences that may leave a tile each; seen: tokens that the longest may
+// see; tokens: rows of q
+void plan_rows(RowsPlan* pl, int dtype, int head_dim, long long rows, int ragged, long long seen, int Hkv, int H, long long tokens,
+               int rb, int num_splits) {
+  pl->rb = rb;
+  pl->n_tiles = (int)(rows / (32 * rb) + ragged);
+  const long long blocks = std::max<long long>(1, (rows + 32 * rb - 1) / (32 * rb)) * Hkv;
+  long long S = num_splits;
+  if (S == 0) S = std::min<long long>(kNumCU / blocks, seen / 512);
+  S = std::max<long long>(1, std::min<long long>(S, std::min<long long>(kMaxRowSplits, (seen + 63) / 64)));
+  if (tokens * H > (1 << 25)) S = 1;                          // (the merge's launch: 64 threads a row and head, below 2^32)
+  pl->S = (int)S;
+  const size_t slots = S > 1 ? (size_t)S * tokens * H : 0;
+  pl->off_m = align_up(slots * head_dim * sizeof(float), 256);
+  pl->off_l = pl->off_m + align_up(slots * sizeof(float), 256);
+  pl->bytes = std::max<size_t>(256, pl->off_l + align_up(slots * sizeof(float), 256));
+  (void)dtype;
+}
+
+int check_packed(const hippo_packed_desc* d) {
+  if (d == nullptr) return HIPPO_ERR_NULL_ARG;
+  if (d->dtype != HIPPO_DTYPE_F32 && d->dtype != HIPPO_DTYPE_BF16) return HIPPO_ERR_BAD_DTYPE;
+  if (d->n_kv_heads < 1 || d->n_q_heads < 1 || d->n_q_heads % d->n_kv_heads != 0) return HIPPO_ERR_BAD_SHAPE;
+  if (d->n_q_heads > 65535 || (d->head_dim != 64 && d->head_dim != 128)) return HIPPO_ERR_BAD_SHAPE;
+  if (d->q_stride_n < 0 || d->q_stride_h < 0 || d->kv_stride_n < 0 || d->kv_stride_h < 0) return HIPPO_ERR_BAD_SHAPE;
+  const int per16 = 16 / elem_bytes(d->dtype);
+  if (d->q_stride_n % per16 || d->q_stride_h % per16 || d->kv_stride_n % per16 || d->kv_stride_h % per16) return HIPPO_ERR_BAD_ALIGN;
+  return HIPPO_OK;
+}
+
+// total_k: rows of packed K and V, or the most that a sequence's pages hold
+int plan_prefill(const hippo_packed_desc* d, int total_q, int total_k, int n_seqs, int num_splits, RowsPlan* pl) {
+  if (total_q < 0 || total_k < 0 || n_seqs < 1 || n_seqs > 65535 || num_splits < 0) return HIPPO_ERR_BAD_SHAPE;
+  const int G = d->n_q_heads / d->n_kv_heads;
+  const long long rows = (long long)total_q * G;
+  // (block and thread numbers of the launches, and a merge's wave for every row of q and query head)
+  if (rows > (1 << 30) || (long long)total_q * d->n_q_heads > (1 << 30) || total_k > 0x7fffff00) return HIPPO_ERR_BAD_SHAPE;
+  int rb = 8;
+  while (rb > 1 && rows * d->n_kv_heads / (32 * rb) < 192) rb /= 2;
+  plan_rows(pl, d->dtype, d->head_dim, rows, n_seqs, total_k, d->n_kv_heads, d->n_q_heads, total_q, rb, num_splits);
+  if ((long long)pl->n_tiles * d->n_kv_heads > (1 << 30) / 512) return HIPPO_ERR_BAD_SHAPE;
+  return HIPPO_OK;
+}
+
+int plan_tree(const hippo_kv_desc* kv, int nodes, long long seq_len, int num_splits, RowsPlan* pl) {
+  if (nodes < 1 || nodes > 64 || seq_len < nodes || seq_len > 0x7fffff00ll || num_splits < 0) return HIPPO_ERR_BAD_SHAPE;
+  const int G = kv->n_q_heads / kv->n_kv_heads;
+  if (G > 4096) return HIPPO_ERR_BAD_SHAPE;
+  const int R = G * nodes;
+  int rb = 8;
+  while (rb > 1 && R <= 16 * rb) rb /= 2;
+  const int per_seq = (R + 32 * rb - 1) / (32 * rb);
+  plan_rows(pl, kv->dtype, kv->head_dim, (long long)per_seq * 32 * rb * kv->batch, 0, seq_len, kv->n_kv_heads, kv->n_q_heads,
+            (long long)kv->batch * nodes, rb, num_splits);
+  if ((long long)pl->n_tiles * kv->n_kv_heads > (1 << 30) / 512 || (long long)kv->batch * nodes * kv->n_q_heads > (1 << 30))
+    return HIPPO_ERR_BAD_SHAPE;
+  return HIPPO_OK;
+}
+
+// A pool as the kernels take it: every element of a page lies inside the page's stride, so that a clamped page number keeps every
+// access inside the pool.
+int check_pool(const hippo_paged_kv_desc* pd) {
+  if (pd == nullptr) return HIPPO_ERR_NULL_ARG;
+  if (pd->dtype != HIPPO_DTYPE_F32 && pd->dtype != HIPPO_DTYPE_BF16) return HIPPO_ERR_BAD_DTYPE;
+  if (pd->n_kv_heads < 1 || pd->n_kv_heads > 65535 || (pd->head_dim != 64 && pd->head_dim != 128)) return HIPPO_ERR_BAD_SHAPE;
+  if (pd->page_size < 16 || pd->page_size > 256 || (pd->page_size & (pd->page_size - 1))) return HIPPO_ERR_BAD_SHAPE;
+  if (pd->n_pool_pages < 1 || pd->n_pool_pages > kPlanMost) return HIPPO_ERR_BAD_SHAPE;
+  if (pd->stride_n < pd->head_dim || pd->stride_n > (1ll << 24) || pd->stride_h < 0) return HIPPO_ERR_BAD_SHAPE;
+  if ((long long)(pd->page_size - 1) * pd->stride_n + (long long)(pd->n_kv_heads - 1) * pd->stride_h + pd->head_dim > pd->stride_page)
+    return HIPPO_ERR_BAD_SHAPE;
+  const int per16 = 16 / elem_bytes(pd->dtype);
+  if (pd->stride_n % per16 || pd->stride_h % per16 || pd->stride_page % per16) return HIPPO_ERR_BAD_ALIGN;
+  return HIPPO_OK;
+}
+
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+void carve_rows(RowsParams* p, const RowsPlan& pl, void* workspace) {
+  p->S = pl.S;
+  p->n_tiles = pl.n_tiles;
+  p->part_o = static_cast<float*>(workspace);
+  p->part_m = reinterpret_cast<float*>(static_cast<char*>(workspace) + pl.off_m);
+  p->part_l = reinterpret_cast<float*>(static_cast<char*>(workspace) + pl.off_l);
+}
+
+float scale_or_default(float softmax_scale, int head_dim) {
+  return (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)head_dim)) * kLog2e;
 }
 
 // ---- log probabilities: planning ------------------------------------------------------------------
@@ -944,6 +1036,189 @@ int hippo_quantize_kv_e4m3(const void* k_src, const void* v_src, const hippo_kv_
                            void* workspace, size_t workspace_bytes, void* stream) {
   return hippo_quantize_kv_e4m3_polls(k_src, v_src, src, n_rows, k_codes, v_codes, dst, k_scale, v_scale, workspace,
                                       workspace_bytes, stream, -1);
+}
+
+size_t hippo_prefill_workspace_bytes(const hippo_packed_desc* desc, int32_t total_q, int32_t total_k, int32_t n_seqs,
+                                     int32_t num_splits) {
+  RowsPlan pl;
+  if (check_packed(desc) != HIPPO_OK || plan_prefill(desc, total_q, total_k, n_seqs, num_splits, &pl) != HIPPO_OK) return 0;
+  return pl.bytes;
+}
+
+// pd null: packed K and V
+static int prefill_entry(const void* q, int32_t total_q, const void* k, const void* v, int32_t total_k, const hippo_packed_desc* desc,
+                         const hippo_paged_kv_desc* pd, const int32_t* block_table, const int32_t* cu_q, const int32_t* cu_k,
+                         int32_t n_seqs, float softmax_scale, int32_t num_splits, void* out, float* lse_out, void* workspace,
+                         size_t workspace_bytes, void* stream) {
+  int rc = check_packed(desc);
+  if (rc != HIPPO_OK) return rc;
+  RowsPlan pl;
+  rc = plan_prefill(desc, total_q, total_k, n_seqs, num_splits, &pl);
+  if (rc != HIPPO_OK) return rc;
+  if (total_q == 0) return HIPPO_OK;                          // no rows
+  if (q == nullptr || cu_q == nullptr || cu_k == nullptr || out == nullptr || workspace == nullptr) return HIPPO_ERR_NULL_ARG;
+  if ((k == nullptr || v == nullptr) && total_k > 0) return HIPPO_ERR_NULL_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || (reinterpret_cast<uintptr_t>(workspace) & 255u) ||
+      !aligned4(cu_q) || !aligned4(cu_k) || !aligned4(lse_out) || !aligned4(block_table))
+    return HIPPO_ERR_BAD_ALIGN;
+  if (workspace_bytes < pl.bytes) return HIPPO_ERR_WORKSPACE_TOO_SMALL;
+  RowsParams p{};
+  p.q = q; p.k = k; p.v = v; p.out = out; p.lse = lse_out;
+  p.q_sn = desc->q_stride_n; p.q_sh = desc->q_stride_h; p.k_sn = desc->kv_stride_n; p.k_sh = desc->kv_stride_h;
+  p.n_seq = n_seqs; p.H = desc->n_q_heads; p.Hkv = desc->n_kv_heads; p.G = p.H / p.Hkv;
+  p.total_q = total_q; p.total_k = total_k; p.cu_q = cu_q;
+  if (pd == nullptr) {
+    p.cu_k = cu_k;
+  } else {
+    p.kv_lens = cu_k;
+    p.block_table = block_table; p.max_pages = pd->max_pages; p.n_pool_pages = pd->n_pool_pages; p.page_stride = pd->stride_page;
+    while ((1 << p.page_shift) < pd->page_size) ++p.page_shift;
+  }
+  p.scale_log2 = scale_or_default(softmax_scale, desc->head_dim);
+  carve_rows(&p, pl, workspace);
+  const hipError_t e = launch_prefill(p, pl.rb, desc->dtype, desc->head_dim, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? HIPPO_OK : HIPPO_ERR_HIP;
+}
+
+int hippo_prefill_attention(const void* q, int32_t total_q, const void* k, const void* v, int32_t total_k,
+                            const hippo_packed_desc* desc, const int32_t* cu_q, const int32_t* cu_k, int32_t n_seqs,
+                            float softmax_scale, int32_t num_splits, void* out, float* lse_out, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+  return prefill_entry(q, total_q, k, v, total_k, desc, nullptr, nullptr, cu_q, cu_k, n_seqs, softmax_scale, num_splits, out, lse_out,
+                       workspace, workspace_bytes, stream);
+}
+
+int hippo_prefill_attention_paged(const void* q, int32_t total_q, int64_t q_stride_n, int64_t q_stride_h, const void* k_pool,
+                                  const void* v_pool, const int32_t* block_table, const hippo_paged_kv_desc* kv, const int32_t* cu_q,
+                                  const int32_t* kv_lens, float softmax_scale, int32_t num_splits, void* out, float* lse_out,
+                                  void* workspace, size_t workspace_bytes, void* stream) {
+  const int rc = check_pool(kv);
+  if (rc != HIPPO_OK) return rc;
+  if (block_table == nullptr || k_pool == nullptr || v_pool == nullptr) return HIPPO_ERR_NULL_ARG;
+  if (kv->max_pages < 1 || (long long)kv->max_pages * kv->page_size > 0x7fffff00ll) return HIPPO_ERR_BAD_SHAPE;
+  const hippo_packed_desc d = {kv->n_q_heads, kv->n_kv_heads, kv->head_dim, kv->dtype, q_stride_n, q_stride_h, kv->stride_n, kv->stride_h};
+  return prefill_entry(q, total_q, k_pool, v_pool, kv->max_pages * kv->page_size, &d, kv, block_table, cu_q, kv_lens, kv->batch,
+                       softmax_scale, num_splits, out, lse_out, workspace, workspace_bytes, stream);
+}
+
+size_t hippo_tree_workspace_bytes(const hippo_kv_desc* kv, int32_t n_nodes, int32_t seq_len, int32_t num_splits) {
+  RowsPlan pl;
+  if (check_kv(kv) != HIPPO_OK || plan_tree(kv, n_nodes, seq_len, num_splits, &pl) != HIPPO_OK) return 0;
+  return pl.bytes;
+}
+
+static int tree_entry(const void* q, int32_t n_nodes, const void* k, const void* v, const hippo_kv_desc* kv,
+                      const hippo_paged_kv_desc* pd, const int32_t* block_table, int32_t seq_len, const int32_t* parents,
+                      int64_t parents_stride_b, const int32_t* ctx_lens, int32_t ctx_len, float softmax_scale, int32_t num_splits,
+                      void* out, float* lse_out, void* workspace, size_t workspace_bytes, void* stream) {
+  if (q == nullptr || k == nullptr || v == nullptr || parents == nullptr || out == nullptr || workspace == nullptr)
+    return HIPPO_ERR_NULL_ARG;
+  int rc = check_kv(kv);
+  if (rc != HIPPO_OK) return rc;
+  RowsPlan pl;
+  rc = plan_tree(kv, n_nodes, seq_len, num_splits, &pl);
+  if (rc != HIPPO_OK) return rc;
+  if (parents_stride_b < 0) return HIPPO_ERR_BAD_SHAPE;
+  if (ctx_lens == nullptr && (ctx_len < 0 || ctx_len > seq_len - n_nodes)) return HIPPO_ERR_BAD_SHAPE;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || (reinterpret_cast<uintptr_t>(workspace) & 255u) ||
+      !aligned4(parents) || !aligned4(ctx_lens) || !aligned4(lse_out) || !aligned4(block_table))
+    return HIPPO_ERR_BAD_ALIGN;
+  if (workspace_bytes < pl.bytes) return HIPPO_ERR_WORKSPACE_TOO_SMALL;
+  RowsParams p{};
+  p.q = q; p.k = k; p.v = v; p.out = out; p.lse = lse_out;
+  p.n_seq = kv->batch; p.H = kv->n_q_heads; p.Hkv = kv->n_kv_heads; p.G = p.H / p.Hkv;
+  p.q_sn = (int64_t)p.H * kv->head_dim; p.q_sh = kv->head_dim;
+  p.k_sb = kv->stride_b; p.k_sn = kv->stride_n; p.k_sh = kv->stride_h;
+  p.total_q = kv->batch * n_nodes; p.total_k = seq_len;
+  p.kv_lens = ctx_lens; p.ctx_len = ctx_len;
+  p.parents = parents; p.parents_sb = parents_stride_b; p.nodes = n_nodes;
+  if (pd != nullptr) {
+    p.block_table = block_table; p.max_pages = pd->max_pages; p.n_pool_pages = pd->n_pool_pages; p.page_stride = pd->stride_page;
+    while ((1 << p.page_shift) < pd->page_size) ++p.page_shift;
+  }
+  p.scale_log2 = scale_or_default(softmax_scale, kv->head_dim);
+  carve_rows(&p, pl, workspace);
+  const hipError_t e = launch_tree(p, pl.rb, kv->dtype, kv->head_dim, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? HIPPO_OK : HIPPO_ERR_HIP;
+}
+
+int hippo_tree_attention(const void* q, int32_t n_nodes, const void* k_cache, const void* v_cache, const hippo_kv_desc* kv,
+                         int32_t seq_len, const int32_t* parents, int64_t parents_stride_b, const int32_t* ctx_lens, int32_t ctx_len,
+                         float softmax_scale, int32_t num_splits, void* out, float* lse_out, void* workspace, size_t workspace_bytes,
+                         void* stream) {
+  return tree_entry(q, n_nodes, k_cache, v_cache, kv, nullptr, nullptr, seq_len, parents, parents_stride_b, ctx_lens, ctx_len,
+                    softmax_scale, num_splits, out, lse_out, workspace, workspace_bytes, stream);
+}
+
+int hippo_tree_attention_paged(const void* q, int32_t n_nodes, const void* k_pool, const void* v_pool, const int32_t* block_table,
+                               const hippo_paged_kv_desc* kv, const int32_t* parents, int64_t parents_stride_b,
+                               const int32_t* ctx_lens, int32_t ctx_len, float softmax_scale, int32_t num_splits, void* out,
+                               float* lse_out, void* workspace, size_t workspace_bytes, void* stream) {
+  const int rc = check_pool(kv);
+  if (rc != HIPPO_OK) return rc;
+  if (block_table == nullptr) return HIPPO_ERR_NULL_ARG;
+  if (kv->max_pages < 1 || (long long)kv->max_pages * kv->page_size > 0x7fffff00ll) return HIPPO_ERR_BAD_SHAPE;
+  const hippo_kv_desc flat = {kv->batch, kv->n_q_heads, kv->n_kv_heads, kv->head_dim, kv->dtype, 0, kv->stride_h, kv->stride_n};
+  return tree_entry(q, n_nodes, k_pool, v_pool, &flat, kv, block_table, kv->max_pages * kv->page_size, parents, parents_stride_b,
+                    ctx_lens, ctx_len, softmax_scale, num_splits, out, lse_out, workspace, workspace_bytes, stream);
+}
+
+int hippo_plan_pages(const int32_t* ctx_lens, const int32_t* new_lens, int32_t batch, int32_t* block_table, int32_t max_pages,
+                     int32_t* free_pages, int32_t n_pool_pages, const int32_t* n_free, int32_t page_size, int32_t max_tokens,
+                     int32_t* slots_out, int32_t* positions_out, int32_t* cu_q_out, int32_t* kv_lens_out, int32_t* n_free_out,
+                     void* stream) {
+  if (ctx_lens == nullptr || new_lens == nullptr || block_table == nullptr || free_pages == nullptr || n_free == nullptr ||
+      cu_q_out == nullptr || kv_lens_out == nullptr || n_free_out == nullptr)
+    return HIPPO_ERR_NULL_ARG;
+  if (max_tokens > 0 && (slots_out == nullptr || positions_out == nullptr)) return HIPPO_ERR_NULL_ARG;
+  if (batch < 1 || batch > kPlanMaxBatch || max_pages < 1 || (long long)batch * max_pages > (1 << 30) || max_pages > kPlanMost ||
+      n_pool_pages < 1 || n_pool_pages > kPlanMost || max_tokens < 0 || max_tokens > kPlanMost)
+    return HIPPO_ERR_BAD_SHAPE;
+  if (page_size < 16 || page_size > 256 || (page_size & (page_size - 1))) return HIPPO_ERR_BAD_SHAPE;
+  const void* all[] = {ctx_lens, new_lens, block_table, free_pages, n_free, slots_out, positions_out, cu_q_out, kv_lens_out, n_free_out};
+  for (const void* x : all)
+    if (!aligned4(x)) return HIPPO_ERR_BAD_ALIGN;
+  // every block reads the lengths and the stack's height while the first one writes the new ones
+  for (const void* in : {(const void*)ctx_lens, (const void*)new_lens, (const void*)n_free})
+    for (const void* o : {(const void*)slots_out, (const void*)positions_out, (const void*)cu_q_out, (const void*)kv_lens_out,
+                          (const void*)n_free_out})
+      if (in == o) return HIPPO_ERR_BAD_SHAPE;
+  PlanParams p;
+  p.ctx_lens = ctx_lens; p.new_lens = new_lens; p.block_table = block_table; p.free_pages = free_pages; p.n_free = n_free;
+  p.n_free_out = n_free_out; p.slots = slots_out; p.positions = positions_out; p.cu_q = cu_q_out; p.kv_lens = kv_lens_out;
+  p.B = batch; p.max_pages = max_pages; p.n_pool = n_pool_pages; p.max_tokens = max_tokens;
+  p.page_shift = 0;
+  while ((1 << p.page_shift) < page_size) ++p.page_shift;
+  const hipError_t e = launch_plan_pages(p, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? HIPPO_OK : HIPPO_ERR_HIP;
+}
+
+int hippo_write_kv_paged(const void* k_new, const void* v_new, int32_t n_rows, int64_t stride_n, int64_t stride_h,
+                         const int32_t* slots, const int32_t* rows, int32_t n_tokens, void* k_pool, void* v_pool,
+                         const hippo_paged_kv_desc* kv, void* stream) {
+  const int rc = check_pool(kv);
+  if (rc != HIPPO_OK) return rc;
+  if (n_tokens < 0 || n_rows < 0 || stride_n < 0 || stride_h < 0) return HIPPO_ERR_BAD_SHAPE;
+  // heads and rows of a page must not meet
+  if (rows_meet({kv->n_pool_pages, kv->stride_page}, {kv->n_kv_heads, kv->stride_h}, {kv->page_size, kv->stride_n}, kv->head_dim))
+    return HIPPO_ERR_BAD_SHAPE;
+  const int es = elem_bytes(kv->dtype);
+  if (stride_n % (16 / es) || stride_h % (16 / es)) return HIPPO_ERR_BAD_ALIGN;
+  const int pieces = kv->head_dim * es / 16;
+  if ((long long)n_tokens * kv->n_kv_heads * pieces > (1ll << 31)) return HIPPO_ERR_BAD_SHAPE;
+  if (n_tokens == 0 || n_rows == 0) return HIPPO_OK;          // nothing to write
+  if (k_new == nullptr || v_new == nullptr || slots == nullptr || k_pool == nullptr || v_pool == nullptr) return HIPPO_ERR_NULL_ARG;
+  if (k_pool == v_pool) return HIPPO_ERR_BAD_SHAPE;
+  if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(k_pool) || !aligned16(v_pool) || !aligned4(slots) || !aligned4(rows))
+    return HIPPO_ERR_BAD_ALIGN;
+  WriteParams p;
+  p.k = k_new; p.v = v_new; p.slots = slots; p.rows = rows; p.k_pool = k_pool; p.v_pool = v_pool;
+  p.n_tokens = n_tokens; p.n_rows = n_rows; p.Hkv = kv->n_kv_heads; p.pieces = pieces; p.page_size = kv->page_size;
+  p.n_slots = (long long)kv->n_pool_pages * kv->page_size;
+  p.sn = stride_n * es; p.sh = stride_h * es;
+  p.page_stride = kv->stride_page * es; p.pool_sn = kv->stride_n * es; p.pool_sh = kv->stride_h * es;
+  const hipError_t e = launch_write_kv(p, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? HIPPO_OK : HIPPO_ERR_HIP;
 }
 
 }  // extern "C"

@@ -12,7 +12,6 @@
 //     launch itself, paged caches, and caches of 8-bit floating-point codes (converted to bf16
 //     after the LDS read).
 //   * attn_partial_f32   -- fp32, MFMA 16x16x4 with fp32 operands.
-#include <atomic>
 #include <type_traits>
 
 #include "common.h"
@@ -1217,23 +1216,6 @@ __global__ __launch_bounds__(256) void attn_combine(ParamsOf<(MASS > 0)> p) {
 // =================================================================================================
 // host launch
 // =================================================================================================
-// Lets KERNEL use `smem` bytes of dynamic LDS.  The attribute belongs to a (kernel, device) pair: it is set once for
-// each device this process uses.
-template <auto KERNEL>
-static hipError_t allow_dynamic_lds(int smem) {
-  static std::atomic<unsigned long long> attr_set{0};
-  int dev = 0;
-  hipError_t e = hipGetDevice(&dev);
-  if (e != hipSuccess) return e;
-  const unsigned long long bit = 1ull << (dev & 63);
-  if (!(attr_set.load(std::memory_order_acquire) & bit)) {
-    e = hipFuncSetAttribute((const void*)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e != hipSuccess) return e;
-    attr_set.fetch_or(bit, std::memory_order_release);
-  }
-  return hipSuccess;
-}
-
 template <int D, int RB, int TG, int TT, int NST, int MODE, bool KV8 = false, bool NT = false, bool ROT = false,
           bool ONE = false, bool MASS = false>
 static hipError_t launch_grid_mode(const ParamsOf<MASS>& p, hipStream_t st) {

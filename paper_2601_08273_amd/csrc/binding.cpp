@@ -38,7 +38,10 @@ namespace {
   X(hippo_quantize_kv_e4m3) X(hippo_spec_verify_workspace_bytes) X(hippo_spec_verify)                                   \
   X(hippo_token_logprobs_workspace_bytes) X(hippo_token_logprobs) X(hippo_evict_kv_workspace_bytes) X(hippo_evict_kv)   \
   X(hippo_attention_mass_workspace_bytes)                                                                               \
-  X(hippo_verify_attention_mass) X(hippo_draft_attention_mass)
+  X(hippo_verify_attention_mass) X(hippo_draft_attention_mass)                                                          \
+  X(hippo_prefill_workspace_bytes) X(hippo_prefill_attention) X(hippo_prefill_attention_paged)                          \
+  X(hippo_tree_workspace_bytes) X(hippo_tree_attention) X(hippo_tree_attention_paged)                                   \
+  X(hippo_plan_pages) X(hippo_write_kv_paged)
 struct Library {
 #define X(name) decltype(&::name) name;
   HIPPO_LIBRARY(X)
@@ -607,6 +610,209 @@ PyObject* token_logprobs(PyObject* const* a) {
   return n_top > 0 ? tuple({wrap(logprob), wrap(entropy), wrap(ids), wrap(top)}) : tuple({wrap(logprob), wrap(entropy)});
 }
 
+// ---- prompts, trees, pages ------------------------------------------------------------------------------------
+// int32 on the device, contiguous, of this shape
+void require_int32(const Tensor& t, at::IntArrayRef sizes) {
+  REQUIRE(t.scalar_type() == at::kInt && t.sizes() == sizes && t.is_contiguous());
+}
+// pools [n_pages, page_size, H_kv, d], any strides with unit stride on d
+hippo_paged_kv_desc describe_pool(const Tensor& k, const Tensor& v, long long batch, long long n_q_heads, long long max_pages) {
+  REQUIRE(k.dim() == 4 && k.stride(3) == 1 && same_layout(v, k) && v.scalar_type() == k.scalar_type());
+  hippo_paged_kv_desc pd;
+  pd.batch = (int32_t)batch;
+  pd.n_q_heads = (int32_t)n_q_heads;
+  pd.n_kv_heads = (int32_t)k.size(2);
+  pd.head_dim = (int32_t)k.size(3);
+  pd.dtype = dtype_code(k);
+  pd.page_size = (int32_t)k.size(1);
+  pd.max_pages = (int32_t)max_pages;
+  pd.n_pool_pages = (int32_t)k.size(0);
+  pd.stride_page = k.stride(0);
+  pd.stride_n = k.stride(1);
+  pd.stride_h = k.size(2) == 1 ? 0 : k.stride(2);             // (the stride of a single head is nobody's)
+  REQUIRE(k.size(0) <= 0x7fffffff && k.size(1) <= 0x7fffffff && max_pages <= 0x7fffffff);
+  return pd;
+}
+void require_packed(const Tensor& t) {
+  REQUIRE(t.dim() == 3 && (t.stride(2) == 1 || t.numel() == 0) && t.size(0) <= 0x7fffffff);
+}
+
+// q, k, v, cu_q, cu_k, softmax_scale, num_splits, want_lse, out, workspace
+PyObject* prefill(PyObject* const* a) {
+  const Tensor &q = tensor(a[0]), &k = tensor(a[1]), &v = tensor(a[2]), &cu_q = tensor(a[3]);
+  const Tensor cu_k = a[4] == Py_None ? cu_q : tensor(a[4]);
+  const float scale = scale_or_none(a[5]);
+  const long long splits = integer(a[6]);
+  for (const Tensor* t : {&q, &k, &v}) require_packed(*t);
+  REQUIRE(same_layout(v, k) && v.scalar_type() == k.scalar_type() && q.scalar_type() == k.scalar_type() && q.size(2) == k.size(2));
+  REQUIRE(cu_q.dim() == 1 && cu_q.size(0) >= 2 && splits >= 0 && splits <= 0x7fffffff);
+  for (const Tensor* t : {&cu_q, &cu_k}) require_int32(*t, cu_q.sizes());
+  REQUIRE(a[4] != Py_None || q.size(0) == k.size(0));          // whole prompts
+  hippo_packed_desc d;
+  d.n_q_heads = (int32_t)q.size(1);
+  d.n_kv_heads = (int32_t)k.size(1);
+  d.head_dim = (int32_t)q.size(2);
+  d.dtype = dtype_code(q);
+  d.q_stride_n = q.size(0) <= 1 ? 0 : q.stride(0);            // (the stride of a single element is nobody's)
+  d.q_stride_h = q.size(1) <= 1 ? 0 : q.stride(1);
+  d.kv_stride_n = k.size(0) <= 1 ? 0 : k.stride(0);
+  d.kv_stride_h = k.size(1) <= 1 ? 0 : k.stride(1);
+  const int32_t n_q = (int32_t)q.size(0), n_k = (int32_t)k.size(0), n_seqs = (int32_t)cu_q.size(0) - 1;
+  const Tensor out = output(a[8], q.sizes(), q.scalar_type(), q);
+  Tensor lse;
+  if (truth(a[7])) lse = empty({q.size(1), q.size(0)}, at::kFloat, q);
+  const Tensor ws = workspace(a[9], q, [&] { return lib.hippo_prefill_workspace_bytes(&d, n_q, n_k, n_seqs, (int32_t)splits); });
+  require_here({&q, &k, &v, &cu_q, &cu_k, &out, &lse, &ws});
+  check(unlocked(lib.hippo_prefill_attention, ptr<const void>(q), n_q, ptr<const void>(k), ptr<const void>(v), n_k, &d,
+                 ptr<const int32_t>(cu_q), ptr<const int32_t>(cu_k), n_seqs, scale, (int32_t)splits, ptr(out), ptr<float>(lse), ptr(ws),
+                 (size_t)ws.nbytes(), stream()),
+        "hippo_prefill_attention");
+  return lse.defined() ? tuple({wrap(out), wrap(lse)}) : wrap(out);
+}
+
+// q, k_pool, v_pool, block_table, cu_q, kv_lens, softmax_scale, num_splits, want_lse, out, workspace
+PyObject* prefill_paged(PyObject* const* a) {
+  const Tensor &q = tensor(a[0]), &k = tensor(a[1]), &v = tensor(a[2]), &table = tensor(a[3]), &cu_q = tensor(a[4]), &lens = tensor(a[5]);
+  const float scale = scale_or_none(a[6]);
+  const long long splits = integer(a[7]);
+  require_packed(q);
+  REQUIRE(table.dim() == 2 && table.size(0) >= 1 && splits >= 0 && splits <= 0x7fffffff);
+  const long long B = table.size(0);
+  require_int32(table, {B, table.size(1)});
+  require_int32(cu_q, {B + 1});
+  require_int32(lens, {B});
+  const hippo_paged_kv_desc pd = describe_pool(k, v, B, q.size(1), table.size(1));
+  REQUIRE(q.scalar_type() == k.scalar_type() && q.size(2) == k.size(3));
+  const int32_t n_q = (int32_t)q.size(0);
+  const int64_t sn = q.size(0) <= 1 ? 0 : q.stride(0), sh = q.size(1) <= 1 ? 0 : q.stride(1);
+  const hippo_packed_desc d = {pd.n_q_heads, pd.n_kv_heads, pd.head_dim, pd.dtype, sn, sh, pd.stride_n, pd.stride_h};
+  const Tensor out = output(a[9], q.sizes(), q.scalar_type(), q);
+  Tensor lse;
+  if (truth(a[8])) lse = empty({q.size(1), q.size(0)}, at::kFloat, q);
+  const long long room = std::min<long long>(table.size(1) * k.size(1), 0x7fffffff);
+  const Tensor ws = workspace(a[10], q, [&] { return lib.hippo_prefill_workspace_bytes(&d, n_q, (int32_t)room, (int32_t)B, (int32_t)splits); });
+  require_here({&q, &k, &v, &table, &cu_q, &lens, &out, &lse, &ws});
+  check(unlocked(lib.hippo_prefill_attention_paged, ptr<const void>(q), n_q, sn, sh, ptr<const void>(k), ptr<const void>(v),
+                 ptr<const int32_t>(table), &pd, ptr<const int32_t>(cu_q), ptr<const int32_t>(lens), scale, (int32_t)splits, ptr(out),
+                 ptr<float>(lse), ptr(ws), (size_t)ws.nbytes(), stream()),
+        "hippo_prefill_attention_paged");
+  return lse.defined() ? tuple({wrap(out), wrap(lse)}) : wrap(out);
+}
+
+// what the tree calls have in common: the tree, the sequences' lengths
+struct TreeCall {
+  const Tensor &q, &parents;
+  Tensor ctx_lens, out, lse, ws;
+  long long ctx_len = 0, splits;
+  float scale;
+  int64_t parents_stride = 0;
+  TreeCall(PyObject* q_o, PyObject* parents_o, PyObject* ctx, PyObject* scale_o, PyObject* splits_o)
+      : q(tensor(q_o)), parents(tensor(parents_o)), splits(integer(splits_o)), scale(scale_or_none(scale_o)) {
+    REQUIRE(q.dim() == 4 && q.is_contiguous() && splits >= 0 && splits <= 0x7fffffff);
+    REQUIRE(q.size(0) <= 0x7fffffff && q.size(1) <= 0x7fffffff && q.size(2) <= 0x7fffffff);
+    // [B, n_nodes], or [n_nodes]: one tree for all
+    REQUIRE(parents.scalar_type() == at::kInt && (parents.dim() == 1 || parents.dim() == 2) && parents.size(-1) == q.size(1));
+    REQUIRE(parents.size(-1) == 1 || parents.stride(-1) == 1);
+    if (parents.dim() == 2) {
+      REQUIRE(parents.size(0) == q.size(0));
+      parents_stride = q.size(0) == 1 ? 0 : parents.stride(0);
+    }
+    if (THPVariable_Check(ctx)) {
+      ctx_lens = tensor(ctx);
+      require_int32(ctx_lens, {q.size(0)});
+    } else {
+      ctx_len = integer(ctx);
+      REQUIRE(ctx_len >= 0 && ctx_len <= 0x7fffffff);
+    }
+  }
+  void buffers(const hippo_kv_desc& kv, int32_t rows, PyObject* want_lse, PyObject* out_o, PyObject* ws_o) {
+    out = output(out_o, q.sizes(), q.scalar_type(), q);
+    if (truth(want_lse)) lse = empty({q.size(0), q.size(2), q.size(1)}, at::kFloat, q);
+    ws = workspace(ws_o, q, [&] { return lib.hippo_tree_workspace_bytes(&kv, (int32_t)q.size(1), rows, (int32_t)splits); });
+  }
+  PyObject* result() const { return lse.defined() ? tuple({wrap(out), wrap(lse)}) : wrap(out); }
+};
+
+// q, k_cache, v_cache, parents, ctx_lens, softmax_scale, num_splits, want_lse, out, workspace
+PyObject* tree(PyObject* const* a) {
+  TreeCall c(a[0], a[3], a[4], a[5], a[6]);
+  const Tensor &k = tensor(a[1]), &v = tensor(a[2]);
+  const hippo_kv_desc kv = describe(k, c.q.size(2));
+  REQUIRE(same_layout(v, k) && v.scalar_type() == k.scalar_type() && c.q.scalar_type() == k.scalar_type());
+  REQUIRE(c.q.size(0) == k.size(0) && c.q.size(3) == k.size(3) && k.size(2) <= 0x7fffffff);
+  const int32_t rows = (int32_t)k.size(2);
+  c.buffers(kv, rows, a[7], a[8], a[9]);
+  require_here({&c.q, &k, &v, &c.parents, &c.ctx_lens, &c.out, &c.lse, &c.ws});
+  check(unlocked(lib.hippo_tree_attention, ptr<const void>(c.q), (int32_t)c.q.size(1), ptr<const void>(k), ptr<const void>(v), &kv, rows,
+                 ptr<const int32_t>(c.parents), c.parents_stride, ptr<const int32_t>(c.ctx_lens), (int32_t)c.ctx_len, c.scale,
+                 (int32_t)c.splits, ptr(c.out), ptr<float>(c.lse), ptr(c.ws), (size_t)c.ws.nbytes(), stream()),
+        "hippo_tree_attention");
+  return c.result();
+}
+
+// q, k_pool, v_pool, block_table, parents, ctx_lens, softmax_scale, num_splits, want_lse, out, workspace
+PyObject* tree_paged(PyObject* const* a) {
+  TreeCall c(a[0], a[4], a[5], a[6], a[7]);
+  const Tensor &k = tensor(a[1]), &v = tensor(a[2]), &table = tensor(a[3]);
+  REQUIRE(table.dim() == 2);
+  require_int32(table, {c.q.size(0), table.size(1)});
+  const hippo_paged_kv_desc pd = describe_pool(k, v, c.q.size(0), c.q.size(2), table.size(1));
+  REQUIRE(c.q.scalar_type() == k.scalar_type() && c.q.size(3) == k.size(3));
+  const hippo_kv_desc flat = {pd.batch, pd.n_q_heads, pd.n_kv_heads, pd.head_dim, pd.dtype, 0, pd.stride_h, pd.stride_n};
+  c.buffers(flat, (int32_t)std::min<long long>(table.size(1) * k.size(1), 0x7fffffff), a[8], a[9], a[10]);
+  require_here({&c.q, &k, &v, &table, &c.parents, &c.ctx_lens, &c.out, &c.lse, &c.ws});
+  check(unlocked(lib.hippo_tree_attention_paged, ptr<const void>(c.q), (int32_t)c.q.size(1), ptr<const void>(k), ptr<const void>(v),
+                 ptr<const int32_t>(table), &pd, ptr<const int32_t>(c.parents), c.parents_stride, ptr<const int32_t>(c.ctx_lens),
+                 (int32_t)c.ctx_len, c.scale, (int32_t)c.splits, ptr(c.out), ptr<float>(c.lse), ptr(c.ws), (size_t)c.ws.nbytes(),
+                 stream()),
+        "hippo_tree_attention_paged");
+  return c.result();
+}
+
+// ctx_lens, new_lens, block_table, free_pages, n_free, page_size, max_tokens, slots_out, positions_out, cu_q_out, kv_lens_out, n_free_out
+PyObject* plan_pages(PyObject* const* a) {
+  const Tensor &ctx = tensor(a[0]), &add = tensor(a[1]), &table = tensor(a[2]), &free_pages = tensor(a[3]), &n_free = tensor(a[4]);
+  const long long page = integer(a[5]), most = integer(a[6]);
+  REQUIRE(ctx.dim() == 1 && table.dim() == 2 && free_pages.dim() == 1);
+  const long long B = ctx.size(0);
+  REQUIRE(page >= 0 && page <= 0x7fffffff && most >= 0 && most <= 0x7fffffff && B <= 0x7fffffff);
+  REQUIRE(table.size(1) <= 0x7fffffff && free_pages.size(0) <= 0x7fffffff);
+  require_int32(ctx, {B});
+  require_int32(add, {B});
+  require_int32(table, {B, table.size(1)});
+  require_int32(free_pages, {free_pages.size(0)});
+  require_int32(n_free, {1});
+  const Tensor slots = output(a[7], {most}, at::kInt, ctx), positions = output(a[8], {most}, at::kInt, ctx);
+  const Tensor cu_q = output(a[9], {B + 1}, at::kInt, ctx), kv_lens = output(a[10], {B}, at::kInt, ctx);
+  const Tensor left = output(a[11], {1}, at::kInt, ctx);
+  require_here({&ctx, &add, &table, &free_pages, &n_free, &slots, &positions, &cu_q, &kv_lens, &left});
+  check(unlocked(lib.hippo_plan_pages, ptr<const int32_t>(ctx), ptr<const int32_t>(add), (int32_t)B, ptr<int32_t>(table),
+                 (int32_t)table.size(1), ptr<int32_t>(free_pages), (int32_t)free_pages.size(0), ptr<const int32_t>(n_free),
+                 (int32_t)page, (int32_t)most, ptr<int32_t>(slots), ptr<int32_t>(positions), ptr<int32_t>(cu_q), ptr<int32_t>(kv_lens),
+                 ptr<int32_t>(left), stream()),
+        "hippo_plan_pages");
+  return tuple({wrap(slots), wrap(positions), wrap(cu_q), wrap(kv_lens), wrap(left)});
+}
+
+// k_new, v_new, slots, k_pool, v_pool, rows
+PyObject* write_pages(PyObject* const* a) {
+  const Tensor &k = tensor(a[0]), &v = tensor(a[1]), &slots = tensor(a[2]), &k_pool = tensor(a[3]), &v_pool = tensor(a[4]);
+  const Tensor rows = tensor_or_none(a[5]);
+  for (const Tensor* t : {&k, &v}) require_packed(*t);
+  REQUIRE(same_layout(v, k) && v.scalar_type() == k.scalar_type());
+  REQUIRE(slots.dim() == 1 && slots.size(0) <= 0x7fffffff);
+  require_int32(slots, {slots.size(0)});
+  if (rows.defined()) require_int32(rows, slots.sizes());
+  const hippo_paged_kv_desc pd = describe_pool(k_pool, v_pool, 1, 1, 1);
+  REQUIRE(k_pool.scalar_type() == k.scalar_type() && k.size(1) == k_pool.size(2) && k.size(2) == k_pool.size(3));
+  require_here({&k, &v, &slots, &rows, &k_pool, &v_pool});
+  check(unlocked(lib.hippo_write_kv_paged, ptr<const void>(k), ptr<const void>(v), (int32_t)k.size(0),
+                 (int64_t)(k.size(0) <= 1 ? 0 : k.stride(0)), (int64_t)(k.size(1) <= 1 ? 0 : k.stride(1)), ptr<const int32_t>(slots),
+                 ptr<const int32_t>(rows), (int32_t)slots.size(0), ptr(k_pool), ptr(v_pool), &pd, stream()),
+        "hippo_write_kv_paged");
+  return none();
+}
+
 // bind(path of libhippo.so, VideoDesc, HippoError)
 PyObject* bind(PyObject* const* a) {
   const char* path = PyUnicode_AsUTF8(a[0]);
@@ -652,7 +858,8 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 PyMethodDef methods[] = {
     ENTRY(bind, 3), ENTRY(score_tokens, 9), ENTRY(score_tokens_layers, 10), ENTRY(select_gather, 11), ENTRY(attention, 12),
     ENTRY(attention_fp8kv, 12), ENTRY(attention_paged, 11), ENTRY(quantize, 6), ENTRY(spec_verify, 10),
-    ENTRY(token_logprobs, 9), ENTRY(evict, 12), ENTRY(attention_mass, 14), {nullptr, nullptr, 0, nullptr}};
+    ENTRY(token_logprobs, 9), ENTRY(evict, 12), ENTRY(attention_mass, 14), ENTRY(prefill, 10), ENTRY(prefill_paged, 11),
+    ENTRY(tree, 10), ENTRY(tree_paged, 11), ENTRY(plan_pages, 12), ENTRY(write_pages, 6), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

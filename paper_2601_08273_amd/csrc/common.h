@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "hippo.h"
 
 namespace hippo {
@@ -243,6 +245,23 @@ struct WaitLadder<0> {
 // ---- host side ---------------------------------------------------------------------------------
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
+// Lets KERNEL use `smem` bytes of dynamic LDS.  The attribute belongs to a (kernel, device) pair: it is set once for
+// each device this process uses.
+template <auto KERNEL>
+static hipError_t allow_dynamic_lds(int smem) {
+  static std::atomic<unsigned long long> attr_set{0};
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const unsigned long long bit = 1ull << (dev & 63);
+  if (!(attr_set.load(std::memory_order_acquire) & bit)) {
+    e = hipFuncSetAttribute((const void*)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != hipSuccess) return e;
+    attr_set.fetch_or(bit, std::memory_order_release);
+  }
+  return hipSuccess;
+}
+
 // One attention call, as the kernels see it.
 struct AttnParams {
   const void* q;
@@ -408,6 +427,38 @@ struct QuantParams {
 };
 int quant_slices(int n_rows, int head_dim);
 hipError_t launch_quantize(const QuantParams& p, hipStream_t st);
+
+// ---- pages of a paged cache ---------------------------------------------------------------------
+constexpr int kPlanMaxBatch = 4096;   // requests of a step
+constexpr int kPlanMost = 1 << 22;    // tokens of a step, pages of a pool, columns of a table: their sums over 64 requests fit 32 bits
+
+struct PlanParams {
+  const int32_t* ctx_lens;   // [B]
+  const int32_t* new_lens;   // [B]; negative: rows given back
+  int32_t* block_table;      // [B, max_pages]
+  int32_t* free_pages;       // [n_pool], a stack
+  const int32_t* n_free;     // [1]
+  int32_t* n_free_out;
+  int32_t* slots;            // [max_tokens]
+  int32_t* positions;        // [max_tokens]
+  int32_t* cu_q;             // [B + 1]
+  int32_t* kv_lens;          // [B]
+  int B, max_pages, n_pool, page_shift, max_tokens;
+};
+hipError_t launch_plan_pages(const PlanParams& p, hipStream_t st);
+
+struct WriteParams {
+  const void* k;
+  const void* v;
+  const int32_t* slots;      // [n_tokens]
+  const int32_t* rows;       // [n_tokens] or null: token t's row is t
+  void* k_pool;
+  void* v_pool;
+  int n_tokens, n_rows, Hkv, pieces, page_size;   // pieces: 16 bytes each, of one head's row
+  long long n_slots;
+  long long sn, sh, page_stride, pool_sn, pool_sh;   // bytes
+};
+hipError_t launch_write_kv(const WriteParams& p, hipStream_t st);
 
 // ---- speculative-sampling verification ---------------------------------------------------------
 constexpr int kSdSeg = 8192;        // vocabulary entries handled by one block

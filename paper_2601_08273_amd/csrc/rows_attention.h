@@ -1,0 +1,638 @@
+// Attention of many query rows: the prompt calls (prefill.hip) and the draft-tree calls (tree.hip).
+//
+// The calls of attention.hip have a few query rows a KV head and are bound by the cache's bytes.  Here a KV head has tens to
+// thousands of them (row r = i * G + g: row i of the sequence, query head g of the group, so that the heads of a group share every
+// K and V row that reaches the LDS), and what counts is how much of a K or V row's trip from the LDS to the matrix unit is used: a wave
+// owns 32 query rows (v_mfma_f32_32x32x16_bf16, in fp32 32x32x2), half the LDS bytes per product of 16-row tiles.
+//
+//   S^T = K Q^T      A = 32 tokens of K, B = 32 query rows: lane (j = lane % 32, h = lane / 32) gets query row j's logits of tokens
+//                    8 (e / 4) + 4 h + e % 4 of the block, e = 0..15
+//   O^T = V^T P^T    B = those same registers (the order of the tokens in a contraction is free), A = V^T by transposing LDS reads
+//   softmax          one pass, with a running maximum and sum per row; a row's tokens lie in lanes j and j + 32, so one exchange of the
+//                    wave's halves completes a maximum
+//
+// A block has RB x TG waves: wave (rb, tg) owns rows 32 rb .. 32 rb + 31 of the block's tile and of every stage tokens
+// tg TW .. tg TW + TW - 1; the TG states of a row block meet in the LDS at the end.  K and V reach the LDS without registers in between,
+// NST stages deep.  A sequence's stages may be dealt to S blocks (few rows over many tokens): their states go to a merge.
+#pragma once
+
+#include <type_traits>
+
+#include "common.h"
+
+namespace hippo {
+
+struct RowsParams {
+  const void* q;
+  const void* k;
+  const void* v;
+  void* out;                    // [tokens, H, D]
+  float* lse;                   // may be null: [H, total_q] of prompts, [B, H, nodes] of trees
+  long long q_sn, q_sh;         // element strides of q's tokens and heads
+  long long k_sb, k_sn, k_sh;   // of K and V: batch elements (contiguous caches), rows, KV heads
+  int n_seq, H, Hkv, G;
+  int total_q, total_k;         // rows of q; rows of packed K and V, or the most that a sequence's part of the cache holds
+  const int32_t* cu_q;          // prompts: [n_seq + 1]
+  const int32_t* cu_k;          // packed prompts: [n_seq + 1]
+  const int32_t* kv_lens;       // paged prompts: rows of each sequence; trees: rows before the tree, null: ctx_len
+  int ctx_len;
+  const int32_t* parents;       // trees: [B, nodes]
+  long long parents_sb;
+  int nodes;
+  const int32_t* block_table;   // [n_seq, max_pages]
+  int page_shift, max_pages, n_pool_pages;
+  long long page_stride;
+  float scale_log2;
+  int S;                        // blocks that share a tile's stages
+  int n_tiles;                  // row tiles of the launch
+  float* part_o;                // [S, tokens * H, D] outputs before the division
+  float* part_m;                // [S, tokens * H] maxima (log2), -inf: nothing seen
+  float* part_l;
+};
+
+// how a call is cut: rows of a block (RB x 32), blocks that share a tile
+struct RowsPlan {
+  int rb, S, n_tiles;
+  size_t off_m, off_l, bytes;
+};
+
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) short rows_s16x4;
+typedef __attribute__((ext_vector_type(2))) __bf16 rows_bf16x2;
+typedef __attribute__((ext_vector_type(2))) float rows_f32x2;
+
+// LDS geometry of a K or V tile: rows as in memory, the 16-byte pieces of a row exchanged so that neither the K reads (16 lanes, 16
+// consecutive rows, the same piece) nor the V reads (bf16: 32 lanes, four rows, four neighbouring pieces; fp32: 64 lanes, two rows four
+// apart, eight pieces each) meet in a bank: of 256 bytes, the K reads' rows differ in all four bits, the V reads' in those above.
+template <typename T, int D>
+struct RowsTile {
+  static constexpr int kRowBytes = D * (int)sizeof(T);
+  static constexpr int kPieces = kRowBytes / 16;
+  static constexpr int kRowsPerXfer = 1024 / kRowBytes;
+  static __device__ __forceinline__ int swizzle(int r) {
+    if constexpr (sizeof(T) == 4) return (((r >> 2) & 1) << 3) | (((r >> 3) & 1) << 2) | (r & 3);
+    else if constexpr (D == 128) return ((r & 3) << 2) | ((r >> 2) & 3);
+    else return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+  }
+};
+
+template <typename T, int D, int RB, int TG, int TW, int NST>
+struct RowsSmem {
+  static constexpr int kTileBytes = TG * TW * RowsTile<T, D>::kRowBytes;   // of a stage's K (or V)
+  static constexpr int kStage = 2 * kTileBytes;
+  static constexpr int kMerge = (TG - 1) * RB * (D / 2) * 256;             // accumulators of the waves that are not the first group's
+  static constexpr int kRing = NST * kStage > kMerge ? NST * kStage : kMerge;
+  static constexpr int total() { return kRing + 2 * TG * RB * 32 * 4; }
+};
+
+// The block's (sequence, row tile).  Prompts: tiles in descending order of the tokens that they see, so that the longest start first:
+// tile k of a sequence has the level (rows before it) / (rows of a tile) + k, and block t takes the t-th tile from the highest level
+// down.  (A lane looks after a sequence; the level is found by bisection.  More than 64 sequences go in their own order, each
+// from its last tile.)  False: no such tile.
+template <int ROWS>
+__device__ __forceinline__ bool rows_find_tile(const RowsParams& p, int t, int* seq, int* tile) {
+  const int lane = threadIdx.x & 63;
+  auto tiles_of = [&](int b, int* base) {
+    if (b >= p.n_seq) { *base = 0; return 0; }
+    const int lo = min(max(p.cu_q[b], 0), p.total_q), hi = min(max(p.cu_q[b + 1], lo), p.total_q);
+    int len_k;
+    if (p.block_table != nullptr) len_k = min(max(p.kv_lens[b], 0), p.total_k);
+    else {
+      const int ko = min(max(p.cu_k[b], 0), p.total_k);
+      len_k = min(max(p.cu_k[b + 1], ko), p.total_k) - ko;
+    }
+    *base = (int)min((long long)max(len_k - (hi - lo), 0) * p.G / ROWS, (long long)(1 << 29));
+    return (int)(((long long)(hi - lo) * p.G + ROWS - 1) / ROWS);
+  };
+  auto add = [](int a, int b) { return a + b; };
+  if (p.n_seq == 1) {
+    int base;
+    const int n = tiles_of(0, &base);
+    *seq = 0;
+    *tile = n - 1 - t;
+    return t < n;
+  }
+  if (p.n_seq <= 64) {
+    int base;
+    const int n = tiles_of(lane, &base);
+    if (t >= wave_reduce_i32(n, add)) return false;
+    // the largest level that more than t tiles reach
+    int lo = 0, hi = wave_reduce_i32(base + n, [](int a, int b) { return max(a, b); });
+    while (hi - lo > 1) {
+      const int mid = lo + (hi - lo) / 2;
+      if (wave_reduce_i32(min(max(base + n - mid, 0), n), add) > t) lo = mid;
+      else hi = mid;
+    }
+    const int above = wave_reduce_i32(min(max(base + n - lo - 1, 0), n), add);
+    unsigned long long here = __ballot(base <= lo && lo < base + n);
+    for (int i = t - above; i > 0; --i) here &= here - 1;
+    const int b = __ffsll((long long)here) - 1;
+    *seq = b;
+    *tile = lo - __builtin_amdgcn_readlane(base, b);
+    return true;
+  }
+  int before = 0;
+  for (int b0 = 0; b0 < p.n_seq; b0 += 64) {
+    int base;
+    const int n = tiles_of(b0 + lane, &base);
+    const int incl = (int)wave_scan_incl((unsigned)n) + before;
+    const unsigned long long past = __ballot(incl > t);
+    if (past != 0) {
+      const int l = __ffsll((long long)past) - 1;
+      *seq = b0 + l;
+      *tile = __builtin_amdgcn_readlane(incl, l) - 1 - t;     // the last one first
+      return true;
+    }
+    before = __builtin_amdgcn_readlane(incl, 63);
+  }
+  return false;
+}
+
+// Which nodes a node sees: lane i gets node i's, itself among them; 0: the node is none (its parent is below -1 or not before it, or
+// an ancestor is none).  After round r the bits of 2^r ancestors are there.
+__device__ __forceinline__ unsigned long long tree_masks(const int32_t* parents, int nodes) {
+  const int lane = threadIdx.x & 63;
+  int up = lane < nodes ? parents[lane] : -2;
+  int none = up < -1 || up >= lane;
+  unsigned lo = none ? 0u : lane < 32 ? 1u << lane : 0u, hi = none ? 0u : lane >= 32 ? 1u << (lane - 32) : 0u;
+  if (none) up = -1;
+#pragma unroll
+  for (int r = 0; r < 6; ++r) {
+    const int from = up < 0 ? lane : up;
+    const unsigned alo = __shfl(lo, from), ahi = __shfl(hi, from);
+    const int anone = __shfl(none, from), aup = __shfl(up, from);
+    lo |= alo; hi |= ahi; none |= anone;
+    up = up < 0 ? -1 : aup;
+  }
+  return none ? 0ull : (unsigned long long)hi << 32 | lo;
+}
+
+template <typename T, int D, int RB, int TG, int TW, int NST, bool PAGED, bool TREE>
+__global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
+  using Tile = RowsTile<T, D>;
+  using SM = RowsSmem<T, D, RB, TG, TW, NST>;
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int ES = sizeof(T), ROWB = Tile::kRowBytes, RPT = Tile::kRowsPerXfer, CPR = Tile::kPieces;
+  constexpr int WAVES = RB * TG, ROWS = RB * 32, ST = TG * TW, TB = TW / 32, DB = D / 32;
+  constexpr int NLD = ST / RPT, PER = 2 * NLD / WAVES;      // transfers of a stage's K (or V); of a wave a stage
+  constexpr int QN = CPR / 2;                               // 16-byte pieces of a query row in a lane
+  static_assert(2 * NLD % WAVES == 0 && PER * (NST - 1) <= 63 && NST >= 2, "transfer split");
+
+  extern __shared__ __align__(16) unsigned char smem[];
+  unsigned char* ring = smem;
+  float* stat_m = (float*)(smem + SM::kRing);               // [TG][ROWS]
+  float* stat_l = stat_m + TG * ROWS;
+  const unsigned ring_addr = (unsigned)(uintptr_t)ring;
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rb = wave % RB, tg = wave / RB;
+  const int j = lane & 31, h = lane >> 5;
+  const int hk = blockIdx.x % p.Hkv, split = blockIdx.y;
+
+  // ---- the block's rows and the tokens that they may see ----
+  int seq, tile, len_q, len_k, tok0;
+  long long row0_k = 0;
+  if constexpr (TREE) {
+    const int per_seq = p.n_tiles / p.n_seq;
+    seq = blockIdx.x / p.Hkv / per_seq;
+    tile = blockIdx.x / p.Hkv % per_seq;
+    len_q = p.nodes;
+    tok0 = seq * p.nodes;
+    const int ctx = p.kv_lens != nullptr ? p.kv_lens[seq] : p.ctx_len;
+    len_k = min(max(ctx, 0), p.total_k - p.nodes) + p.nodes;
+  } else {
+    if (!rows_find_tile<ROWS>(p, blockIdx.x / p.Hkv, &seq, &tile)) return;
+    seq = __builtin_amdgcn_readfirstlane(seq);
+    tile = __builtin_amdgcn_readfirstlane(tile);
+    tok0 = min(max(p.cu_q[seq], 0), p.total_q);
+    len_q = min(max(p.cu_q[seq + 1], tok0), p.total_q) - tok0;
+    if constexpr (PAGED) len_k = min(max(p.kv_lens[seq], 0), p.total_k);
+    else {
+      const int lo = min(max(p.cu_k[seq], 0), p.total_k);
+      len_k = min(max(p.cu_k[seq + 1], lo), p.total_k) - lo;
+      row0_k = lo;
+    }
+  }
+  const int off = len_k - len_q;                            // trees: the context's length
+  const int R = len_q * p.G;
+  const int last = (min(tile * ROWS + ROWS, R) - 1) / p.G;  // of the tile's rows
+  const int ext = TREE ? len_k : min(max(off + last + 1, 0), len_k);
+  const int all_stages = (ext + ST - 1) / ST;
+  const int s_lo = (int)((long long)all_stages * split / p.S), s_hi = (int)((long long)all_stages * (split + 1) / p.S);
+  const int n_stage = s_hi - s_lo;
+
+  // ---- transfers ----
+  const char* kbase = (const char*)p.k + ((PAGED ? 0ll : TREE ? (long long)seq * p.k_sb : row0_k * p.k_sn) + (long long)hk * p.k_sh) * ES;
+  const char* vbase = (const char*)p.v + ((PAGED ? 0ll : TREE ? (long long)seq * p.k_sb : row0_k * p.k_sn) + (long long)hk * p.k_sh) * ES;
+  const int ld_row = lane / CPR, ld_pc = lane % CPR;
+  const int cap = ext - 1;
+  const int page_mask = PAGED ? (1 << p.page_shift) - 1 : 0;
+  const int32_t* table = PAGED ? p.block_table + (long long)seq * p.max_pages : nullptr;
+  auto issue = [&](int si) {
+    const unsigned dst = ring_addr + (si % NST) * SM::kStage;
+    const int n0 = (s_lo + si) * ST;
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      const int x = wave * PER + u, which = x / NLD, n = x % NLD;
+      const int r = n * RPT + ld_row;
+      const int row = min(n0 + r, cap);                     // rows behind the last one repeat it
+      long long at;
+      if constexpr (PAGED) {
+        // a transfer's rows share a page: it starts at a multiple of its rows, which divide a page's
+        int pg = table[min(n0 + n * RPT, cap) >> p.page_shift];
+        pg = min(max(pg, 0), p.n_pool_pages - 1);
+        at = (long long)pg * p.page_stride + (long long)(row & page_mask) * p.k_sn;
+      } else {
+        at = (long long)row * p.k_sn;
+      }
+      dma16((which ? vbase : kbase) + at * ES + ((ld_pc ^ Tile::swizzle(r)) * 16), dst + which * SM::kTileBytes + n * 1024);
+    }
+  };
+  int issued = min(n_stage, NST - 1);
+  for (int si = 0; si < issued; ++si) issue(si);
+
+  // ---- the wave's query rows ----
+  const int row = tile * ROWS + rb * 32 + j;
+  const int qi = min(row, R - 1) / p.G, head = hk * p.G + min(row, R - 1) - qi * p.G;
+  using QPiece = typename std::conditional<F32, f32x4, bf16x8>::type;
+  QPiece qop[QN];
+  {
+    const T* src = (const T*)p.q + (long long)(tok0 + qi) * p.q_sn + (long long)head * p.q_sh;
+#pragma unroll
+    for (int c = 0; c < QN; ++c) qop[c] = *(const QPiece*)(src + (2 * c + h) * (16 / ES));
+  }
+  unsigned long long sees = 0;                              // trees: the nodes that the lane's row sees
+  if constexpr (TREE) {
+    const unsigned long long m = tree_masks(p.parents + seq * p.parents_sb, p.nodes);
+    sees = (unsigned long long)(unsigned)__shfl((int)(m >> 32), qi) << 32 | (unsigned)__shfl((int)(unsigned)m, qi);
+  }
+  const int lim = off + qi;                                 // prompts: the last token that the row sees
+  // the first token that some row of the wave does not see
+  const int edge = TREE ? off : __builtin_amdgcn_readfirstlane(off + min(tile * ROWS + rb * 32, R - 1) / p.G) + 1;
+
+  float m_run = -INFINITY, l_run = 0.f;
+  f32x16 acc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[db][e] = 0.f;
+
+  // LDS offsets of the lane's operands in a tile: K piece c of row j, V piece of d block db
+  unsigned k_off[QN], v_off[DB];
+#pragma unroll
+  for (int c = 0; c < QN; ++c) k_off[c] = j * ROWB + (((2 * c + h) ^ Tile::swizzle(j)) * 16);
+  const int v_row = F32 ? 4 * h : 4 * h + ((lane & 15) >> 2);
+#pragma unroll
+  for (int db = 0; db < DB; ++db) {
+    if constexpr (F32) v_off[db] = 0;
+    else v_off[db] = v_row * ROWB + (((4 * db + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ Tile::swizzle(v_row)) * 16) + (lane & 1) * 8;
+  }
+
+  for (int si = 0; si < n_stage; ++si) {
+    WaitLadder<NST - 2>::template run<PER>(issued - 1 - si);
+    __syncthreads();                                        // stage si is in the LDS; everyone is past stage si - 1
+    if (issued < n_stage) issue(issued++);
+    const unsigned char* Kt = ring + (si % NST) * SM::kStage + tg * TW * ROWB;
+    const unsigned char* Vt = Kt + SM::kTileBytes;
+    const int n0 = (s_lo + si) * ST + tg * TW;
+
+    f32x16 s[TB];
+#pragma unroll
+    for (int tb = 0; tb < TB; ++tb) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[tb][e] = 0.f;
+#pragma unroll
+      for (int c = 0; c < QN; ++c) {
+        const QPiece kop = *(const QPiece*)(Kt + tb * 32 * ROWB + k_off[c]);
+        if constexpr (F32) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) s[tb] = __builtin_amdgcn_mfma_f32_32x32x2f32(kop[x], qop[c][x], s[tb], 0, 0, 0);
+        } else {
+          s[tb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop, qop[c], s[tb], 0, 0, 0);
+        }
+      }
+    }
+    const bool at_edge = n0 + TW > edge;
+    unsigned vis = 0xffffffffu;
+    if (at_edge) {
+      vis = 0;
+#pragma unroll
+      for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int n = n0 + tb * 32 + 8 * (e / 4) + 4 * h + e % 4;
+          bool see;
+          if constexpr (TREE) {
+            const int node = n - off;
+            see = node < 0 ? sees != 0 : node < 64 && ((sees >> (node & 63)) & 1);
+          } else {
+            see = n <= lim;
+          }
+          if (see) vis |= 1u << (tb * 16 + e);
+          else s[tb][e] = -INFINITY;
+        }
+    }
+    float sv[TB * 16];
+#pragma unroll
+    for (int e = 0; e < TB * 16; ++e) sv[e] = s[e / 16][e % 16];
+    float mx = max_nan_of(sv);
+    {
+      auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      mx = max_nan(__uint_as_float(x[0]), __uint_as_float(x[1])) * p.scale_log2;
+    }
+    // the reference moves only when the maximum exceeds it by 2^8: probabilities stay below that, and rescaling is rare
+    const bool up = mx > m_run + 8.f;                       // also true of the first finite maximum
+    if (__any(up)) {
+      const float a = up ? fast_exp2(m_run - mx) : 1.f;
+      if (up) m_run = mx;
+      l_run *= a;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[db][e] *= a;
+    }
+    const float neg_m = m_run == -INFINITY ? 0.f : -m_run;
+
+    if constexpr (F32) {
+#pragma unroll
+      for (int e = 0; e < TB * 16; ++e) {
+        sv[e] = fast_exp2(fmaf(s[e / 16][e % 16], p.scale_log2, neg_m));
+        l_run += sv[e];
+      }
+      // V^T's operand: channel j of d block db, the token that register e holds in this half
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        bool odd = false;
+#pragma unroll
+        for (int e = 0; e < TB * 16; ++e) {
+          const int t = (e / 16) * 32 + 8 * ((e % 16) / 4) + 4 * h + e % 4;
+          float vop = *(const float*)(Vt + t * ROWB + (((8 * db + j / 4) ^ Tile::swizzle(t)) * 16) + (j & 3) * 4);
+          if (at_edge) {
+            const bool bad = !(fabsf(vop) < INFINITY);
+            odd |= bad;
+            vop = bad ? 0.f : vop;
+          }
+          acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(vop, sv[e], acc[db], 0, 0, 0);
+        }
+        if (at_edge && __any(odd)) {
+          // infinities and NaN of tokens that some rows see: counted for each row among those that it sees
+          constexpr float kind[3] = {INFINITY, -INFINITY, NAN};
+          for (int w = 0; w < 3; ++w) {
+            f32x16 n;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) n[e] = 0.f;
+#pragma unroll
+            for (int e = 0; e < TB * 16; ++e) {
+              const int t = (e / 16) * 32 + 8 * ((e % 16) / 4) + 4 * h + e % 4;
+              const float x = *(const float*)(Vt + t * ROWB + (((8 * db + j / 4) ^ Tile::swizzle(t)) * 16) + (j & 3) * 4);
+              const bool is = w == 0 ? x == INFINITY : w == 1 ? x == -INFINITY : x != x;
+              n = __builtin_amdgcn_mfma_f32_32x32x2f32(is ? 1.f : 0.f, (vis >> e) & 1 ? 1.f : 0.f, n, 0, 0, 0);
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[db][e] = n[e] > 0.f ? acc[db][e] + kind[w] : acc[db][e];
+          }
+        }
+      }
+    } else {
+      // P is rounded to bf16 for the matrix unit, and the denominator sums the same rounded values: a token that has nearly all the
+      // weight keeps its row of V
+      unsigned pk[TB * 8];
+#pragma unroll
+      for (int i = 0; i < TB * 8; ++i) {
+        const rows_f32x2 x = {fast_exp2(fmaf(s[i / 8][(2 * i) % 16], p.scale_log2, neg_m)),
+                              fast_exp2(fmaf(s[i / 8][(2 * i + 1) % 16], p.scale_log2, neg_m))};
+        pk[i] = __builtin_bit_cast(unsigned, __builtin_convertvector(x, rows_bf16x2));
+        l_run += __uint_as_float(pk[i] << 16) + __uint_as_float(pk[i] & 0xffff0000u);
+      }
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        bool odd = false;
+#pragma unroll
+        for (int ks = 0; ks < TB * 2; ++ks) {
+          const rows_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) rows_s16x4*)(Vt + (16 * ks) * ROWB + v_off[db]));
+          // (eight rows on: the rows' swizzle differs in one bit)
+          const rows_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) rows_s16x4*)(Vt + (16 * ks + 8) * ROWB + (v_off[db] ^ 32)));
+          u32x4 vr = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+          if (at_edge) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              const bool b0 = (vr[w] & 0x7f80u) == 0x7f80u, b1 = (vr[w] & 0x7f800000u) == 0x7f800000u;
+              odd |= b0 || b1;
+              vr[w] = (b0 ? 0u : vr[w] & 0xffffu) | (b1 ? 0u : vr[w] & 0xffff0000u);
+            }
+          }
+          const u32x4 pr = {pk[4 * ks], pk[4 * ks + 1], pk[4 * ks + 2], pk[4 * ks + 3]};
+          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vr), __builtin_bit_cast(bf16x8, pr), acc[db], 0, 0, 0);
+        }
+        if (at_edge && __any(odd)) {
+          for (int w = 0; w < 3; ++w) {
+            f32x16 n;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) n[e] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < TB * 2; ++ks) {
+              u32x4 is, seen;
+#pragma unroll
+              for (int x = 0; x < 4; ++x) {
+                unsigned both[2];
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                  const int e = 2 * x + y, t = 16 * ks + 8 * (e / 4) + 4 * h + e % 4, c = 32 * db + j;
+                  const unsigned b = *(const uint16_t*)(Vt + t * ROWB + (((c / 8) ^ Tile::swizzle(t)) * 16) + (c % 8) * 2);
+                  const bool hit = w == 0 ? b == 0x7f80u : w == 1 ? b == 0xff80u : (b & 0x7fffu) > 0x7f80u;
+                  both[y] = hit ? 0x3f80u : 0u;
+                }
+                is[x] = both[0] | both[1] << 16;
+                seen[x] = ((vis >> (8 * ks + 2 * x)) & 1 ? 0x3f80u : 0u) | ((vis >> (8 * ks + 2 * x + 1)) & 1 ? 0x3f800000u : 0u);
+              }
+              n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, is), __builtin_bit_cast(bf16x8, seen), n, 0, 0, 0);
+            }
+            const float add = w == 0 ? INFINITY : w == 1 ? -INFINITY : NAN;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[db][e] = n[e] > 0.f ? acc[db][e] + add : acc[db][e];
+          }
+        }
+      }
+    }
+  }
+  wait_vmcnt<0>();                                          // no transfer may still be writing LDS past this point
+
+  // ---- the row's sums, the token groups' states ----
+  {
+    auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run), false, false);
+    l_run = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+  }
+  if constexpr (TG > 1) {
+    if (h == 0) {
+      stat_m[tg * ROWS + rb * 32 + j] = m_run;
+      stat_l[tg * ROWS + rb * 32 + j] = l_run;
+    }
+    __syncthreads();                                        // everyone is done reading the ring
+    f32x4* xbuf = (f32x4*)ring;                             // [TG - 1][RB][DB * 4][64]
+    if (tg > 0) {
+#pragma unroll
+      for (int i = 0; i < DB * 4; ++i)
+        xbuf[(((tg - 1) * RB + rb) * DB * 4 + i) * 64 + lane] =
+            (f32x4){acc[i / 4][4 * (i % 4)], acc[i / 4][4 * (i % 4) + 1], acc[i / 4][4 * (i % 4) + 2], acc[i / 4][4 * (i % 4) + 3]};
+    }
+    __syncthreads();
+    if (tg > 0) return;
+    float mm = m_run;
+#pragma unroll
+    for (int w = 1; w < TG; ++w) mm = max_nan(mm, stat_m[w * ROWS + rb * 32 + j]);
+    float f = m_run == -INFINITY ? 0.f : fast_exp2(m_run - mm);
+    l_run *= f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[db][e] *= f;
+#pragma unroll
+    for (int w = 1; w < TG; ++w) {
+      const float mw = stat_m[w * ROWS + rb * 32 + j];
+      f = mw == -INFINITY ? 0.f : fast_exp2(mw - mm);
+      l_run = fmaf(f, stat_l[w * ROWS + rb * 32 + j], l_run);
+#pragma unroll
+      for (int i = 0; i < DB * 4; ++i) {
+        const f32x4 o = xbuf[(((w - 1) * RB + rb) * DB * 4 + i) * 64 + lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i / 4][4 * (i % 4) + e] = fmaf(f, o[e], acc[i / 4][4 * (i % 4) + e]);
+      }
+    }
+    m_run = mm;
+  }
+  if (row >= R) return;
+  const bool nothing = TREE ? sees == 0 : lim < 0;
+  if (nothing) {
+    m_run = -INFINITY;
+    l_run = 0.f;
+  }
+  const long long at = (long long)(tok0 + qi) * p.H + head;
+  if (p.S > 1) {
+    const long long slot = (long long)split * p.total_q * p.H + at;
+    if (h == 0) {
+      p.part_m[slot] = m_run;
+      p.part_l[slot] = l_run;
+    }
+    float* o = p.part_o + slot * D;
+#pragma unroll
+    for (int i = 0; i < DB * 4; ++i) {
+      f32x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = nothing ? 0.f : acc[i / 4][4 * (i % 4) + e];
+      *(f32x4*)(o + (i / 4) * 32 + (i % 4) * 8 + 4 * h) = x;
+    }
+    return;
+  }
+  const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
+  T* o = (T*)p.out + at * D;
+#pragma unroll
+  for (int i = 0; i < DB * 4; ++i) {
+    float x[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = l_run == 0.f ? 0.f : acc[i / 4][4 * (i % 4) + e] * inv;
+    T* to = o + (i / 4) * 32 + (i % 4) * 8 + 4 * h;
+    if constexpr (F32) *(f32x4*)to = (f32x4){x[0], x[1], x[2], x[3]};
+    else {
+      const rows_f32x2 a = {x[0], x[1]}, b = {x[2], x[3]};
+      uint2 w;
+      w.x = __builtin_bit_cast(unsigned, __builtin_convertvector(a, rows_bf16x2));
+      w.y = __builtin_bit_cast(unsigned, __builtin_convertvector(b, rows_bf16x2));
+      *(uint2*)to = w;
+    }
+  }
+  if (p.lse != nullptr && h == 0) {
+    const long long to = TREE ? ((long long)seq * p.H + head) * p.nodes + qi : (long long)head * p.total_q + tok0 + qi;
+    p.lse[to] = (m_run + __log2f(l_run)) * kLn2;
+  }
+}
+
+// Merge of the S blocks that shared a tile: a wave takes one (token, query head).
+template <typename T, int D, bool TREE>
+__global__ __launch_bounds__(256) void rows_combine(RowsParams p) {
+  const int lane = threadIdx.x & 63;
+  const long long n = (long long)p.total_q * p.H, at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (at >= n) return;
+  const int tok = (int)(at / p.H), head = (int)(at - (long long)tok * p.H);
+  // rows of no sequence stay as they were
+  if (!TREE && (tok < p.cu_q[0] || tok >= p.cu_q[p.n_seq])) return;
+  float m = -INFINITY, l = 0.f;
+  if (lane < p.S) {
+    m = p.part_m[lane * n + at];
+    l = p.part_l[lane * n + at];
+  }
+  const float mm = wave_max(m);
+  const float w = m == -INFINITY ? 0.f : fast_exp2(m - mm);
+  const float den = wave_sum(w * l);
+  constexpr int PER = D / 64;
+  float o[PER] = {};
+  for (int s = 0; s < p.S; ++s) {
+    const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s));
+    if (f == 0.f) continue;
+    const float* src = p.part_o + ((long long)s * n + at) * D + lane * PER;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) o[e] = fmaf(f, src[e], o[e]);
+  }
+  const float inv = den == 0.f ? 0.f : 1.f / den;
+  T* to = (T*)p.out + at * D + lane * PER;
+#pragma unroll
+  for (int e = 0; e < PER; ++e) Elem<T>::store(to + e, den == 0.f ? 0.f : o[e] * inv);
+  if (p.lse != nullptr && lane == 0) {
+    const int i = TREE ? tok % p.nodes : tok;
+    p.lse[TREE ? ((long long)(tok / p.nodes) * p.H + head) * p.nodes + i : (long long)head * p.total_q + tok] = (mm + __log2f(den)) * kLn2;
+  }
+}
+
+// what a block of RB row blocks looks like: token groups, tokens of a wave in a stage, stages
+template <typename T, int D, int RB> struct RowsShape;
+template <int D> struct RowsShape<uint16_t, D, 8> { static constexpr int TG = 1, TW = 64, NST = 3; };
+template <int D> struct RowsShape<uint16_t, D, 4> { static constexpr int TG = 2, TW = 32, NST = 3; };
+template <int D> struct RowsShape<uint16_t, D, 2> { static constexpr int TG = 4, TW = 32, NST = 2; };
+template <int D> struct RowsShape<uint16_t, D, 1> { static constexpr int TG = 4, TW = 32, NST = 2; };
+template <int D> struct RowsShape<float, D, 8> { static constexpr int TG = 1, TW = 32, NST = 3; };
+template <int D> struct RowsShape<float, D, 4> { static constexpr int TG = 2, TW = 32, NST = 2; };
+template <int D> struct RowsShape<float, D, 2> { static constexpr int TG = 2, TW = 32, NST = 2; };
+template <int D> struct RowsShape<float, D, 1> { static constexpr int TG = 2, TW = 32, NST = 2; };
+
+template <typename T, int D, int RB, bool PAGED, bool TREE>
+static hipError_t launch_rows_rb(const RowsParams& p, hipStream_t st) {
+  using Sh = RowsShape<T, D, RB>;
+  constexpr int smem = RowsSmem<T, D, RB, Sh::TG, Sh::TW, Sh::NST>::total();
+  constexpr auto kernel = attn_rows<T, D, RB, Sh::TG, Sh::TW, Sh::NST, PAGED, TREE>;
+  const hipError_t e = allow_dynamic_lds<kernel>(smem);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)p.n_tiles * p.Hkv, p.S), dim3(RB * Sh::TG * 64), smem, st, p);
+  return hipGetLastError();
+}
+
+template <typename T, int D, bool PAGED, bool TREE>
+static hipError_t launch_rows_d(const RowsParams& p, int rb, hipStream_t st) {
+  hipError_t e;
+  switch (rb) {
+    case 8: e = launch_rows_rb<T, D, 8, PAGED, TREE>(p, st); break;
+    case 4: e = launch_rows_rb<T, D, 4, PAGED, TREE>(p, st); break;
+    case 2: e = launch_rows_rb<T, D, 2, PAGED, TREE>(p, st); break;
+    default: e = launch_rows_rb<T, D, 1, PAGED, TREE>(p, st); break;
+  }
+  if (e != hipSuccess || p.S == 1) return e;
+  hipLaunchKernelGGL((rows_combine<T, D, TREE>), dim3((unsigned)(((long long)p.total_q * p.H + 3) / 4)), dim3(256), 0, st, p);
+  return hipGetLastError();
+}
+
+template <bool TREE>
+static hipError_t launch_rows(const RowsParams& p, int rb, int dtype, int head_dim, hipStream_t st) {
+  const bool paged = p.block_table != nullptr, bf16 = dtype == HIPPO_DTYPE_BF16;
+  if (head_dim == 128) {
+    if (bf16) return paged ? launch_rows_d<uint16_t, 128, true, TREE>(p, rb, st) : launch_rows_d<uint16_t, 128, false, TREE>(p, rb, st);
+    return paged ? launch_rows_d<float, 128, true, TREE>(p, rb, st) : launch_rows_d<float, 128, false, TREE>(p, rb, st);
+  }
+  if (bf16) return paged ? launch_rows_d<uint16_t, 64, true, TREE>(p, rb, st) : launch_rows_d<uint16_t, 64, false, TREE>(p, rb, st);
+  return paged ? launch_rows_d<float, 64, true, TREE>(p, rb, st) : launch_rows_d<float, 64, false, TREE>(p, rb, st);
+}
+
+hipError_t launch_prefill(const RowsParams& p, int rb, int dtype, int head_dim, hipStream_t st);
+hipError_t launch_tree(const RowsParams& p, int rb, int dtype, int head_dim, hipStream_t st);
+
+}  // namespace hippo
