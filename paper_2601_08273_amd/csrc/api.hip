@@ -390,6 +390,7 @@ int check_packed(const hippo_packed_desc* d) {
   if (d->n_kv_heads < 1 || d->n_q_heads < 1 || d->n_q_heads % d->n_kv_heads != 0) return HIPPO_ERR_BAD_SHAPE;
   if (d->n_q_heads > 65535 || (d->head_dim != 64 && d->head_dim != 128)) return HIPPO_ERR_BAD_SHAPE;
   if (d->q_stride_n < 0 || d->q_stride_h < 0 || d->kv_stride_n < 0 || d->kv_stride_h < 0) return HIPPO_ERR_BAD_SHAPE;
+  if (d->kv_stride_n > (1ll << 24)) return HIPPO_ERR_BAD_SHAPE;   // row offsets inside a transfer stay 32-bit
   const int per16 = 16 / elem_bytes(d->dtype);
   if (d->q_stride_n % per16 || d->q_stride_h % per16 || d->kv_stride_n % per16 || d->kv_stride_h % per16) return HIPPO_ERR_BAD_ALIGN;
   return HIPPO_OK;

@@ -167,6 +167,21 @@ __device__ __forceinline__ unsigned long long tree_masks(const int32_t* parents,
   return none ? 0ull : (unsigned long long)hi << 32 | lo;
 }
 
+// 16 bytes a lane from `base` (uniform) + `off` (of the lane) straight into LDS at lds_addr + lane * 16, see dma16
+__device__ __forceinline__ void dma16_from(const void* base, unsigned off, unsigned lds_addr) {
+  const unsigned uniform_addr = __builtin_amdgcn_readfirstlane(lds_addr);
+  unsigned saved_m0;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
+               : "=&s"(saved_m0)
+               : "v"(off), "s"(base), "s"(uniform_addr)
+               : "memory");
+}
+// The compiler cannot always tell that a value is the same in all lanes.
+__device__ __forceinline__ long long uniform64(long long x) {
+  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)x), hi = __builtin_amdgcn_readfirstlane((unsigned)((unsigned long long)x >> 32));
+  return (long long)((unsigned long long)hi << 32 | lo);
+}
+
 template <typename T, int D, int RB, int TG, int TW, int NST, bool PAGED, bool TREE>
 __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   using Tile = RowsTile<T, D>;
@@ -175,8 +190,11 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   constexpr int ES = sizeof(T), ROWB = Tile::kRowBytes, RPT = Tile::kRowsPerXfer, CPR = Tile::kPieces;
   constexpr int WAVES = RB * TG, ROWS = RB * 32, ST = TG * TW, TB = TW / 32, DB = D / 32;
   constexpr int NLD = ST / RPT, PER = 2 * NLD / WAVES;      // transfers of a stage's K (or V); of a wave a stage
+  constexpr int NSW = 16 / RPT < PER ? 16 / RPT : PER;      // a wave's transfers after which the rows' swizzle repeats
+  constexpr int NPG = PER * RPT > 16 ? PER * RPT / 16 : 1;  // runs of 16 rows (of a page each) in a wave's transfers
   constexpr int QN = CPR / 2;                               // 16-byte pieces of a query row in a lane
-  static_assert(2 * NLD % WAVES == 0 && PER * (NST - 1) <= 63 && NST >= 2, "transfer split");
+  constexpr int SN = TB * 16;                               // logits of a wave's stage in a lane
+  static_assert(2 * NLD % WAVES == 0 && NLD % PER == 0 && PER * (NST - 1) <= 63 && NST >= 2, "transfer split");
 
   extern __shared__ __align__(16) unsigned char smem[];
   unsigned char* ring = smem;
@@ -221,36 +239,61 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   const int all_stages = (ext + ST - 1) / ST;
   const int s_lo = (int)((long long)all_stages * split / p.S), s_hi = (int)((long long)all_stages * (split + 1) / p.S);
   const int n_stage = s_hi - s_lo;
+  // the first token that some row of the block does not see: the stages before it need no mask
+  const int block_edge = TREE ? off : off + tile * ROWS / p.G + 1;
+  const int n_plain = min(max(block_edge / ST - s_lo, 0), n_stage);
 
-  // ---- transfers ----
-  const char* kbase = (const char*)p.k + ((PAGED ? 0ll : TREE ? (long long)seq * p.k_sb : row0_k * p.k_sn) + (long long)hk * p.k_sh) * ES;
-  const char* vbase = (const char*)p.v + ((PAGED ? 0ll : TREE ? (long long)seq * p.k_sb : row0_k * p.k_sn) + (long long)hk * p.k_sh) * ES;
+  // ---- transfers: the first half of the waves fetches K, the other half V ----
+  const bool fetch_v = wave >= WAVES / 2;
+  const char* base = (const char*)(fetch_v ? p.v : p.k) +
+                     ((PAGED ? 0ll : TREE ? (long long)seq * p.k_sb : row0_k * p.k_sn) + (long long)hk * p.k_sh) * ES;
   const int ld_row = lane / CPR, ld_pc = lane % CPR;
-  const int cap = ext - 1;
+  const int cap = ext - 1, first_row = wave % (WAVES / 2) * PER * RPT;       // of the stage's rows, the wave's first
+  const unsigned row_bytes = (unsigned)(p.k_sn * ES);       // (the host keeps a row's stride below 2^24 elements)
+  unsigned lane_off[NSW];
+#pragma unroll
+  for (int i = 0; i < NSW; ++i) lane_off[i] = ld_row * row_bytes + ((ld_pc ^ Tile::swizzle(first_row + i * RPT + ld_row)) * 16);
   const int page_mask = PAGED ? (1 << p.page_shift) - 1 : 0;
   const int32_t* table = PAGED ? p.block_table + (long long)seq * p.max_pages : nullptr;
-  auto issue = [&](int si) {
-    const unsigned dst = ring_addr + (si % NST) * SM::kStage;
-    const int n0 = (s_lo + si) * ST;
+  // pages of the next stage to be fetched: asked for a stage ahead, through the scalar cache.  Rows of a run of 16 share a page, as
+  // a page's size is a multiple of 16.
+  int page[NPG];
+  auto ask_pages = [&](int si) {
+    if constexpr (PAGED) {
 #pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      const int x = wave * PER + u, which = x / NLD, n = x % NLD;
-      const int r = n * RPT + ld_row;
-      const int row = min(n0 + r, cap);                     // rows behind the last one repeat it
-      long long at;
-      if constexpr (PAGED) {
-        // a transfer's rows share a page: it starts at a multiple of its rows, which divide a page's
-        int pg = table[min(n0 + n * RPT, cap) >> p.page_shift];
-        pg = min(max(pg, 0), p.n_pool_pages - 1);
-        at = (long long)pg * p.page_stride + (long long)(row & page_mask) * p.k_sn;
-      } else {
-        at = (long long)row * p.k_sn;
+      for (int i = 0; i < NPG; ++i) {
+        const int row = min((s_lo + si) * ST + first_row + i * 16, cap);
+        page[i] = table[max(row, 0) >> p.page_shift];
       }
-      dma16((which ? vbase : kbase) + at * ES + ((ld_pc ^ Tile::swizzle(r)) * 16), dst + which * SM::kTileBytes + n * 1024);
     }
   };
-  int issued = min(n_stage, NST - 1);
-  for (int si = 0; si < issued; ++si) issue(si);
+  auto issue = [&](int si) {
+    const unsigned dst = ring_addr + (si % NST) * SM::kStage + (fetch_v ? SM::kTileBytes : 0) + first_row * ROWB;
+    const int n0 = (s_lo + si) * ST + first_row;
+    const bool whole = n0 + PER * RPT <= ext;
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      const int row0 = n0 + u * RPT;
+      const int pg = PAGED ? min(max(page[u * RPT / 16], 0), p.n_pool_pages - 1) : 0;
+      if (whole) {
+        const long long at = PAGED ? (long long)pg * p.page_stride + (long long)(row0 & page_mask) * p.k_sn : (long long)row0 * p.k_sn;
+        dma16_from((const char*)uniform64((long long)(base + at * ES)), lane_off[u % NSW], dst + u * 1024);
+      } else {                                              // rows behind the last one repeat it
+        const int row = min(row0 + ld_row, cap);
+        const long long at = PAGED ? (long long)pg * p.page_stride + (long long)(row & page_mask) * p.k_sn : (long long)row * p.k_sn;
+        dma16(base + at * ES + ((ld_pc ^ Tile::swizzle(first_row + u * RPT + ld_row)) * 16), dst + u * 1024);
+      }
+    }
+  };
+  int issued = 0;
+  auto issue_next = [&]() {
+    if (issued >= n_stage) return;
+    issue(issued++);
+    if (issued < n_stage) ask_pages(issued);
+  };
+  if (n_stage > 0) ask_pages(0);
+#pragma unroll
+  for (int i = 0; i < NST - 1; ++i) issue_next();
 
   // ---- the wave's query rows ----
   const int row = tile * ROWS + rb * 32 + j;
@@ -268,8 +311,6 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
     sees = (unsigned long long)(unsigned)__shfl((int)(m >> 32), qi) << 32 | (unsigned)__shfl((int)(unsigned)m, qi);
   }
   const int lim = off + qi;                                 // prompts: the last token that the row sees
-  // the first token that some row of the wave does not see
-  const int edge = TREE ? off : __builtin_amdgcn_readfirstlane(off + min(tile * ROWS + rb * 32, R - 1) / p.G) + 1;
 
   float m_run = -INFINITY, l_run = 0.f;
   f32x16 acc[DB];
@@ -278,33 +319,29 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[db][e] = 0.f;
 
-  // LDS offsets of the lane's operands in a tile: K piece c of row j, V piece of d block db
-  unsigned k_off[QN], v_off[DB];
-#pragma unroll
-  for (int c = 0; c < QN; ++c) k_off[c] = j * ROWB + (((2 * c + h) ^ Tile::swizzle(j)) * 16);
-  const int v_row = F32 ? 4 * h : 4 * h + ((lane & 15) >> 2);
-#pragma unroll
-  for (int db = 0; db < DB; ++db) {
-    if constexpr (F32) v_off[db] = 0;
-    else v_off[db] = v_row * ROWB + (((4 * db + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ Tile::swizzle(v_row)) * 16) + (lane & 1) * 8;
-  }
+  // LDS offsets of the lane's operands in a tile: K piece c of row j at k_off ^ 32 c, V piece of d block db at v_off ^ 64 db (a tile's
+  // rows are powers of two apart, and the swizzle is an exclusive or).  The reads' addresses are formed stage by stage: kept in
+  // registers they are more than there are.
+  const unsigned k_off = j * ROWB + ((h ^ Tile::swizzle(j)) * 16);
+  const int v_row = 4 * h + ((lane & 15) >> 2);
+  const unsigned v_off = v_row * ROWB + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ Tile::swizzle(v_row)) * 16) + (lane & 1) * 8;
 
-  for (int si = 0; si < n_stage; ++si) {
-    WaitLadder<NST - 2>::template run<PER>(issued - 1 - si);
-    __syncthreads();                                        // stage si is in the LDS; everyone is past stage si - 1
-    if (issued < n_stage) issue(issued++);
-    const unsigned char* Kt = ring + (si % NST) * SM::kStage + tg * TW * ROWB;
-    const unsigned char* Vt = Kt + SM::kTileBytes;
-    const int n0 = (s_lo + si) * ST + tg * TW;
+  // LDS addresses of a stage's tiles (numbers: constants that are added to them become the reads' immediate offsets)
+  auto k_tile = [&](int si) { return ring_addr + (si % NST) * SM::kStage + tg * TW * ROWB; };
+  auto v_tile = [&](int si) { return ring_addr + (si % NST) * SM::kStage + SM::kTileBytes + tg * TW * ROWB; };
+#define ROWS_LDS(type, address) ((__attribute__((address_space(3))) type*)(uintptr_t)(address))
 
-    f32x16 s[TB];
+  // S^T = K Q^T
+  auto logits = [&](unsigned Kt, f32x16 (&s)[TB]) {
 #pragma unroll
-    for (int tb = 0; tb < TB; ++tb) {
+    for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[tb][e] = 0.f;
 #pragma unroll
-      for (int c = 0; c < QN; ++c) {
-        const QPiece kop = *(const QPiece*)(Kt + tb * 32 * ROWB + k_off[c]);
+    for (int c = 0; c < QN; ++c) {
+#pragma unroll
+      for (int tb = 0; tb < TB; ++tb) {
+        const QPiece kop = *(ROWS_LDS(const QPiece, (Kt + k_off) ^ (32 * c)) + tb * 32 * ROWB / 16);
         if constexpr (F32) {
 #pragma unroll
           for (int x = 0; x < 4; ++x) s[tb] = __builtin_amdgcn_mfma_f32_32x32x2f32(kop[x], qop[c][x], s[tb], 0, 0, 0);
@@ -313,35 +350,14 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
         }
       }
     }
-    const bool at_edge = n0 + TW > edge;
-    unsigned vis = 0xffffffffu;
-    if (at_edge) {
-      vis = 0;
-#pragma unroll
-      for (int tb = 0; tb < TB; ++tb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int n = n0 + tb * 32 + 8 * (e / 4) + 4 * h + e % 4;
-          bool see;
-          if constexpr (TREE) {
-            const int node = n - off;
-            see = node < 0 ? sees != 0 : node < 64 && ((sees >> (node & 63)) & 1);
-          } else {
-            see = n <= lim;
-          }
-          if (see) vis |= 1u << (tb * 16 + e);
-          else s[tb][e] = -INFINITY;
-        }
-    }
-    float sv[TB * 16];
-#pragma unroll
-    for (int e = 0; e < TB * 16; ++e) sv[e] = s[e / 16][e % 16];
-    float mx = max_nan_of(sv);
+  };
+  // The rows' reference moves only when a maximum exceeds it by 2^8: weights stay below that, and rescaling is rare.  mx: of the tokens
+  // in this half of the wave, unscaled
+  auto refer_to = [&](float mx) {
     {
       auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
       mx = max_nan(__uint_as_float(x[0]), __uint_as_float(x[1])) * p.scale_log2;
     }
-    // the reference moves only when the maximum exceeds it by 2^8: probabilities stay below that, and rescaling is rare
     const bool up = mx > m_run + 8.f;                       // also true of the first finite maximum
     if (__any(up)) {
       const float a = up ? fast_exp2(m_run - mx) : 1.f;
@@ -352,111 +368,259 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[db][e] *= a;
     }
+  };
+  auto refer = [&](const f32x16 (&s)[TB]) {
+    float sv[SN];
+#pragma unroll
+    for (int e = 0; e < SN; ++e) sv[e] = s[e / 16][e % 16];
+    refer_to(max_nan_of(sv));
+  };
+  // Logits become weights: fp32 in place, for bf16 pairs in pk.  For the matrix unit P is rounded to bf16, and the denominator sums the
+  // same rounded values: a token that has nearly all the weight keeps its row of V.
+  auto weights = [&](f32x16 (&s)[TB], unsigned (&pk)[SN / 2]) {
     const float neg_m = m_run == -INFINITY ? 0.f : -m_run;
-
     if constexpr (F32) {
 #pragma unroll
-      for (int e = 0; e < TB * 16; ++e) {
-        sv[e] = fast_exp2(fmaf(s[e / 16][e % 16], p.scale_log2, neg_m));
-        l_run += sv[e];
-      }
-      // V^T's operand: channel j of d block db, the token that register e holds in this half
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        bool odd = false;
-#pragma unroll
-        for (int e = 0; e < TB * 16; ++e) {
-          const int t = (e / 16) * 32 + 8 * ((e % 16) / 4) + 4 * h + e % 4;
-          float vop = *(const float*)(Vt + t * ROWB + (((8 * db + j / 4) ^ Tile::swizzle(t)) * 16) + (j & 3) * 4);
-          if (at_edge) {
-            const bool bad = !(fabsf(vop) < INFINITY);
-            odd |= bad;
-            vop = bad ? 0.f : vop;
-          }
-          acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(vop, sv[e], acc[db], 0, 0, 0);
-        }
-        if (at_edge && __any(odd)) {
-          // infinities and NaN of tokens that some rows see: counted for each row among those that it sees
-          constexpr float kind[3] = {INFINITY, -INFINITY, NAN};
-          for (int w = 0; w < 3; ++w) {
-            f32x16 n;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) n[e] = 0.f;
-#pragma unroll
-            for (int e = 0; e < TB * 16; ++e) {
-              const int t = (e / 16) * 32 + 8 * ((e % 16) / 4) + 4 * h + e % 4;
-              const float x = *(const float*)(Vt + t * ROWB + (((8 * db + j / 4) ^ Tile::swizzle(t)) * 16) + (j & 3) * 4);
-              const bool is = w == 0 ? x == INFINITY : w == 1 ? x == -INFINITY : x != x;
-              n = __builtin_amdgcn_mfma_f32_32x32x2f32(is ? 1.f : 0.f, (vis >> e) & 1 ? 1.f : 0.f, n, 0, 0, 0);
-            }
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[db][e] = n[e] > 0.f ? acc[db][e] + kind[w] : acc[db][e];
-          }
-        }
+      for (int e = 0; e < SN; ++e) {
+        s[e / 16][e % 16] = fast_exp2(fmaf(s[e / 16][e % 16], p.scale_log2, neg_m));
+        l_run += s[e / 16][e % 16];
       }
     } else {
-      // P is rounded to bf16 for the matrix unit, and the denominator sums the same rounded values: a token that has nearly all the
-      // weight keeps its row of V
-      unsigned pk[TB * 8];
+      const rows_bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
 #pragma unroll
-      for (int i = 0; i < TB * 8; ++i) {
+      for (int i = 0; i < SN / 2; ++i) {
         const rows_f32x2 x = {fast_exp2(fmaf(s[i / 8][(2 * i) % 16], p.scale_log2, neg_m)),
                               fast_exp2(fmaf(s[i / 8][(2 * i + 1) % 16], p.scale_log2, neg_m))};
-        pk[i] = __builtin_bit_cast(unsigned, __builtin_convertvector(x, rows_bf16x2));
-        l_run += __uint_as_float(pk[i] << 16) + __uint_as_float(pk[i] & 0xffff0000u);
-      }
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        bool odd = false;
-#pragma unroll
-        for (int ks = 0; ks < TB * 2; ++ks) {
-          const rows_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (__attribute__((address_space(3))) rows_s16x4*)(Vt + (16 * ks) * ROWB + v_off[db]));
-          // (eight rows on: the rows' swizzle differs in one bit)
-          const rows_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (__attribute__((address_space(3))) rows_s16x4*)(Vt + (16 * ks + 8) * ROWB + (v_off[db] ^ 32)));
-          u32x4 vr = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-          if (at_edge) {
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              const bool b0 = (vr[w] & 0x7f80u) == 0x7f80u, b1 = (vr[w] & 0x7f800000u) == 0x7f800000u;
-              odd |= b0 || b1;
-              vr[w] = (b0 ? 0u : vr[w] & 0xffffu) | (b1 ? 0u : vr[w] & 0xffff0000u);
-            }
-          }
-          const u32x4 pr = {pk[4 * ks], pk[4 * ks + 1], pk[4 * ks + 2], pk[4 * ks + 3]};
-          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vr), __builtin_bit_cast(bf16x8, pr), acc[db], 0, 0, 0);
-        }
-        if (at_edge && __any(odd)) {
-          for (int w = 0; w < 3; ++w) {
-            f32x16 n;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) n[e] = 0.f;
-#pragma unroll
-            for (int ks = 0; ks < TB * 2; ++ks) {
-              u32x4 is, seen;
-#pragma unroll
-              for (int x = 0; x < 4; ++x) {
-                unsigned both[2];
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                  const int e = 2 * x + y, t = 16 * ks + 8 * (e / 4) + 4 * h + e % 4, c = 32 * db + j;
-                  const unsigned b = *(const uint16_t*)(Vt + t * ROWB + (((c / 8) ^ Tile::swizzle(t)) * 16) + (c % 8) * 2);
-                  const bool hit = w == 0 ? b == 0x7f80u : w == 1 ? b == 0xff80u : (b & 0x7fffu) > 0x7f80u;
-                  both[y] = hit ? 0x3f80u : 0u;
-                }
-                is[x] = both[0] | both[1] << 16;
-                seen[x] = ((vis >> (8 * ks + 2 * x)) & 1 ? 0x3f80u : 0u) | ((vis >> (8 * ks + 2 * x + 1)) & 1 ? 0x3f800000u : 0u);
-              }
-              n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, is), __builtin_bit_cast(bf16x8, seen), n, 0, 0, 0);
-            }
-            const float add = w == 0 ? INFINITY : w == 1 ? -INFINITY : NAN;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[db][e] = n[e] > 0.f ? acc[db][e] + add : acc[db][e];
-          }
-        }
+        const rows_bf16x2 r = __builtin_convertvector(x, rows_bf16x2);
+        pk[i] = __builtin_bit_cast(unsigned, r);
+        l_run = __builtin_amdgcn_fdot2_f32_bf16(r, ones, l_run, false);
       }
     }
+  };
+  // V^T's operand of d block db: bf16 16 tokens (two transposing reads, eight rows apart: the rows' swizzle differs in one bit), fp32
+  // channel j and the token that register e holds in this half
+  auto v_bf16 = [&](unsigned Vt, int db, int ks) {
+    const rows_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(ROWS_LDS(rows_s16x4, (Vt + v_off) ^ (64 * db)) + 16 * ks * ROWB / 8);
+    const rows_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(ROWS_LDS(rows_s16x4, (Vt + v_off) ^ (64 * db + 32)) + (16 * ks + 8) * ROWB / 8);
+    return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  auto token_of = [&](int e) { return e / 16 * 32 + e % 16 / 4 * 8 + 4 * h + e % 4; };
+  auto v_f32 = [&](unsigned Vt, int db, int e) {
+    const int t = token_of(e);
+    return *ROWS_LDS(const float, Vt + t * ROWB + (((8 * db + j / 4) ^ Tile::swizzle(t)) * 16) + (j & 3) * 4);
+  };
+  // O^T += V^T P^T
+  auto values = [&](unsigned Vt, const f32x16 (&s)[TB], const unsigned (&pk)[SN / 2]) {
+    if constexpr (F32) {
+#pragma unroll
+      for (int e = 0; e < SN; ++e)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v_f32(Vt, db, e), s[e / 16][e % 16], acc[db], 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int ks = 0; ks < SN / 8; ++ks) {
+        const u32x4 pr = {pk[4 * ks], pk[4 * ks + 1], pk[4 * ks + 2], pk[4 * ks + 3]};
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_bf16(Vt, db, ks)), __builtin_bit_cast(bf16x8, pr),
+                                                            acc[db], 0, 0, 0);
+      }
+    }
+  };
+  // The same where some rows do not see some tokens, whose V may hold anything: 0 times an infinity or NaN would reach the rows that
+  // do not see it.  Such entries go as zeros; where there are any, each kind is counted for each row among the tokens that it sees.
+  auto values_at_edge = [&](unsigned Vt, const f32x16 (&s)[TB], const unsigned (&pk)[SN / 2], unsigned vis) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      bool odd = false;
+      if constexpr (F32) {
+#pragma unroll
+        for (int e = 0; e < SN; ++e) {
+          const float x = v_f32(Vt, db, e);
+          const bool bad = !(fabsf(x) < INFINITY);
+          odd |= bad;
+          acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(bad ? 0.f : x, s[e / 16][e % 16], acc[db], 0, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int ks = 0; ks < SN / 8; ++ks) {
+          u32x4 x = v_bf16(Vt, db, ks);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const bool b0 = (x[w] & 0x7f80u) == 0x7f80u, b1 = (x[w] & 0x7f800000u) == 0x7f800000u;
+            odd |= b0 || b1;
+            x[w] = (b0 ? 0u : x[w] & 0xffffu) | (b1 ? 0u : x[w] & 0xffff0000u);
+          }
+          const u32x4 pr = {pk[4 * ks], pk[4 * ks + 1], pk[4 * ks + 2], pk[4 * ks + 3]};
+          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, pr), acc[db], 0, 0, 0);
+        }
+      }
+      if (!__any(odd)) continue;
+#pragma unroll 1
+      for (int w = 0; w < 3; ++w) {
+        f32x16 n;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) n[e] = 0.f;
+        if constexpr (F32) {
+#pragma unroll
+          for (int e = 0; e < SN; ++e) {
+            const float x = v_f32(Vt, db, e);
+            const bool is = w == 0 ? x == INFINITY : w == 1 ? x == -INFINITY : x != x;
+            n = __builtin_amdgcn_mfma_f32_32x32x2f32(is ? 1.f : 0.f, (vis >> e) & 1 ? 1.f : 0.f, n, 0, 0, 0);
+          }
+        } else {
+#pragma unroll
+          for (int ks = 0; ks < SN / 8; ++ks) {
+            const u32x4 x = v_bf16(Vt, db, ks);
+            u32x4 is, seen;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              unsigned both = 0;
+#pragma unroll
+              for (int y = 0; y < 2; ++y) {
+                const unsigned b = (x[i] >> (16 * y)) & 0xffffu;
+                const bool hit = w == 0 ? b == 0x7f80u : w == 1 ? b == 0xff80u : (b & 0x7fffu) > 0x7f80u;
+                both |= hit ? 0x3f80u << (16 * y) : 0u;
+              }
+              is[i] = both;
+              seen[i] = ((vis >> (8 * ks + 2 * i)) & 1 ? 0x3f80u : 0u) | ((vis >> (8 * ks + 2 * i + 1)) & 1 ? 0x3f800000u : 0u);
+            }
+            n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, is), __builtin_bit_cast(bf16x8, seen), n, 0, 0, 0);
+          }
+        }
+        const float add = w == 0 ? INFINITY : w == 1 ? -INFINITY : NAN;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[db][e] = n[e] > 0.f ? acc[db][e] + add : acc[db][e];
+      }
+    }
+  };
+  // Stage si is in the LDS, and everyone is past stage `past`'s products: the places up to that one's are filled again.
+  auto arrive = [&](int si, int past) {
+    WaitLadder<NST - 2>::template run<PER>(issued - 1 - si);
+    __syncthreads();
+    while (issued < n_stage && issued <= past + NST) issue_next();
+  };
+
+  // One step of the loop below, bf16: the next stage's logits (t), this stage's weights (from s) and their products with V, and the
+  // next stage's maxima, in this order of instructions: LDS reads AHEAD products before their use, the vector unit's work between the
+  // products.  (Left to itself the compiler reads an operand right before its product and forms the weights between the two
+  // runs of products.)
+  auto step_bf16 = [&](unsigned Kt, unsigned Vt, const f32x16 (&s)[TB], f32x16 (&t)[TB]) {
+    constexpr int NK = TB * QN, NV = DB * SN / 8, AHEAD = 4, EK = SN / NK, EV = SN / NV;
+    u32x4 ops[AHEAD];
+    unsigned pk[SN / 2];
+    const float neg_m = m_run == -INFINITY ? 0.f : -m_run;
+    const rows_bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
+    auto k_read = [&](int i) { return __builtin_bit_cast(u32x4, *(ROWS_LDS(const bf16x8, (Kt + k_off) ^ (32 * (i / TB))) + i % TB * 32 * ROWB / 16)); };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) ops[i] = k_read(i);
+#pragma unroll
+    for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) t[tb][e] = 0.f;
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      t[i % TB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ops[i % AHEAD]), qop[i / TB], t[i % TB], 0, 0, 0);
+      const int next = i + AHEAD;
+      ops[i % AHEAD] = next < NK ? k_read(next < NK ? next : 0) : v_bf16(Vt, (next - NK) % DB, (next - NK) / DB);
+#pragma unroll
+      for (int x = i * EK / 2; x < (i + 1) * EK / 2; ++x) {
+        const rows_f32x2 w = {fast_exp2(fmaf(s[x / 8][(2 * x) % 16], p.scale_log2, neg_m)),
+                              fast_exp2(fmaf(s[x / 8][(2 * x + 1) % 16], p.scale_log2, neg_m))};
+        const rows_bf16x2 r = __builtin_convertvector(w, rows_bf16x2);
+        pk[x] = __builtin_bit_cast(unsigned, r);
+        l_run = __builtin_amdgcn_fdot2_f32_bf16(r, ones, l_run, false);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    float mx = t[0][0];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int ks = i / DB;
+      const u32x4 pr = {pk[4 * ks], pk[4 * ks + 1], pk[4 * ks + 2], pk[4 * ks + 3]};
+      acc[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ops[(NK + i) % AHEAD]), __builtin_bit_cast(bf16x8, pr),
+                                                            acc[i % DB], 0, 0, 0);
+      if (i + AHEAD < NV) ops[(NK + i) % AHEAD] = v_bf16(Vt, (i + AHEAD) % DB, (i + AHEAD) / DB);
+#pragma unroll
+      for (int x = i * EV; x < (i + 1) * EV; x += 2) mx = max_nan(max_nan(mx, t[x / 16][x % 16]), t[x / 16][x % 16 + 1]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    refer_to(mx);
+  };
+
+  // ---- the stages that every row sees whole ----
+  int si = 0;
+  if constexpr (NST >= 3) {
+    // a stage's logits are formed while the one before becomes weights: two independent streams for the matrix and the vector unit
+    if (n_plain > 0) {
+      f32x16 s[TB];
+      unsigned pk[SN / 2];
+      arrive(0, -2);
+      logits(k_tile(0), s);
+      refer(s);
+      auto step = [&](f32x16 (&from)[TB], f32x16 (&to)[TB]) {
+        arrive(si + 1, si - 1);
+        if constexpr (F32) {
+          logits(k_tile(si + 1), to);
+          weights(from, pk);
+          values(v_tile(si), from, pk);
+          refer(to);
+        } else {
+          step_bf16(k_tile(si + 1), v_tile(si), from, to);
+        }
+        ++si;
+      };
+      while (si + 2 < n_plain) {                            // two at a time: which registers hold which stage is fixed
+        f32x16 t[TB];
+        step(s, t);
+        step(t, s);
+      }
+      if (si + 1 < n_plain) {
+        f32x16 t[TB];
+        step(s, t);
+#pragma unroll
+        for (int tb = 0; tb < TB; ++tb) s[tb] = t[tb];
+      }
+      weights(s, pk);
+      values(v_tile(si), s, pk);
+      ++si;
+    }
+  } else {
+    for (; si < n_plain; ++si) {
+      arrive(si, si - 1);
+      f32x16 s[TB];
+      unsigned pk[SN / 2];
+      logits(k_tile(si), s);
+      refer(s);
+      weights(s, pk);
+      values(v_tile(si), s, pk);
+    }
+  }
+  // ---- the others ----
+  for (; si < n_stage; ++si) {
+    arrive(si, si - 1);
+    f32x16 s[TB];
+    unsigned pk[SN / 2];
+    logits(k_tile(si), s);
+    const int n0 = (s_lo + si) * ST + tg * TW;
+    unsigned vis = 0;
+#pragma unroll
+    for (int e = 0; e < SN; ++e) {
+      const int n = n0 + token_of(e);
+      bool see;
+      if constexpr (TREE) {
+        const int node = n - off;
+        see = node < 0 ? sees != 0 : node < 64 && ((sees >> (node & 63)) & 1);
+      } else {
+        see = n <= lim;
+      }
+      if (see) vis |= 1u << e;
+      else s[e / 16][e % 16] = -INFINITY;
+    }
+    refer(s);
+    weights(s, pk);
+    values_at_edge(v_tile(si), s, pk, vis);
   }
   wait_vmcnt<0>();                                          // no transfer may still be writing LDS past this point
 
@@ -587,11 +751,11 @@ __global__ __launch_bounds__(256) void rows_combine(RowsParams p) {
 
 // what a block of RB row blocks looks like: token groups, tokens of a wave in a stage, stages
 template <typename T, int D, int RB> struct RowsShape;
-template <int D> struct RowsShape<uint16_t, D, 8> { static constexpr int TG = 1, TW = 64, NST = 3; };
-template <int D> struct RowsShape<uint16_t, D, 4> { static constexpr int TG = 2, TW = 32, NST = 3; };
+template <int D> struct RowsShape<uint16_t, D, 8> { static constexpr int TG = 1, TW = 64, NST = 4; };
+template <int D> struct RowsShape<uint16_t, D, 4> { static constexpr int TG = 2, TW = 32, NST = 4; };
 template <int D> struct RowsShape<uint16_t, D, 2> { static constexpr int TG = 4, TW = 32, NST = 2; };
 template <int D> struct RowsShape<uint16_t, D, 1> { static constexpr int TG = 4, TW = 32, NST = 2; };
-template <int D> struct RowsShape<float, D, 8> { static constexpr int TG = 1, TW = 32, NST = 3; };
+template <int D> struct RowsShape<float, D, 8> { static constexpr int TG = 1, TW = 32, NST = 4; };
 template <int D> struct RowsShape<float, D, 4> { static constexpr int TG = 2, TW = 32, NST = 2; };
 template <int D> struct RowsShape<float, D, 2> { static constexpr int TG = 2, TW = 32, NST = 2; };
 template <int D> struct RowsShape<float, D, 1> { static constexpr int TG = 2, TW = 32, NST = 2; };
