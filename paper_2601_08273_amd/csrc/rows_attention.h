@@ -167,14 +167,32 @@ __device__ __forceinline__ unsigned long long tree_masks(const int32_t* parents,
   return none ? 0ull : (unsigned long long)hi << 32 | lo;
 }
 
-// 16 bytes a lane from `base` (uniform) + `off` (of the lane) straight into LDS at lds_addr + lane * 16, see dma16
-__device__ __forceinline__ void dma16_from(const void* base, unsigned off, unsigned lds_addr) {
-  const unsigned uniform_addr = __builtin_amdgcn_readfirstlane(lds_addr);
-  unsigned saved_m0;
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
-               : "=&s"(saved_m0)
-               : "v"(off), "s"(base), "s"(uniform_addr)
-               : "memory");
+// N runs of 1 KB: 16 bytes a lane from `base` (uniform) + off[i] (of the lane) straight into LDS at lds_addr + 1024 i + lane * 16, see
+// dma16
+template <int N>
+__device__ __forceinline__ void dma16_runs(const void* base, const unsigned* off, unsigned lds_addr) {
+  if constexpr (N > 4) {
+    dma16_runs<4>(base, off, lds_addr);
+    dma16_runs<N - 4>(base, off + 4, lds_addr + 4096);
+  } else {
+    static_assert(N == 2 || N == 4, "");
+    const unsigned uniform_addr = __builtin_amdgcn_readfirstlane(lds_addr);
+    unsigned saved_m0;
+    if constexpr (N == 2)
+      asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\t"
+                   "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
+                   : "=&s"(saved_m0)
+                   : "v"(off[0]), "v"(off[1]), "s"(base), "s"(uniform_addr)
+                   : "memory", "scc");
+    else
+      asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %6\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\t"
+                   "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %5\n\t"
+                   "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %5\n\t"
+                   "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, %5\n\ts_mov_b32 m0, %0"
+                   : "=&s"(saved_m0)
+                   : "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base), "s"(uniform_addr)
+                   : "memory", "scc");
+  }
 }
 // The compiler cannot always tell that a value is the same in all lanes.
 __device__ __forceinline__ long long uniform64(long long x) {
@@ -190,8 +208,8 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   constexpr int ES = sizeof(T), ROWB = Tile::kRowBytes, RPT = Tile::kRowsPerXfer, CPR = Tile::kPieces;
   constexpr int WAVES = RB * TG, ROWS = RB * 32, ST = TG * TW, TB = TW / 32, DB = D / 32;
   constexpr int NLD = ST / RPT, PER = 2 * NLD / WAVES;      // transfers of a stage's K (or V); of a wave a stage
-  constexpr int NSW = 16 / RPT < PER ? 16 / RPT : PER;      // a wave's transfers after which the rows' swizzle repeats
   constexpr int NPG = PER * RPT > 16 ? PER * RPT / 16 : 1;  // runs of 16 rows (of a page each) in a wave's transfers
+  constexpr int TR = PER / NPG;                             // transfers of a run
   constexpr int QN = CPR / 2;                               // 16-byte pieces of a query row in a lane
   constexpr int SN = TB * 16;                               // logits of a wave's stage in a lane
   static_assert(2 * NLD % WAVES == 0 && NLD % PER == 0 && PER * (NST - 1) <= 63 && NST >= 2, "transfer split");
@@ -250,9 +268,10 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   const int ld_row = lane / CPR, ld_pc = lane % CPR;
   const int cap = ext - 1, first_row = wave % (WAVES / 2) * PER * RPT;       // of the stage's rows, the wave's first
   const unsigned row_bytes = (unsigned)(p.k_sn * ES);       // (the host keeps a row's stride below 2^24 elements)
-  unsigned lane_off[NSW];
+  unsigned lane_off[TR];                                    // of a run's transfers, from its first row on
 #pragma unroll
-  for (int i = 0; i < NSW; ++i) lane_off[i] = ld_row * row_bytes + ((ld_pc ^ Tile::swizzle(first_row + i * RPT + ld_row)) * 16);
+  for (int u = 0; u < TR; ++u)
+    lane_off[u] = (u * RPT + ld_row) * row_bytes + ((ld_pc ^ Tile::swizzle(first_row + u * RPT + ld_row)) * 16);
   const int page_mask = PAGED ? (1 << p.page_shift) - 1 : 0;
   const int32_t* table = PAGED ? p.block_table + (long long)seq * p.max_pages : nullptr;
   // pages of the next stage to be fetched: asked for a stage ahead, through the scalar cache.  Rows of a run of 16 share a page, as
@@ -272,16 +291,19 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
     const int n0 = (s_lo + si) * ST + first_row;
     const bool whole = n0 + PER * RPT <= ext;
 #pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      const int row0 = n0 + u * RPT;
-      const int pg = PAGED ? min(max(page[u * RPT / 16], 0), p.n_pool_pages - 1) : 0;
+    for (int i = 0; i < NPG; ++i) {
+      const int row0 = n0 + i * TR * RPT;
+      const long long pg = PAGED ? (long long)min(max(page[i], 0), p.n_pool_pages - 1) * p.page_stride : 0ll;
       if (whole) {
-        const long long at = PAGED ? (long long)pg * p.page_stride + (long long)(row0 & page_mask) * p.k_sn : (long long)row0 * p.k_sn;
-        dma16_from((const char*)uniform64((long long)(base + at * ES)), lane_off[u % NSW], dst + u * 1024);
+        const long long at = pg + (long long)(PAGED ? row0 & page_mask : row0) * p.k_sn;
+        dma16_runs<TR>((const char*)uniform64((long long)(base + at * ES)), lane_off, dst + i * TR * 1024);
       } else {                                              // rows behind the last one repeat it
-        const int row = min(row0 + ld_row, cap);
-        const long long at = PAGED ? (long long)pg * p.page_stride + (long long)(row & page_mask) * p.k_sn : (long long)row * p.k_sn;
-        dma16(base + at * ES + ((ld_pc ^ Tile::swizzle(first_row + u * RPT + ld_row)) * 16), dst + u * 1024);
+#pragma unroll
+        for (int u = 0; u < TR; ++u) {
+          const int row = min(row0 + u * RPT + ld_row, cap);
+          const long long at = pg + (long long)(PAGED ? row & page_mask : row) * p.k_sn;
+          dma16(base + at * ES + ((ld_pc ^ Tile::swizzle(first_row + u * RPT + ld_row)) * 16), dst + (i * TR + u) * 1024);
+        }
       }
     }
   };
@@ -353,13 +375,13 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   };
   // The rows' reference moves only when a maximum exceeds it by 2^8: weights stay below that, and rescaling is rare.  mx: of the tokens
   // in this half of the wave, unscaled
-  auto refer_to = [&](float mx) {
-    {
-      auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-      mx = max_nan(__uint_as_float(x[0]), __uint_as_float(x[1])) * p.scale_log2;
-    }
+  auto refer_to = [&](float mx, auto at_last) {
+    auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+    mx = max_nan(__uint_as_float(x[0]), __uint_as_float(x[1])) * p.scale_log2;
     const bool up = mx > m_run + 8.f;                       // also true of the first finite maximum
-    if (__any(up)) {
+    const bool any = __any(up);
+    at_last();
+    if (any) {
       const float a = up ? fast_exp2(m_run - mx) : 1.f;
       if (up) m_run = mx;
       l_run *= a;
@@ -373,7 +395,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
     float sv[SN];
 #pragma unroll
     for (int e = 0; e < SN; ++e) sv[e] = s[e / 16][e % 16];
-    refer_to(max_nan_of(sv));
+    refer_to(max_nan_of(sv), [] {});
   };
   // Logits become weights: fp32 in place, for bf16 pairs in pk.  For the matrix unit P is rounded to bf16, and the denominator sums the
   // same rounded values: a token that has nearly all the weight keeps its row of V.
@@ -495,58 +517,75 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
     }
   };
   // Stage si is in the LDS, and everyone is past stage `past`'s products: the places up to that one's are filled again.
-  auto arrive = [&](int si, int past) {
-    WaitLadder<NST - 2>::template run<PER>(issued - 1 - si);
+  auto arrive = [&](int si) {
+    WaitLadder<NST - 2>::template run<PER>(max(issued - 1 - si, 0));
     __syncthreads();
+  };
+  auto refill = [&](int past) {
     while (issued < n_stage && issued <= past + NST) issue_next();
   };
 
   // One step of the loop below, bf16: the next stage's logits (t), this stage's weights (from s) and their products with V, and the
-  // next stage's maxima, in this order of instructions: LDS reads AHEAD products before their use, the vector unit's work between the
-  // products.  (Left to itself the compiler reads an operand right before its product and forms the weights between the two
-  // runs of products.)
-  auto step_bf16 = [&](unsigned Kt, unsigned Vt, const f32x16 (&s)[TB], f32x16 (&t)[TB]) {
-    constexpr int NK = TB * QN, NV = DB * SN / 8, AHEAD = 4, EK = SN / NK, EV = SN / NV;
-    u32x4 ops[AHEAD];
-    unsigned pk[SN / 2];
+  // next stage's maxima, in this order of instructions.  LDS reads go out AHEAD products before their use, the first ones of the step
+  // behind it among them (`ops` on the way in and out; that stage has landed); the vector unit's work lies evenly between the products,
+  // where a step's weights need it.  (Left to itself the compiler reads an operand right before its product and forms the weights between
+  // the two runs of products: 16640 x 28 heads x 128 2071 us, like this 1771.)
+  constexpr int AHEAD = 4;
+  u32x4 ops[AHEAD];
+  auto k_read = [&](unsigned Kt, int i) {
+    return __builtin_bit_cast(u32x4, *(ROWS_LDS(const bf16x8, (Kt + k_off) ^ (32 * (i / TB))) + i % TB * 32 * ROWB / 16));
+  };
+  auto step_bf16 = [&](unsigned Kt, unsigned Vt, unsigned Kt_behind, const f32x16 (&s)[TB], f32x16 (&t)[TB], auto fetch) {
+    constexpr int NK = TB * QN, NV = DB * SN / 8, NP = SN / 2, SPAN = NK + (SN / 8 - 1) * DB, MAX = SN / NV;
+    unsigned pk[NP];
     const float neg_m = m_run == -INFINITY ? 0.f : -m_run;
     const rows_bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
-    auto k_read = [&](int i) { return __builtin_bit_cast(u32x4, *(ROWS_LDS(const bf16x8, (Kt + k_off) ^ (32 * (i / TB))) + i % TB * 32 * ROWB / 16)); };
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i) ops[i] = k_read(i);
 #pragma unroll
     for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
       for (int e = 0; e < 16; ++e) t[tb][e] = 0.f;
-    __builtin_amdgcn_sched_barrier(0);
+    auto pairs = [&](int slot) {                            // the weights that belong into this slot
+#pragma unroll
+      for (int x = 0; x < NP; ++x)
+        if (x * SPAN / NP == slot) {
+          const rows_f32x2 w = {fast_exp2(fmaf(s[x / 8][(2 * x) % 16], p.scale_log2, neg_m)),
+                                fast_exp2(fmaf(s[x / 8][(2 * x + 1) % 16], p.scale_log2, neg_m))};
+          const rows_bf16x2 r = __builtin_convertvector(w, rows_bf16x2);
+          pk[x] = __builtin_bit_cast(unsigned, r);
+          l_run = __builtin_amdgcn_fdot2_f32_bf16(r, ones, l_run, false);
+        }
+    };
 #pragma unroll
     for (int i = 0; i < NK; ++i) {
       t[i % TB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ops[i % AHEAD]), qop[i / TB], t[i % TB], 0, 0, 0);
       const int next = i + AHEAD;
-      ops[i % AHEAD] = next < NK ? k_read(next < NK ? next : 0) : v_bf16(Vt, (next - NK) % DB, (next - NK) / DB);
-#pragma unroll
-      for (int x = i * EK / 2; x < (i + 1) * EK / 2; ++x) {
-        const rows_f32x2 w = {fast_exp2(fmaf(s[x / 8][(2 * x) % 16], p.scale_log2, neg_m)),
-                              fast_exp2(fmaf(s[x / 8][(2 * x + 1) % 16], p.scale_log2, neg_m))};
-        const rows_bf16x2 r = __builtin_convertvector(w, rows_bf16x2);
-        pk[x] = __builtin_bit_cast(unsigned, r);
-        l_run = __builtin_amdgcn_fdot2_f32_bf16(r, ones, l_run, false);
-      }
+      ops[i % AHEAD] = next < NK ? k_read(Kt, next < NK ? next : 0) : v_bf16(Vt, (next - NK) % DB, (next - NK) / DB);
+      pairs(i);
       __builtin_amdgcn_sched_barrier(0);
+      if (i == 0) fetch();
     }
     float mx = t[0][0];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
+    auto product = [&](int i) {
       const int ks = i / DB;
       const u32x4 pr = {pk[4 * ks], pk[4 * ks + 1], pk[4 * ks + 2], pk[4 * ks + 3]};
       acc[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ops[(NK + i) % AHEAD]), __builtin_bit_cast(bf16x8, pr),
                                                             acc[i % DB], 0, 0, 0);
-      if (i + AHEAD < NV) ops[(NK + i) % AHEAD] = v_bf16(Vt, (i + AHEAD) % DB, (i + AHEAD) / DB);
+      const int next = i + AHEAD;
+      ops[(NK + i) % AHEAD] = next < NV ? v_bf16(Vt, next % DB, next / DB) : k_read(Kt_behind, next - NV);
+      pairs(NK + i);
+      if (i >= 1 && i <= NV / 2) {
 #pragma unroll
-      for (int x = i * EV; x < (i + 1) * EV; x += 2) mx = max_nan(max_nan(mx, t[x / 16][x % 16]), t[x / 16][x % 16 + 1]);
+        for (int x = (i - 1) * MAX; x < i * MAX; ++x)
+          mx = max_nan(max_nan(mx, t[x / 8][(2 * x) % 16]), t[x / 8][(2 * x) % 16 + 1]);
+      }
       __builtin_amdgcn_sched_barrier(0);
-    }
-    refer_to(mx);
+    };
+#pragma unroll
+    for (int i = 0; i <= NV / 2; ++i) product(i);
+    refer_to(mx, [&] {
+#pragma unroll
+      for (int i = NV / 2 + 1; i < NV; ++i) product(i);
+    });
   };
 
   // ---- the stages that every row sees whole ----
@@ -556,18 +595,23 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
     if (n_plain > 0) {
       f32x16 s[TB];
       unsigned pk[SN / 2];
-      arrive(0, -2);
+      arrive(F32 ? 0 : 1);
       logits(k_tile(0), s);
       refer(s);
+      if constexpr (!F32) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) ops[i] = k_read(k_tile(1), i);   // (of a stage that may not exist: then not used)
+      }
       auto step = [&](f32x16 (&from)[TB], f32x16 (&to)[TB]) {
-        arrive(si + 1, si - 1);
+        arrive(F32 ? si + 1 : si + 2);
         if constexpr (F32) {
+          refill(si - 1);
           logits(k_tile(si + 1), to);
           weights(from, pk);
           values(v_tile(si), from, pk);
           refer(to);
         } else {
-          step_bf16(k_tile(si + 1), v_tile(si), from, to);
+          step_bf16(k_tile(si + 1), v_tile(si), k_tile(si + 2), from, to, [&] { refill(si - 1); });
         }
         ++si;
       };
@@ -588,7 +632,8 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
     }
   } else {
     for (; si < n_plain; ++si) {
-      arrive(si, si - 1);
+      arrive(si);
+      refill(si - 1);
       f32x16 s[TB];
       unsigned pk[SN / 2];
       logits(k_tile(si), s);
@@ -599,7 +644,8 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   }
   // ---- the others ----
   for (; si < n_stage; ++si) {
-    arrive(si, si - 1);
+    arrive(si);
+    refill(si - 1);
     f32x16 s[TB];
     unsigned pk[SN / 2];
     logits(k_tile(si), s);
