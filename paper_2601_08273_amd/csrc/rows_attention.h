@@ -82,7 +82,7 @@ struct RowsSmem {
   static constexpr int kStage = 2 * kTileBytes;
   static constexpr int kMerge = (TG - 1) * RB * (D / 2) * 256;             // accumulators of the waves that are not the first group's
   static constexpr int kRing = NST * kStage > kMerge ? NST * kStage : kMerge;
-  static constexpr int total() { return kRing + 2 * TG * RB * 32 * 4; }
+  static constexpr int total() { return kRing + 2 * TG * RB * 32 * 4 + 16; }
 };
 
 // The block's (sequence, row tile).  Prompts: tiles in descending order of the tokens that they see, so that the longest start first:
@@ -218,6 +218,8 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   unsigned char* ring = smem;
   float* stat_m = (float*)(smem + SM::kRing);               // [TG][ROWS]
   float* stat_l = stat_m + TG * ROWS;
+  int* odd_stage = (int*)(stat_l + TG * ROWS);              // the last edge stage whose V has infinities or NaN, from 1
+  if (threadIdx.x == 0) *odd_stage = 0;                     // (before the barriers of the stages)
   const unsigned ring_addr = (unsigned)(uintptr_t)ring;
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -273,7 +275,10 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   for (int u = 0; u < TR; ++u)
     lane_off[u] = (u * RPT + ld_row) * row_bytes + ((ld_pc ^ Tile::swizzle(first_row + u * RPT + ld_row)) * 16);
   const int page_mask = PAGED ? (1 << p.page_shift) - 1 : 0;
-  const int32_t* table = PAGED ? p.block_table + (long long)seq * p.max_pages : nullptr;
+  // (in the constant address space: read through the scalar cache whatever assembly stands between.  As vector loads they wait for every
+  // transfer that is under way: pieces over 37K pages 1747 us instead of 1487.)
+  typedef const int32_t __attribute__((address_space(4))) * ScalarTable;
+  const ScalarTable table = PAGED ? (ScalarTable)(uintptr_t)(p.block_table + (long long)seq * p.max_pages) : nullptr;
   // pages of the next stage to be fetched: asked for a stage ahead, through the scalar cache.  Rows of a run of 16 share a page, as
   // a page's size is a multiple of 16.
   int page[NPG];
@@ -289,21 +294,26 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   auto issue = [&](int si) {
     const unsigned dst = ring_addr + (si % NST) * SM::kStage + (fetch_v ? SM::kTileBytes : 0) + first_row * ROWB;
     const int n0 = (s_lo + si) * ST + first_row;
-    const bool whole = n0 + PER * RPT <= ext;
+    if (n0 + PER * RPT <= ext) {
 #pragma unroll
-    for (int i = 0; i < NPG; ++i) {
-      const int row0 = n0 + i * TR * RPT;
-      const long long pg = PAGED ? (long long)min(max(page[i], 0), p.n_pool_pages - 1) * p.page_stride : 0ll;
-      if (whole) {
+      for (int i = 0; i < NPG; ++i) {
+        const int row0 = n0 + i * TR * RPT;
+        const long long pg = PAGED ? (long long)min(max(page[i], 0), p.n_pool_pages - 1) * p.page_stride : 0ll;
         const long long at = pg + (long long)(PAGED ? row0 & page_mask : row0) * p.k_sn;
         dma16_runs<TR>((const char*)uniform64((long long)(base + at * ES)), lane_off, dst + i * TR * 1024);
-      } else {                                              // rows behind the last one repeat it
-#pragma unroll
-        for (int u = 0; u < TR; ++u) {
-          const int row = min(row0 + u * RPT + ld_row, cap);
-          const long long at = pg + (long long)(PAGED ? row & page_mask : row) * p.k_sn;
-          dma16(base + at * ES + ((ld_pc ^ Tile::swizzle(first_row + u * RPT + ld_row)) * 16), dst + (i * TR + u) * 1024);
+      }
+    } else {                                                // the sequence's last stage: rows behind its end repeat the last one
+#pragma unroll 1
+      for (int u = 0; u < PER; ++u) {
+        const int row = min(n0 + u * RPT + ld_row, cap);
+        long long at = 0;
+        if constexpr (PAGED) {
+          const int pg = table[min(n0 + u * RPT, cap) >> p.page_shift];
+          at = (long long)min(max(pg, 0), p.n_pool_pages - 1) * p.page_stride + (long long)(row & page_mask) * p.k_sn;
+        } else {
+          at = (long long)row * p.k_sn;
         }
+        dma16(base + at * ES + ((ld_pc ^ Tile::swizzle(first_row + u * RPT + ld_row)) * 16), dst + u * 1024);
       }
     }
   };
@@ -314,7 +324,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
     if (issued < n_stage) ask_pages(issued);
   };
   if (n_stage > 0) ask_pages(0);
-#pragma unroll
+#pragma unroll 1
   for (int i = 0; i < NST - 1; ++i) issue_next();
 
   // ---- the wave's query rows ----
@@ -427,9 +437,10 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
     return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   };
   auto token_of = [&](int e) { return e / 16 * 32 + e % 16 / 4 * 8 + 4 * h + e % 4; };
-  auto v_f32 = [&](unsigned Vt, int db, int e) {
-    const int t = token_of(e);
-    return *ROWS_LDS(const float, Vt + t * ROWB + (((8 * db + j / 4) ^ Tile::swizzle(t)) * 16) + (j & 3) * 4);
+  const unsigned v32_off = 4 * h * ROWB + (((j >> 2) ^ (h << 3)) * 16) + (j & 3) * 4;
+  auto v_f32 = [&](unsigned Vt, int db, int e) {            // (the swizzle of the token's row, apart from its part in v32_off, and 8 db pieces)
+    const unsigned flip = 128 * db + ((e % 16 / 4 & 1) << 6 | (e & 3) << 4);
+    return *(ROWS_LDS(const float, (Vt + v32_off) ^ flip) + (e / 16 * 32 + e % 16 / 4 * 8 + e % 4) * ROWB / 4);
   };
   // O^T += V^T P^T
   auto values = [&](unsigned Vt, const f32x16 (&s)[TB], const unsigned (&pk)[SN / 2]) {
@@ -449,37 +460,14 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
       }
     }
   };
-  // The same where some rows do not see some tokens, whose V may hold anything: 0 times an infinity or NaN would reach the rows that
-  // do not see it.  Such entries go as zeros; where there are any, each kind is counted for each row among the tokens that it sees.
-  auto values_at_edge = [&](unsigned Vt, const f32x16 (&s)[TB], const unsigned (&pk)[SN / 2], unsigned vis) {
-#pragma unroll
-    for (int db = 0; db < DB; ++db) {
-      bool odd = false;
-      if constexpr (F32) {
-#pragma unroll
-        for (int e = 0; e < SN; ++e) {
-          const float x = v_f32(Vt, db, e);
-          const bool bad = !(fabsf(x) < INFINITY);
-          odd |= bad;
-          acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(bad ? 0.f : x, s[e / 16][e % 16], acc[db], 0, 0, 0);
-        }
-      } else {
-#pragma unroll
-        for (int ks = 0; ks < SN / 8; ++ks) {
-          u32x4 x = v_bf16(Vt, db, ks);
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const bool b0 = (x[w] & 0x7f80u) == 0x7f80u, b1 = (x[w] & 0x7f800000u) == 0x7f800000u;
-            odd |= b0 || b1;
-            x[w] = (b0 ? 0u : x[w] & 0xffffu) | (b1 ? 0u : x[w] & 0xffff0000u);
-          }
-          const u32x4 pr = {pk[4 * ks], pk[4 * ks + 1], pk[4 * ks + 2], pk[4 * ks + 3]};
-          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, pr), acc[db], 0, 0, 0);
-        }
-      }
-      if (!__any(odd)) continue;
+  // The same where some rows do not see some tokens and V holds infinities or NaN: 0 times one of them would reach the rows that do not
+  // see it.  Such entries go as zeros, and each kind is counted for each row among the tokens that it sees.  Rare: written to be short.
+  auto values_odd = [&](unsigned Vt, const f32x16 (&s)[TB], const unsigned (&pk)[SN / 2], unsigned vis) {
 #pragma unroll 1
-      for (int w = 0; w < 3; ++w) {
+    for (int db = 0; db < DB; ++db) {
+      f32x16 sum;
+#pragma unroll 1
+      for (int kind = 0; kind < 4; ++kind) {                // the finite entries, inf, -inf, NaN
         f32x16 n;
 #pragma unroll
         for (int e = 0; e < 16; ++e) n[e] = 0.f;
@@ -487,40 +475,61 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
 #pragma unroll
           for (int e = 0; e < SN; ++e) {
             const float x = v_f32(Vt, db, e);
-            const bool is = w == 0 ? x == INFINITY : w == 1 ? x == -INFINITY : x != x;
-            n = __builtin_amdgcn_mfma_f32_32x32x2f32(is ? 1.f : 0.f, (vis >> e) & 1 ? 1.f : 0.f, n, 0, 0, 0);
+            const float a = kind == 0 ? (fabsf(x) < INFINITY ? x : 0.f)
+                                      : (kind == 1 ? x == INFINITY : kind == 2 ? x == -INFINITY : x != x) ? 1.f : 0.f;
+            n = __builtin_amdgcn_mfma_f32_32x32x2f32(a, kind == 0 ? s[e / 16][e % 16] : (vis >> e) & 1 ? 1.f : 0.f, n, 0, 0, 0);
           }
         } else {
 #pragma unroll
           for (int ks = 0; ks < SN / 8; ++ks) {
             const u32x4 x = v_bf16(Vt, db, ks);
-            u32x4 is, seen;
+            u32x4 a, w;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              unsigned both = 0;
+              a[i] = 0;
 #pragma unroll
               for (int y = 0; y < 2; ++y) {
-                const unsigned b = (x[i] >> (16 * y)) & 0xffffu;
-                const bool hit = w == 0 ? b == 0x7f80u : w == 1 ? b == 0xff80u : (b & 0x7fffu) > 0x7f80u;
-                both |= hit ? 0x3f80u << (16 * y) : 0u;
+                const unsigned v = (x[i] >> (16 * y)) & 0xffffu, one = 0x3f80u;
+                const bool finite = (v & 0x7f80u) != 0x7f80u;
+                const bool hit = kind == 1 ? v == 0x7f80u : kind == 2 ? v == 0xff80u : (v & 0x7fffu) > 0x7f80u;
+                a[i] |= (kind == 0 ? (finite ? v : 0u) : hit ? one : 0u) << (16 * y);
               }
-              is[i] = both;
-              seen[i] = ((vis >> (8 * ks + 2 * i)) & 1 ? 0x3f80u : 0u) | ((vis >> (8 * ks + 2 * i + 1)) & 1 ? 0x3f800000u : 0u);
+              const unsigned seen = ((vis >> (8 * ks + 2 * i)) & 1 ? 0x3f80u : 0u) | ((vis >> (8 * ks + 2 * i + 1)) & 1 ? 0x3f800000u : 0u);
+              w[i] = kind == 0 ? pk[4 * ks + i] : seen;
             }
-            n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, is), __builtin_bit_cast(bf16x8, seen), n, 0, 0, 0);
+            n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, w), n, 0, 0, 0);
           }
         }
-        const float add = w == 0 ? INFINITY : w == 1 ? -INFINITY : NAN;
+        const float add = kind == 1 ? INFINITY : kind == 2 ? -INFINITY : NAN;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[db][e] = n[e] > 0.f ? acc[db][e] + add : acc[db][e];
+        for (int e = 0; e < 16; ++e) sum[e] = kind == 0 ? n[e] : n[e] > 0.f ? sum[e] + add : sum[e];
       }
+#pragma unroll
+      for (int k = 0; k < DB; ++k)
+        if (k == db) acc[k] += sum;
     }
   };
-  // Stage si is in the LDS, and everyone is past stage `past`'s products: the places up to that one's are filled again.
+  // Whether stage si's V has infinities or NaN, for the whole block: every thread looks at its share.
+  auto any_odd = [&](int si) {
+    constexpr int SHARE = SM::kTileBytes / 16 / (WAVES * 64);
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < SHARE; ++i) {
+      const u32x4 x = *ROWS_LDS(const u32x4, ring_addr + (si % NST) * SM::kStage + SM::kTileBytes + (i * WAVES * 64 + tid) * 16);
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+        odd |= F32 ? (x[w] & 0x7f800000u) == 0x7f800000u : (x[w] & 0x7f80u) == 0x7f80u || (x[w] & 0x7f800000u) == 0x7f800000u;
+    }
+    if (odd) *odd_stage = si + 1;                           // (any number of threads, the same value)
+    __syncthreads();
+    return *(volatile int*)odd_stage == si + 1;
+  };
+  // Stage si is in the LDS.
   auto arrive = [&](int si) {
     WaitLadder<NST - 2>::template run<PER>(max(issued - 1 - si, 0));
     __syncthreads();
   };
+  // Everyone is past stage `past`'s products: the places up to that one's are filled again.
   auto refill = [&](int past) {
     while (issued < n_stage && issued <= past + NST) issue_next();
   };
@@ -646,6 +655,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   for (; si < n_stage; ++si) {
     arrive(si);
     refill(si - 1);
+    const bool odd = any_odd(si);
     f32x16 s[TB];
     unsigned pk[SN / 2];
     logits(k_tile(si), s);
@@ -666,7 +676,8 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
     }
     refer(s);
     weights(s, pk);
-    values_at_edge(v_tile(si), s, pk, vis);
+    if (odd) values_odd(v_tile(si), s, pk, vis);
+    else values(v_tile(si), s, pk);
   }
   wait_vmcnt<0>();                                          // no transfer may still be writing LDS past this point
 
@@ -759,12 +770,13 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   }
 }
 
-// Merge of the S blocks that shared a tile: a wave takes one (token, query head).
+// Merge of the S blocks that shared a tile: a wave takes one (token, query head), D / 4 lanes a split's 16-byte pieces, so that 256 / D
+// splits are read at once, four of them in a row under way.  (Few rows: a block a row puts them on as many compute units.)
 template <typename T, int D, bool TREE>
-__global__ __launch_bounds__(256) void rows_combine(RowsParams p) {
-  const int lane = threadIdx.x & 63;
-  const long long n = (long long)p.total_q * p.H, at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (at >= n) return;
+__global__ __launch_bounds__(64) void rows_combine(RowsParams p) {
+  constexpr int LPR = D / 4, GROUPS = 64 / LPR, PF = 4;
+  const int lane = threadIdx.x, g = lane / LPR, vec = lane % LPR;
+  const long long n = (long long)p.total_q * p.H, at = blockIdx.x;
   const int tok = (int)(at / p.H), head = (int)(at - (long long)tok * p.H);
   // rows of no sequence stay as they were
   if (!TREE && (tok < p.cu_q[0] || tok >= p.cu_q[p.n_seq])) return;
@@ -773,22 +785,43 @@ __global__ __launch_bounds__(256) void rows_combine(RowsParams p) {
     m = p.part_m[lane * n + at];
     l = p.part_l[lane * n + at];
   }
+  const float* src = p.part_o + at * D + vec * 4;
+  auto piece = [&](int s) { return *(const f32x4*)(src + (long long)min(s, p.S - 1) * n * D); };
+  f32x4 ahead[PF];
+#pragma unroll
+  for (int u = 0; u < PF; ++u) ahead[u] = piece(g + u * GROUPS);
   const float mm = wave_max(m);
   const float w = m == -INFINITY ? 0.f : fast_exp2(m - mm);
   const float den = wave_sum(w * l);
-  constexpr int PER = D / 64;
-  float o[PER] = {};
-  for (int s = 0; s < p.S; ++s) {
-    const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s));
-    if (f == 0.f) continue;
-    const float* src = p.part_o + ((long long)s * n + at) * D + lane * PER;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < p.S; s0 += PF * GROUPS) {
+    f32x4 now[PF];
 #pragma unroll
-    for (int e = 0; e < PER; ++e) o[e] = fmaf(f, src[e], o[e]);
+    for (int u = 0; u < PF; ++u) {
+      now[u] = ahead[u];
+      ahead[u] = piece(s0 + (PF + u) * GROUPS + g);
+    }
+#pragma unroll
+    for (int u = 0; u < PF; ++u) {
+      const float f = __shfl(w, s0 + u * GROUPS + g);       // (0 behind the last split: its lane has no maximum)
+      if (s0 + u * GROUPS + g < p.S && f != 0.f) o += f * now[u];
+    }
   }
-  const float inv = den == 0.f ? 0.f : 1.f / den;
-  T* to = (T*)p.out + at * D + lane * PER;
 #pragma unroll
-  for (int e = 0; e < PER; ++e) Elem<T>::store(to + e, den == 0.f ? 0.f : o[e] * inv);
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (GROUPS == 4) {
+      auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(o[e]), __float_as_uint(o[e]), false, false);
+      o[e] = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+    }
+    auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(o[e]), __float_as_uint(o[e]), false, false);
+    o[e] = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+  }
+  if (g == 0) {
+    const float inv = den == 0.f ? 0.f : 1.f / den;
+    T* to = (T*)p.out + at * D + vec * 4;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) Elem<T>::store(to + e, den == 0.f ? 0.f : o[e] * inv);
+  }
   if (p.lse != nullptr && lane == 0) {
     const int i = TREE ? tok % p.nodes : tok;
     p.lse[TREE ? ((long long)(tok / p.nodes) * p.H + head) * p.nodes + i : (long long)head * p.total_q + tok] = (mm + __log2f(den)) * kLn2;
@@ -796,15 +829,14 @@ __global__ __launch_bounds__(256) void rows_combine(RowsParams p) {
 }
 
 // what a block of RB row blocks looks like: token groups, tokens of a wave in a stage, stages
-template <typename T, int D, int RB> struct RowsShape;
-template <int D> struct RowsShape<uint16_t, D, 8> { static constexpr int TG = 1, TW = 64, NST = 4; };
-template <int D> struct RowsShape<uint16_t, D, 4> { static constexpr int TG = 2, TW = 32, NST = 4; };
-template <int D> struct RowsShape<uint16_t, D, 2> { static constexpr int TG = 4, TW = 32, NST = 2; };
-template <int D> struct RowsShape<uint16_t, D, 1> { static constexpr int TG = 4, TW = 32, NST = 2; };
-template <int D> struct RowsShape<float, D, 8> { static constexpr int TG = 1, TW = 32, NST = 4; };
-template <int D> struct RowsShape<float, D, 4> { static constexpr int TG = 2, TW = 32, NST = 2; };
-template <int D> struct RowsShape<float, D, 2> { static constexpr int TG = 2, TW = 32, NST = 2; };
-template <int D> struct RowsShape<float, D, 1> { static constexpr int TG = 2, TW = 32, NST = 2; };
+template <typename T, int D, int RB>
+struct RowsShape {
+  static constexpr bool F32 = sizeof(T) == 4, WIDE = D * sizeof(T) > 256;      // WIDE: rows of 512 bytes
+  static constexpr int TG = RB == 8 ? 1 : RB == 4 || WIDE ? 2 : 4;
+  static constexpr int TW = RB == 8 && !F32 ? 64 : 32;
+  static constexpr int STAGE = 2 * TG * TW * D * (int)sizeof(T);
+  static constexpr int NST = 4 * STAGE <= 128 * 1024 ? 4 : 2;
+};
 
 template <typename T, int D, int RB, bool PAGED, bool TREE>
 static hipError_t launch_rows_rb(const RowsParams& p, hipStream_t st) {
@@ -827,7 +859,7 @@ static hipError_t launch_rows_d(const RowsParams& p, int rb, hipStream_t st) {
     default: e = launch_rows_rb<T, D, 1, PAGED, TREE>(p, st); break;
   }
   if (e != hipSuccess || p.S == 1) return e;
-  hipLaunchKernelGGL((rows_combine<T, D, TREE>), dim3((unsigned)(((long long)p.total_q * p.H + 3) / 4)), dim3(256), 0, st, p);
+  hipLaunchKernelGGL((rows_combine<T, D, TREE>), dim3((unsigned)((long long)p.total_q * p.H)), dim3(64), 0, st, p);
   return hipGetLastError();
 }
 
