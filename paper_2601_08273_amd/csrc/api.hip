@@ -404,7 +404,8 @@ int plan_prefill(const hippo_packed_desc* d, int total_q, int total_k, int n_seq
   // (block and thread numbers of the launches, and a merge's wave for every row of q and query head)
   if (rows > (1 << 30) || (long long)total_q * d->n_q_heads > (1 << 30) || total_k > 0x7fffff00) return HIPPO_ERR_BAD_SHAPE;
   int rb = 8;
-  while (rb > 1 && rows * d->n_kv_heads / (32 * rb) < 192) rb /= 2;
+  const int least = d->dtype == HIPPO_DTYPE_F32 && d->head_dim == 128 ? 2 : 1;
+  while (rb > least && rows * d->n_kv_heads / (32 * rb) < 192) rb /= 2;
   plan_rows(pl, d->dtype, d->head_dim, rows, n_seqs, total_k, d->n_kv_heads, d->n_q_heads, total_q, rb, num_splits);
   if ((long long)pl->n_tiles * d->n_kv_heads > (1 << 30) / 512) return HIPPO_ERR_BAD_SHAPE;
   return HIPPO_OK;
@@ -416,7 +417,8 @@ int plan_tree(const hippo_kv_desc* kv, int nodes, long long seq_len, int num_spl
   if (G > 4096) return HIPPO_ERR_BAD_SHAPE;
   const int R = G * nodes;
   int rb = 8;
-  while (rb > 1 && R <= 16 * rb) rb /= 2;
+  const int least = kv->dtype == HIPPO_DTYPE_F32 && kv->head_dim == 128 ? 2 : 1;
+  while (rb > least && R <= 16 * rb) rb /= 2;
   const int per_seq = (R + 32 * rb - 1) / (32 * rb);
   plan_rows(pl, kv->dtype, kv->head_dim, (long long)per_seq * 32 * rb * kv->batch, 0, seq_len, kv->n_kv_heads, kv->n_q_heads,
             (long long)kv->batch * nodes, rb, num_splits);

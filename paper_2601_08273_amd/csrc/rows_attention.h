@@ -80,7 +80,7 @@ template <typename T, int D, int RB, int TG, int TW, int NST>
 struct RowsSmem {
   static constexpr int kTileBytes = TG * TW * RowsTile<T, D>::kRowBytes;   // of a stage's K (or V)
   static constexpr int kStage = 2 * kTileBytes;
-  static constexpr int kMerge = (TG - 1) * RB * (D / 2) * 256;             // accumulators of the waves that are not the first group's
+  static constexpr int kMerge = TG == 1 ? 0 : TG * RB * (D / 2) * 256;     // the waves' accumulators
   static constexpr int kRing = NST * kStage > kMerge ? NST * kStage : kMerge;
   static constexpr int total() { return kRing + 2 * TG * RB * 32 * 4 + 16; }
 };
@@ -194,6 +194,9 @@ __device__ __forceinline__ void dma16_runs(const void* base, const unsigned* off
                    : "memory", "scc");
   }
 }
+// The kernel's parts are lambdas over its registers: one that stayed a function would keep them in memory.
+#define ROWS_INLINE __attribute__((always_inline))
+
 // The compiler cannot always tell that a value is the same in all lanes.
 __device__ __forceinline__ long long uniform64(long long x) {
   const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)x), hi = __builtin_amdgcn_readfirstlane((unsigned)((unsigned long long)x >> 32));
@@ -212,7 +215,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   constexpr int TR = PER / NPG;                             // transfers of a run
   constexpr int QN = CPR / 2;                               // 16-byte pieces of a query row in a lane
   constexpr int SN = TB * 16;                               // logits of a wave's stage in a lane
-  static_assert(2 * NLD % WAVES == 0 && NLD % PER == 0 && PER * (NST - 1) <= 63 && NST >= 2, "transfer split");
+  static_assert(2 * NLD % WAVES == 0 && NLD % PER == 0 && PER * NST <= 63 && NST >= 2, "transfer split");
 
   extern __shared__ __align__(16) unsigned char smem[];
   unsigned char* ring = smem;
@@ -257,8 +260,12 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   const int last = (min(tile * ROWS + ROWS, R) - 1) / p.G;  // of the tile's rows
   const int ext = TREE ? len_k : min(max(off + last + 1, 0), len_k);
   const int all_stages = (ext + ST - 1) / ST;
-  const int s_lo = (int)((long long)all_stages * split / p.S), s_hi = (int)((long long)all_stages * (split + 1) / p.S);
-  const int n_stage = s_hi - s_lo;
+  int s_lo = 0, n_stage = all_stages;
+  if (p.S > 1) {                                            // as evenly as possible, the first blocks taking one more
+    const int each = all_stages / p.S, more = all_stages - each * p.S;
+    s_lo = split * each + min(split, more);
+    n_stage = each + (split < more ? 1 : 0);
+  }
   // the first token that some row of the block does not see: the stages before it need no mask
   const int block_edge = TREE ? off : off + tile * ROWS / p.G + 1;
   const int n_plain = min(max(block_edge / ST - s_lo, 0), n_stage);
@@ -282,7 +289,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   // pages of the next stage to be fetched: asked for a stage ahead, through the scalar cache.  Rows of a run of 16 share a page, as
   // a page's size is a multiple of 16.
   int page[NPG];
-  auto ask_pages = [&](int si) {
+  auto ask_pages = [&](int si) ROWS_INLINE {
     if constexpr (PAGED) {
 #pragma unroll
       for (int i = 0; i < NPG; ++i) {
@@ -291,41 +298,41 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
       }
     }
   };
-  auto issue = [&](int si) {
+  auto issue = [&](int si) ROWS_INLINE {
     const unsigned dst = ring_addr + (si % NST) * SM::kStage + (fetch_v ? SM::kTileBytes : 0) + first_row * ROWB;
     const int n0 = (s_lo + si) * ST + first_row;
-    if (n0 + PER * RPT <= ext) {
+    const bool whole = n0 + PER * RPT <= ext;
 #pragma unroll
-      for (int i = 0; i < NPG; ++i) {
-        const int row0 = n0 + i * TR * RPT;
-        const long long pg = PAGED ? (long long)min(max(page[i], 0), p.n_pool_pages - 1) * p.page_stride : 0ll;
-        const long long at = pg + (long long)(PAGED ? row0 & page_mask : row0) * p.k_sn;
-        dma16_runs<TR>((const char*)uniform64((long long)(base + at * ES)), lane_off, dst + i * TR * 1024);
-      }
-    } else {                                                // the sequence's last stage: rows behind its end repeat the last one
-#pragma unroll 1
-      for (int u = 0; u < PER; ++u) {
-        const int row = min(n0 + u * RPT + ld_row, cap);
-        long long at = 0;
-        if constexpr (PAGED) {
-          const int pg = table[min(n0 + u * RPT, cap) >> p.page_shift];
-          at = (long long)min(max(pg, 0), p.n_pool_pages - 1) * p.page_stride + (long long)(row & page_mask) * p.k_sn;
-        } else {
-          at = (long long)row * p.k_sn;
-        }
-        dma16(base + at * ES + ((ld_pc ^ Tile::swizzle(first_row + u * RPT + ld_row)) * 16), dst + u * 1024);
+    for (int i = 0; i < NPG; ++i) {
+      const int row0 = min(n0 + i * TR * RPT, cap);
+      const long long pg = PAGED ? (long long)min(max(page[i], 0), p.n_pool_pages - 1) * p.page_stride : 0ll;
+      const long long at = pg + (long long)(PAGED ? row0 & page_mask : row0) * p.k_sn;
+      const char* from = (const char*)uniform64((long long)(base + at * ES));
+      if (whole) {
+        dma16_runs<TR>(from, lane_off, dst + i * TR * 1024);
+      } else {                                              // the sequence's last stage: rows behind its end repeat the last one
+        unsigned last_off[TR];
+#pragma unroll
+        for (int u = 0; u < TR; ++u)
+          last_off[u] = (min(n0 + (i * TR + u) * RPT + ld_row, cap) - row0) * row_bytes +
+                        ((ld_pc ^ Tile::swizzle(first_row + u * RPT + ld_row)) * 16);
+        dma16_runs<TR>(from, last_off, dst + i * TR * 1024);
       }
     }
   };
   int issued = 0;
-  auto issue_next = [&]() {
+  auto issue_next = [&]() ROWS_INLINE {
     if (issued >= n_stage) return;
     issue(issued++);
     if (issued < n_stage) ask_pages(issued);
   };
   if (n_stage > 0) ask_pages(0);
+  // Everyone is past stage `past`'s products: the places up to that one's are filled again.
+  auto refill = [&](int past) ROWS_INLINE {
 #pragma unroll 1
-  for (int i = 0; i < NST - 1; ++i) issue_next();
+    while (issued < n_stage && issued <= past + NST) issue_next();
+  };
+  refill(-1);
 
   // ---- the wave's query rows ----
   const int row = tile * ROWS + rb * 32 + j;
@@ -359,12 +366,12 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   const unsigned v_off = v_row * ROWB + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ Tile::swizzle(v_row)) * 16) + (lane & 1) * 8;
 
   // LDS addresses of a stage's tiles (numbers: constants that are added to them become the reads' immediate offsets)
-  auto k_tile = [&](int si) { return ring_addr + (si % NST) * SM::kStage + tg * TW * ROWB; };
-  auto v_tile = [&](int si) { return ring_addr + (si % NST) * SM::kStage + SM::kTileBytes + tg * TW * ROWB; };
+  auto k_tile = [&](int si) ROWS_INLINE { return ring_addr + (si % NST) * SM::kStage + tg * TW * ROWB; };
+  auto v_tile = [&](int si) ROWS_INLINE { return ring_addr + (si % NST) * SM::kStage + SM::kTileBytes + tg * TW * ROWB; };
 #define ROWS_LDS(type, address) ((__attribute__((address_space(3))) type*)(uintptr_t)(address))
 
   // S^T = K Q^T
-  auto logits = [&](unsigned Kt, f32x16 (&s)[TB]) {
+  auto logits = [&](unsigned Kt, f32x16 (&s)[TB]) ROWS_INLINE {
 #pragma unroll
     for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
@@ -385,7 +392,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   };
   // The rows' reference moves only when a maximum exceeds it by 2^8: weights stay below that, and rescaling is rare.  mx: of the tokens
   // in this half of the wave, unscaled
-  auto refer_to = [&](float mx, auto at_last) {
+  auto refer_to = [&](float mx, auto at_last) ROWS_INLINE {
     auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
     mx = max_nan(__uint_as_float(x[0]), __uint_as_float(x[1])) * p.scale_log2;
     const bool up = mx > m_run + 8.f;                       // also true of the first finite maximum
@@ -401,15 +408,15 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
         for (int e = 0; e < 16; ++e) acc[db][e] *= a;
     }
   };
-  auto refer = [&](const f32x16 (&s)[TB]) {
+  auto refer = [&](const f32x16 (&s)[TB]) ROWS_INLINE {
     float sv[SN];
 #pragma unroll
     for (int e = 0; e < SN; ++e) sv[e] = s[e / 16][e % 16];
-    refer_to(max_nan_of(sv), [] {});
+    refer_to(max_nan_of(sv), []() ROWS_INLINE {});
   };
   // Logits become weights: fp32 in place, for bf16 pairs in pk.  For the matrix unit P is rounded to bf16, and the denominator sums the
   // same rounded values: a token that has nearly all the weight keeps its row of V.
-  auto weights = [&](f32x16 (&s)[TB], unsigned (&pk)[SN / 2]) {
+  auto weights = [&](f32x16 (&s)[TB], unsigned (&pk)[SN / 2]) ROWS_INLINE {
     const float neg_m = m_run == -INFINITY ? 0.f : -m_run;
     if constexpr (F32) {
 #pragma unroll
@@ -431,19 +438,19 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   };
   // V^T's operand of d block db: bf16 16 tokens (two transposing reads, eight rows apart: the rows' swizzle differs in one bit), fp32
   // channel j and the token that register e holds in this half
-  auto v_bf16 = [&](unsigned Vt, int db, int ks) {
+  auto v_bf16 = [&](unsigned Vt, int db, int ks) ROWS_INLINE {
     const rows_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(ROWS_LDS(rows_s16x4, (Vt + v_off) ^ (64 * db)) + 16 * ks * ROWB / 8);
     const rows_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(ROWS_LDS(rows_s16x4, (Vt + v_off) ^ (64 * db + 32)) + (16 * ks + 8) * ROWB / 8);
     return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   };
-  auto token_of = [&](int e) { return e / 16 * 32 + e % 16 / 4 * 8 + 4 * h + e % 4; };
+  auto token_of = [&](int e) ROWS_INLINE { return e / 16 * 32 + e % 16 / 4 * 8 + 4 * h + e % 4; };
   const unsigned v32_off = 4 * h * ROWB + (((j >> 2) ^ (h << 3)) * 16) + (j & 3) * 4;
-  auto v_f32 = [&](unsigned Vt, int db, int e) {            // (the swizzle of the token's row, apart from its part in v32_off, and 8 db pieces)
+  auto v_f32 = [&](unsigned Vt, int db, int e) ROWS_INLINE {            // (the swizzle of the token's row, apart from its part in v32_off, and 8 db pieces)
     const unsigned flip = 128 * db + ((e % 16 / 4 & 1) << 6 | (e & 3) << 4);
     return *(ROWS_LDS(const float, (Vt + v32_off) ^ flip) + (e / 16 * 32 + e % 16 / 4 * 8 + e % 4) * ROWB / 4);
   };
   // O^T += V^T P^T
-  auto values = [&](unsigned Vt, const f32x16 (&s)[TB], const unsigned (&pk)[SN / 2]) {
+  auto values = [&](unsigned Vt, const f32x16 (&s)[TB], const unsigned (&pk)[SN / 2]) ROWS_INLINE {
     if constexpr (F32) {
 #pragma unroll
       for (int e = 0; e < SN; ++e)
@@ -462,7 +469,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   };
   // The same where some rows do not see some tokens and V holds infinities or NaN: 0 times one of them would reach the rows that do not
   // see it.  Such entries go as zeros, and each kind is counted for each row among the tokens that it sees.  Rare: written to be short.
-  auto values_odd = [&](unsigned Vt, const f32x16 (&s)[TB], const unsigned (&pk)[SN / 2], unsigned vis) {
+  auto values_odd = [&](unsigned Vt, const f32x16 (&s)[TB], const unsigned (&pk)[SN / 2], unsigned vis) ROWS_INLINE {
 #pragma unroll 1
     for (int db = 0; db < DB; ++db) {
       f32x16 sum;
@@ -506,11 +513,13 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
       }
 #pragma unroll
       for (int k = 0; k < DB; ++k)
-        if (k == db) acc[k] += sum;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[k][e] = k == db ? acc[k][e] + sum[e] : acc[k][e];
     }
   };
-  // Whether stage si's V has infinities or NaN, for the whole block: every thread looks at its share.
-  auto any_odd = [&](int si) {
+  // Whether stage si's V has infinities or NaN, for the whole block: every thread looks at its share, and says so before the barrier
+  // behind which everyone asks.
+  auto look_for_odd = [&](int si) ROWS_INLINE {
     constexpr int SHARE = SM::kTileBytes / 16 / (WAVES * 64);
     bool odd = false;
 #pragma unroll
@@ -521,17 +530,11 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
         odd |= F32 ? (x[w] & 0x7f800000u) == 0x7f800000u : (x[w] & 0x7f80u) == 0x7f80u || (x[w] & 0x7f800000u) == 0x7f800000u;
     }
     if (odd) *odd_stage = si + 1;                           // (any number of threads, the same value)
-    __syncthreads();
-    return *(volatile int*)odd_stage == si + 1;
   };
   // Stage si is in the LDS.
-  auto arrive = [&](int si) {
-    WaitLadder<NST - 2>::template run<PER>(max(issued - 1 - si, 0));
+  auto arrive = [&](int si) ROWS_INLINE {
+    WaitLadder<NST - 1>::template run<PER>(max(issued - 1 - si, 0));
     __syncthreads();
-  };
-  // Everyone is past stage `past`'s products: the places up to that one's are filled again.
-  auto refill = [&](int past) {
-    while (issued < n_stage && issued <= past + NST) issue_next();
   };
 
   // One step of the loop below, bf16: the next stage's logits (t), this stage's weights (from s) and their products with V, and the
@@ -541,10 +544,10 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   // the two runs of products: 16640 x 28 heads x 128 2071 us, like this 1771.)
   constexpr int AHEAD = 4;
   u32x4 ops[AHEAD];
-  auto k_read = [&](unsigned Kt, int i) {
+  auto k_read = [&](unsigned Kt, int i) ROWS_INLINE {
     return __builtin_bit_cast(u32x4, *(ROWS_LDS(const bf16x8, (Kt + k_off) ^ (32 * (i / TB))) + i % TB * 32 * ROWB / 16));
   };
-  auto step_bf16 = [&](unsigned Kt, unsigned Vt, unsigned Kt_behind, const f32x16 (&s)[TB], f32x16 (&t)[TB], auto fetch) {
+  auto step_bf16 = [&](unsigned Kt, unsigned Vt, unsigned Kt_behind, const f32x16 (&s)[TB], f32x16 (&t)[TB], auto fetch) ROWS_INLINE {
     constexpr int NK = TB * QN, NV = DB * SN / 8, NP = SN / 2, SPAN = NK + (SN / 8 - 1) * DB, MAX = SN / NV;
     unsigned pk[NP];
     const float neg_m = m_run == -INFINITY ? 0.f : -m_run;
@@ -553,7 +556,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
     for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
       for (int e = 0; e < 16; ++e) t[tb][e] = 0.f;
-    auto pairs = [&](int slot) {                            // the weights that belong into this slot
+    auto pairs = [&](int slot) ROWS_INLINE {                            // the weights that belong into this slot
 #pragma unroll
       for (int x = 0; x < NP; ++x)
         if (x * SPAN / NP == slot) {
@@ -574,7 +577,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
       if (i == 0) fetch();
     }
     float mx = t[0][0];
-    auto product = [&](int i) {
+    auto product = [&](int i) ROWS_INLINE {
       const int ks = i / DB;
       const u32x4 pr = {pk[4 * ks], pk[4 * ks + 1], pk[4 * ks + 2], pk[4 * ks + 3]};
       acc[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ops[(NK + i) % AHEAD]), __builtin_bit_cast(bf16x8, pr),
@@ -591,7 +594,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
     };
 #pragma unroll
     for (int i = 0; i <= NV / 2; ++i) product(i);
-    refer_to(mx, [&] {
+    refer_to(mx, [&]() ROWS_INLINE {
 #pragma unroll
       for (int i = NV / 2 + 1; i < NV; ++i) product(i);
     });
@@ -611,7 +614,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) ops[i] = k_read(k_tile(1), i);   // (of a stage that may not exist: then not used)
       }
-      auto step = [&](f32x16 (&from)[TB], f32x16 (&to)[TB]) {
+      auto step = [&](f32x16 (&from)[TB], f32x16 (&to)[TB]) ROWS_INLINE {
         arrive(F32 ? si + 1 : si + 2);
         if constexpr (F32) {
           refill(si - 1);
@@ -620,7 +623,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
           values(v_tile(si), from, pk);
           refer(to);
         } else {
-          step_bf16(k_tile(si + 1), v_tile(si), k_tile(si + 2), from, to, [&] { refill(si - 1); });
+          step_bf16(k_tile(si + 1), v_tile(si), k_tile(si + 2), from, to, [&]() ROWS_INLINE { refill(si - 1); });
         }
         ++si;
       };
@@ -655,10 +658,10 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   for (; si < n_stage; ++si) {
     arrive(si);
     refill(si - 1);
-    const bool odd = any_odd(si);
     f32x16 s[TB];
     unsigned pk[SN / 2];
     logits(k_tile(si), s);
+    look_for_odd(si);
     const int n0 = (s_lo + si) * ST + tg * TW;
     unsigned vis = 0;
 #pragma unroll
@@ -676,7 +679,8 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
     }
     refer(s);
     weights(s, pk);
-    if (odd) values_odd(v_tile(si), s, pk, vis);
+    __syncthreads();
+    if (__builtin_expect(*(volatile int*)odd_stage == si + 1, 0)) values_odd(v_tile(si), s, pk, vis);
     else values(v_tile(si), s, pk);
   }
   wait_vmcnt<0>();                                          // no transfer may still be writing LDS past this point
@@ -686,43 +690,45 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
     auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run), false, false);
     l_run = __uint_as_float(x[0]) + __uint_as_float(x[1]);
   }
+  // A wave writes out NI of the row's DB * 4 groups of four channels: of several token groups each takes its part of every row
+  constexpr int NI = DB * 4 / TG;
+  f32x4 o[NI];
+  const int i0 = tg * NI;
   if constexpr (TG > 1) {
     if (h == 0) {
       stat_m[tg * ROWS + rb * 32 + j] = m_run;
       stat_l[tg * ROWS + rb * 32 + j] = l_run;
     }
     __syncthreads();                                        // everyone is done reading the ring
-    f32x4* xbuf = (f32x4*)ring;                             // [TG - 1][RB][DB * 4][64]
-    if (tg > 0) {
+    f32x4* xbuf = (f32x4*)ring;                             // [TG][RB][DB * 4][64]
 #pragma unroll
-      for (int i = 0; i < DB * 4; ++i)
-        xbuf[(((tg - 1) * RB + rb) * DB * 4 + i) * 64 + lane] =
-            (f32x4){acc[i / 4][4 * (i % 4)], acc[i / 4][4 * (i % 4) + 1], acc[i / 4][4 * (i % 4) + 2], acc[i / 4][4 * (i % 4) + 3]};
-    }
+    for (int i = 0; i < DB * 4; ++i)
+      xbuf[((tg * RB + rb) * DB * 4 + i) * 64 + lane] =
+          (f32x4){acc[i / 4][4 * (i % 4)], acc[i / 4][4 * (i % 4) + 1], acc[i / 4][4 * (i % 4) + 2], acc[i / 4][4 * (i % 4) + 3]};
     __syncthreads();
-    if (tg > 0) return;
-    float mm = m_run;
+    float f[TG], mm = -INFINITY;
 #pragma unroll
-    for (int w = 1; w < TG; ++w) mm = max_nan(mm, stat_m[w * ROWS + rb * 32 + j]);
-    float f = m_run == -INFINITY ? 0.f : fast_exp2(m_run - mm);
-    l_run *= f;
+    for (int w = 0; w < TG; ++w) {
+      f[w] = stat_m[w * ROWS + rb * 32 + j];
+      mm = max_nan(mm, f[w]);
+    }
+    l_run = 0.f;
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+    for (int w = 0; w < TG; ++w) {
+      f[w] = f[w] == -INFINITY ? 0.f : fast_exp2(f[w] - mm);
+      l_run = fmaf(f[w], stat_l[w * ROWS + rb * 32 + j], l_run);
+    }
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc[db][e] *= f;
+    for (int i = 0; i < NI; ++i) {
+      o[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 1; w < TG; ++w) {
-      const float mw = stat_m[w * ROWS + rb * 32 + j];
-      f = mw == -INFINITY ? 0.f : fast_exp2(mw - mm);
-      l_run = fmaf(f, stat_l[w * ROWS + rb * 32 + j], l_run);
-#pragma unroll
-      for (int i = 0; i < DB * 4; ++i) {
-        const f32x4 o = xbuf[(((w - 1) * RB + rb) * DB * 4 + i) * 64 + lane];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i / 4][4 * (i % 4) + e] = fmaf(f, o[e], acc[i / 4][4 * (i % 4) + e]);
-      }
+      for (int w = 0; w < TG; ++w) o[i] += f[w] * xbuf[((w * RB + rb) * DB * 4 + i0 + i) * 64 + lane];
     }
     m_run = mm;
+  } else {
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+      o[i] = (f32x4){acc[i / 4][4 * (i % 4)], acc[i / 4][4 * (i % 4) + 1], acc[i / 4][4 * (i % 4) + 2], acc[i / 4][4 * (i % 4) + 3]};
   }
   if (row >= R) return;
   const bool nothing = TREE ? sees == 0 : lim < 0;
@@ -733,38 +739,35 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   const long long at = (long long)(tok0 + qi) * p.H + head;
   if (p.S > 1) {
     const long long slot = (long long)split * p.total_q * p.H + at;
-    if (h == 0) {
+    if (h == 0 && tg == 0) {
       p.part_m[slot] = m_run;
       p.part_l[slot] = l_run;
     }
-    float* o = p.part_o + slot * D;
 #pragma unroll
-    for (int i = 0; i < DB * 4; ++i) {
-      f32x4 x;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = nothing ? 0.f : acc[i / 4][4 * (i % 4) + e];
-      *(f32x4*)(o + (i / 4) * 32 + (i % 4) * 8 + 4 * h) = x;
+    for (int i = 0; i < NI; ++i) {
+      f32x4 x = o[i];
+      if (nothing) x = (f32x4){0.f, 0.f, 0.f, 0.f};
+      *(f32x4*)(p.part_o + slot * D + (i0 + i) * 8 + 4 * h) = x;
     }
     return;
   }
   const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
-  T* o = (T*)p.out + at * D;
+  T* out = (T*)p.out + at * D + 4 * h;
 #pragma unroll
-  for (int i = 0; i < DB * 4; ++i) {
-    float x[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = l_run == 0.f ? 0.f : acc[i / 4][4 * (i % 4) + e] * inv;
-    T* to = o + (i / 4) * 32 + (i % 4) * 8 + 4 * h;
-    if constexpr (F32) *(f32x4*)to = (f32x4){x[0], x[1], x[2], x[3]};
-    else {
+  for (int i = 0; i < NI; ++i) {
+    f32x4 x = o[i] * inv;
+    if (l_run == 0.f) x = (f32x4){0.f, 0.f, 0.f, 0.f};
+    if constexpr (F32) {
+      *(f32x4*)(out + (i0 + i) * 8) = x;
+    } else {
       const rows_f32x2 a = {x[0], x[1]}, b = {x[2], x[3]};
       uint2 w;
       w.x = __builtin_bit_cast(unsigned, __builtin_convertvector(a, rows_bf16x2));
       w.y = __builtin_bit_cast(unsigned, __builtin_convertvector(b, rows_bf16x2));
-      *(uint2*)to = w;
+      *(uint2*)(out + (i0 + i) * 8) = w;
     }
   }
-  if (p.lse != nullptr && h == 0) {
+  if (p.lse != nullptr && h == 0 && tg == 0) {
     const long long to = TREE ? ((long long)seq * p.H + head) * p.nodes + qi : (long long)head * p.total_q + tok0 + qi;
     p.lse[to] = (m_run + __log2f(l_run)) * kLn2;
   }
@@ -832,7 +835,7 @@ __global__ __launch_bounds__(64) void rows_combine(RowsParams p) {
 template <typename T, int D, int RB>
 struct RowsShape {
   static constexpr bool F32 = sizeof(T) == 4, WIDE = D * sizeof(T) > 256;      // WIDE: rows of 512 bytes
-  static constexpr int TG = RB == 8 ? 1 : RB == 4 || WIDE ? 2 : 4;
+  static constexpr int TG = RB == 8 ? 1 : RB == 4 || WIDE ? 2 : RB == 2 && D == 128 ? 2 : 4;
   static constexpr int TW = RB == 8 && !F32 ? 64 : 32;
   static constexpr int STAGE = 2 * TG * TW * D * (int)sizeof(T);
   static constexpr int NST = 4 * STAGE <= 128 * 1024 ? 4 : 2;
@@ -856,7 +859,9 @@ static hipError_t launch_rows_d(const RowsParams& p, int rb, hipStream_t st) {
     case 8: e = launch_rows_rb<T, D, 8, PAGED, TREE>(p, st); break;
     case 4: e = launch_rows_rb<T, D, 4, PAGED, TREE>(p, st); break;
     case 2: e = launch_rows_rb<T, D, 2, PAGED, TREE>(p, st); break;
-    default: e = launch_rows_rb<T, D, 1, PAGED, TREE>(p, st); break;
+    case 1:
+      if constexpr (!RowsShape<T, D, 1>::WIDE) { e = launch_rows_rb<T, D, 1, PAGED, TREE>(p, st); break; }
+    default: return hipErrorInvalidValue;
   }
   if (e != hipSuccess || p.S == 1) return e;
   hipLaunchKernelGGL((rows_combine<T, D, TREE>), dim3((unsigned)((long long)p.total_q * p.H)), dim3(64), 0, st, p);
