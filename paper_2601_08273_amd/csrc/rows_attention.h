@@ -215,6 +215,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   constexpr int TR = PER / NPG;                             // transfers of a run
   constexpr int QN = CPR / 2;                               // 16-byte pieces of a query row in a lane
   constexpr int SN = TB * 16;                               // logits of a wave's stage in a lane
+  constexpr bool PIPE = !F32 && NST >= 4, LATE = PIPE && WAVES == 8;
   static_assert(2 * NLD % WAVES == 0 && NLD % PER == 0 && PER * NST <= 63 && NST >= 2, "transfer split");
 
   extern __shared__ __align__(16) unsigned char smem[];
@@ -298,19 +299,28 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
       }
     }
   };
+  const long long stage_bytes = (long long)ST * p.k_sn * ES;
+  const char* next = (const char*)uniform64((long long)(base + (long long)(s_lo * ST + first_row) * p.k_sn * ES));   // (of the next stage)
   auto issue = [&](int si) ROWS_INLINE {
     const unsigned dst = ring_addr + (si % NST) * SM::kStage + (fetch_v ? SM::kTileBytes : 0) + first_row * ROWB;
     const int n0 = (s_lo + si) * ST + first_row;
-    const bool whole = n0 + PER * RPT <= ext;
+    auto page_at = [&](int i, int row0) ROWS_INLINE {       // where a run of rows starts
+      return (const char*)uniform64((long long)(base + ((long long)min(max(page[i], 0), p.n_pool_pages - 1) * p.page_stride +
+                                                        (long long)(row0 & page_mask) * p.k_sn) * ES));
+    };
+    if (n0 + PER * RPT <= ext) {
 #pragma unroll
-    for (int i = 0; i < NPG; ++i) {
-      const int row0 = min(n0 + i * TR * RPT, cap);
-      const long long pg = PAGED ? (long long)min(max(page[i], 0), p.n_pool_pages - 1) * p.page_stride : 0ll;
-      const long long at = pg + (long long)(PAGED ? row0 & page_mask : row0) * p.k_sn;
-      const char* from = (const char*)uniform64((long long)(base + at * ES));
-      if (whole) {
+      for (int i = 0; i < NPG; ++i) {
+        const char* from = next + (long long)i * TR * RPT * row_bytes;
+        if constexpr (PAGED) from = page_at(i, n0 + i * TR * RPT);
         dma16_runs<TR>(from, lane_off, dst + i * TR * 1024);
-      } else {                                              // the sequence's last stage: rows behind its end repeat the last one
+      }
+    } else {                                                // the sequence's last stage: rows behind its end repeat the last one
+#pragma unroll
+      for (int i = 0; i < NPG; ++i) {
+        const int row0 = min(n0 + i * TR * RPT, cap);
+        const char* from = (const char*)uniform64((long long)(base + (long long)row0 * p.k_sn * ES));
+        if constexpr (PAGED) from = page_at(i, row0);
         unsigned last_off[TR];
 #pragma unroll
         for (int u = 0; u < TR; ++u)
@@ -319,6 +329,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
         dma16_runs<TR>(from, last_off, dst + i * TR * 1024);
       }
     }
+    next += stage_bytes;
   };
   int issued = 0;
   auto issue_next = [&]() ROWS_INLINE {
@@ -329,10 +340,10 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   if (n_stage > 0) ask_pages(0);
   // Everyone is past stage `past`'s products: the places up to that one's are filled again.
   auto refill = [&](int past) ROWS_INLINE {
-#pragma unroll 1
-    while (issued < n_stage && issued <= past + NST) issue_next();
+    if (issued < n_stage && issued <= past + NST) issue_next();
   };
-  refill(-1);
+#pragma unroll 1
+  for (int i = 0; i < NST; ++i) refill(-1);
 
   // ---- the wave's query rows ----
   const int row = tile * ROWS + rb * 32 + j;
@@ -533,7 +544,9 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   };
   // Stage si is in the LDS.
   auto arrive = [&](int si) ROWS_INLINE {
-    WaitLadder<NST - 1>::template run<PER>(max(issued - 1 - si, 0));
+    const int behind = issued - 1 - si;                     // stages asked for behind it
+    if (LATE && behind == 1) wait_vmcnt<PER>();
+    else WaitLadder<NST - 1>::template run<PER>(max(behind, 0));
     __syncthreads();
   };
 
@@ -547,7 +560,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   auto k_read = [&](unsigned Kt, int i) ROWS_INLINE {
     return __builtin_bit_cast(u32x4, *(ROWS_LDS(const bf16x8, (Kt + k_off) ^ (32 * (i / TB))) + i % TB * 32 * ROWB / 16));
   };
-  auto step_bf16 = [&](unsigned Kt, unsigned Vt, unsigned Kt_behind, const f32x16 (&s)[TB], f32x16 (&t)[TB], auto fetch) ROWS_INLINE {
+  auto step_bf16 = [&](unsigned Kt, unsigned Vt, unsigned Kt_behind, const f32x16 (&s)[TB], f32x16 (&t)[TB], auto fetch, auto between) ROWS_INLINE {
     constexpr int NK = TB * QN, NV = DB * SN / 8, NP = SN / 2, SPAN = NK + (SN / 8 - 1) * DB, MAX = SN / NV;
     unsigned pk[NP];
     const float neg_m = m_run == -INFINITY ? 0.f : -m_run;
@@ -565,6 +578,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
           const rows_bf16x2 r = __builtin_convertvector(w, rows_bf16x2);
           pk[x] = __builtin_bit_cast(unsigned, r);
           l_run = __builtin_amdgcn_fdot2_f32_bf16(r, ones, l_run, false);
+          asm volatile("" : "+v"(pk[x]), "+v"(l_run));      // here, and not where the weight is used
         }
     };
 #pragma unroll
@@ -574,8 +588,9 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
       ops[i % AHEAD] = next < NK ? k_read(Kt, next < NK ? next : 0) : v_bf16(Vt, (next - NK) % DB, (next - NK) / DB);
       pairs(i);
       __builtin_amdgcn_sched_barrier(0);
-      if (i == 0) fetch();
+      if (!LATE && i == 0) fetch();
     }
+    between();
     float mx = t[0][0];
     auto product = [&](int i) ROWS_INLINE {
       const int ks = i / DB;
@@ -585,6 +600,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
       const int next = i + AHEAD;
       ops[(NK + i) % AHEAD] = next < NV ? v_bf16(Vt, next % DB, next / DB) : k_read(Kt_behind, next - NV);
       pairs(NK + i);
+      if (LATE && i == 0) fetch();
       if (i >= 1 && i <= NV / 2) {
 #pragma unroll
         for (int x = (i - 1) * MAX; x < i * MAX; ++x)
@@ -602,28 +618,31 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
 
   // ---- the stages that every row sees whole ----
   int si = 0;
-  if constexpr (NST >= 3) {
-    // a stage's logits are formed while the one before becomes weights: two independent streams for the matrix and the vector unit
+  if constexpr (PIPE) {
+    // A stage's logits are formed while the one before becomes weights: independent streams for the matrix and the vector unit.
+    // Eight waves, two on a SIMD: those with V to fetch are half a step late, so that one of a SIMD's waves is at its logits
+    // (much for the vector unit) while the other is at its products with V (little).  Step i: logits of stage i + 1, barrier, products of
+    // stage i, barrier.  With the lateness K of stage i is free when the early waves begin step i and V of stage i - 1 when the late
+    // ones do; each asks for what goes there beside its products, and waits ahead of the barrier in the step's middle for the K of stage
+    // i + 2 (of which the step's end reads the first operands) or the V of stage i + 1.  (In step with each other the waves waited 950 of a
+    // step's 3600 cycles for one another.)
+    const bool late = LATE && fetch_v;
     if (n_plain > 0) {
       f32x16 s[TB];
-      unsigned pk[SN / 2];
-      arrive(F32 ? 0 : 1);
+      arrive(late ? 0 : 1);
       logits(k_tile(0), s);
       refer(s);
-      if constexpr (!F32) {
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) ops[i] = k_read(k_tile(1), i);   // (of a stage that may not exist: then not used)
-      }
+      for (int i = 0; i < AHEAD; ++i) ops[i] = k_read(k_tile(1), i);     // (of a stage that may not exist: then not used)
+      if (late) __syncthreads();
       auto step = [&](f32x16 (&from)[TB], f32x16 (&to)[TB]) ROWS_INLINE {
-        arrive(F32 ? si + 1 : si + 2);
-        if constexpr (F32) {
-          refill(si - 1);
-          logits(k_tile(si + 1), to);
-          weights(from, pk);
-          values(v_tile(si), from, pk);
-          refer(to);
+        if constexpr (LATE) {
+          step_bf16(k_tile(si + 1), v_tile(si), k_tile(si + 2), from, to, [&]() ROWS_INLINE { refill(late ? si - 1 : si); },
+                    [&]() ROWS_INLINE { arrive(late ? si + 1 : si + 2); });
+          __syncthreads();
         } else {
-          step_bf16(k_tile(si + 1), v_tile(si), k_tile(si + 2), from, to, [&]() ROWS_INLINE { refill(si - 1); });
+          arrive(si + 2);
+          step_bf16(k_tile(si + 1), v_tile(si), k_tile(si + 2), from, to, [&]() ROWS_INLINE { refill(si - 1); }, []() ROWS_INLINE {});
         }
         ++si;
       };
@@ -638,6 +657,8 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
 #pragma unroll
         for (int tb = 0; tb < TB; ++tb) s[tb] = t[tb];
       }
+      if (LATE && !late) __syncthreads();
+      unsigned pk[SN / 2];
       weights(s, pk);
       values(v_tile(si), s, pk);
       ++si;
