@@ -166,7 +166,7 @@ def load():
     lib.hippo_token_logprobs.argtypes = [vp, i32, i64, vp, i32, i32, f32, i32, vp, vp, vp, vp, vp, sz, vp]
     lib.hippo_token_logprobs.restype = C.c_int
     pkp, pgp = C.POINTER(PackedDesc), C.POINTER(PagedKvDesc)
-    lib.hippo_prefill_workspace_bytes.argtypes = [pkp, i32, i32, i32, i32]
+    lib.hippo_prefill_workspace_bytes.argtypes = [pkp, i32, i32, i32, i32, i32]
     lib.hippo_tree_workspace_bytes.argtypes = [kvp, i32, i32, i32]
     lib.hippo_prefill_workspace_bytes.restype = lib.hippo_tree_workspace_bytes.restype = sz
     lib.hippo_prefill_attention.argtypes = [vp, i32, vp, vp, i32, pkp, vp, vp, i32, f32, i32, vp, vp, vp, sz, vp]

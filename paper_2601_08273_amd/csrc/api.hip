@@ -365,23 +365,52 @@ int plan_spec(int batch, int gamma, int vocab, int dtype, SpecPlan* pl) {
 // ---- attention of many rows: planning -------------------------------------------------------------
 constexpr int kMaxRowSplits = 64;   // the merge keeps a split's statistics in a lane
 
-// rows: query rows of a KV head, over all sequences; ragged: sequences that may leave a tile each; seen: tokens that the longest may
-// see; tokens: rows of q
-void plan_rows(RowsPlan* pl, int dtype, int head_dim, long long rows, int ragged, long long seen, int Hkv, int H, long long tokens,
-               int rb, int num_splits) {
-  pl->rb = rb;
-  pl->n_tiles = (int)(rows / (32 * rb) + ragged);
-  const long long blocks = std::max<long long>(1, (rows + 32 * rb - 1) / (32 * rb)) * Hkv;
-  long long S = num_splits;
-  if (S == 0) S = std::min<long long>(kNumCU / blocks, seen / 512);
-  S = std::max<long long>(1, std::min<long long>(S, std::min<long long>(kMaxRowSplits, (seen + 63) / 64)));
-  if (tokens * H > (1 << 25)) S = 1;                          // (the merge's launch: 64 threads a row and head, below 2^32)
-  pl->S = (int)S;
-  const size_t slots = S > 1 ? (size_t)S * tokens * H : 0;
+// What a block of RB x 32 rows takes for 64 tokens, in us, measured alone on its compute unit (64 nodes over 16640 rows of 28 heads x
+// 128, 32 over 33280 of 14 x 64; fp32 64 over 16640 of 28 x 128, 16 over 2000 of 14 x 64).
+double rows_pace(int dtype, int head_dim, int rb) {
+  static const double pace[2][2][4] = {{{1.45, 2.3, 4.4, 8.2}, {0, 4.8, 8.2, 16.0}}, {{0.375, 0.33, 0.65, 1.01}, {0.61, 0.80, 0.79, 1.40}}};
+  return pace[dtype == HIPPO_DTYPE_BF16][head_dim == 128][rb == 1 ? 0 : rb == 2 ? 1 : rb == 4 ? 2 : 3];
+}
+
+// How to cut a call: the rows of a block and the blocks that share a tile's tokens, by the time that they are going to take.
+//   a block: kBlockUs besides its tokens (its start and its end), one on a compute unit at a time
+//   a call:  the longest block of all, or all blocks on all compute units; kLaunchUs
+//   blocks that share tiles: a merge, kMergeUs and kMergeMbUs for a megabyte of parts
+// rows: query rows of a KV head of one sequence, on average; seen: the tokens that the last of them sees, seen_mean: that all do; whole:
+// every block takes as many tokens as any other (trees); num_splits: the caller's.
+constexpr double kBlockUs = 4.0, kLaunchUs = 2.5, kMergeUs = 4.0, kMergeMbUs = 0.9;
+void cut_rows(RowsPlan* pl, int dtype, int head_dim, double rows, double n_seqs, double seen, double seen_mean, bool whole, int Hkv,
+              double part_bytes, int num_splits) {
+  static const int splits[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64};
+  double best = 1e30;
+  for (int rb = 8; rb >= 1; rb /= 2) {
+    const double pace = rows_pace(dtype, head_dim, rb);
+    if (pace == 0) continue;
+    const double tiles = n_seqs * (whole ? ceil(rows / (32 * rb)) : std::max(1.0, rows / (32 * rb) + 0.5)) * Hkv;
+    for (int S : splits) {
+      if (num_splits > 0 ? S != 1 : S > 1 && seen < 64.0 * S) break;
+      const double n = num_splits > 0 ? num_splits : S;
+      const double longest = kBlockUs + seen / 64 / n * pace, mean = kBlockUs + seen_mean / 64 / n * pace;
+      const double rounds = tiles * n / kNumCU;
+      const double t = std::max(longest, whole ? ceil(rounds) * longest : rounds * mean) +
+                       (n > 1 ? kMergeUs + kMergeMbUs * n * part_bytes * 1e-6 : 0.0);
+      if (t < best * 0.999) {
+        best = t;
+        pl->rb = rb;
+        pl->S = S;
+      }
+    }
+  }
+  if (num_splits > 0) pl->S = num_splits;
+  pl->S = (int)std::max(1.0, std::min<double>(std::min(pl->S, kMaxRowSplits), (seen + 63) / 64));
+}
+
+void carve_plan(RowsPlan* pl, int head_dim, long long tokens, int H) {
+  if (tokens * H > (1 << 25)) pl->S = 1;                      // (the merge's launch: 64 threads a row and head, below 2^32)
+  const size_t slots = pl->S > 1 ? (size_t)pl->S * tokens * H : 0;
   pl->off_m = align_up(slots * head_dim * sizeof(float), 256);
   pl->off_l = pl->off_m + align_up(slots * sizeof(float), 256);
   pl->bytes = std::max<size_t>(256, pl->off_l + align_up(slots * sizeof(float), 256));
-  (void)dtype;
 }
 
 int check_packed(const hippo_packed_desc* d) {
@@ -397,31 +426,41 @@ int check_packed(const hippo_packed_desc* d) {
 }
 
 // total_k: rows of packed K and V, or the most that a sequence's pages hold
-int plan_prefill(const hippo_packed_desc* d, int total_q, int total_k, int n_seqs, int num_splits, RowsPlan* pl) {
+int plan_prefill(const hippo_packed_desc* d, bool paged, int total_q, int total_k, int n_seqs, int num_splits, RowsPlan* pl) {
   if (total_q < 0 || total_k < 0 || n_seqs < 1 || n_seqs > 65535 || num_splits < 0) return HIPPO_ERR_BAD_SHAPE;
   const int G = d->n_q_heads / d->n_kv_heads;
   const long long rows = (long long)total_q * G;
   // (block and thread numbers of the launches, and a merge's wave for every row of q and query head)
   if (rows > (1 << 30) || (long long)total_q * d->n_q_heads > (1 << 30) || total_k > 0x7fffff00) return HIPPO_ERR_BAD_SHAPE;
-  int rb = 8;
-  const int least = d->dtype == HIPPO_DTYPE_F32 && d->head_dim == 128 ? 2 : 1;
-  while (rb > least && rows * d->n_kv_heads / (32 * rb) < 192) rb /= 2;
-  plan_rows(pl, d->dtype, d->head_dim, rows, n_seqs, total_k, d->n_kv_heads, d->n_q_heads, total_q, rb, num_splits);
+  // (the lengths are on the device: taken as equal, each seeing what is there beside the others)
+  const double len_q = std::max(1.0, (double)total_q / n_seqs), seen = std::max(len_q, paged ? (double)total_k : (double)total_k / n_seqs);
+  cut_rows(pl, d->dtype, d->head_dim, len_q * G, std::min<double>(n_seqs, std::max(1, total_q)), seen, seen - len_q / 2, false,
+           d->n_kv_heads, (double)total_q * d->n_q_heads * d->head_dim * 4, num_splits);
+  pl->deal = 0;
+  pl->n_tiles = (int)(rows / (32 * pl->rb) + n_seqs);
+  carve_plan(pl, d->head_dim, total_q, d->n_q_heads);
   if ((long long)pl->n_tiles * d->n_kv_heads > (1 << 30) / 512) return HIPPO_ERR_BAD_SHAPE;
   return HIPPO_OK;
 }
 
-int plan_tree(const hippo_kv_desc* kv, int nodes, long long seq_len, int num_splits, RowsPlan* pl) {
+// by_length: the sequences have lengths of their own
+int plan_tree(const hippo_kv_desc* kv, int nodes, long long seq_len, bool by_length, int num_splits, RowsPlan* pl) {
   if (nodes < 1 || nodes > 64 || seq_len < nodes || seq_len > 0x7fffff00ll || num_splits < 0) return HIPPO_ERR_BAD_SHAPE;
   const int G = kv->n_q_heads / kv->n_kv_heads;
   if (G > 4096) return HIPPO_ERR_BAD_SHAPE;
-  const int R = G * nodes;
-  int rb = 8;
-  const int least = kv->dtype == HIPPO_DTYPE_F32 && kv->head_dim == 128 ? 2 : 1;
-  while (rb > least && R <= 16 * rb) rb /= 2;
-  const int per_seq = (R + 32 * rb - 1) / (32 * rb);
-  plan_rows(pl, kv->dtype, kv->head_dim, (long long)per_seq * 32 * rb * kv->batch, 0, seq_len, kv->n_kv_heads, kv->n_q_heads,
-            (long long)kv->batch * nodes, rb, num_splits);
+  const long long tokens = (long long)kv->batch * nodes;
+  cut_rows(pl, kv->dtype, kv->head_dim, G * nodes, kv->batch, (double)seq_len, (double)seq_len, true, kv->n_kv_heads,
+           (double)tokens * kv->n_q_heads * kv->head_dim * 4, num_splits);
+  const int per_seq = (G * nodes + 32 * pl->rb - 1) / (32 * pl->rb);
+  if ((long long)per_seq * kv->batch > (1 << 30)) return HIPPO_ERR_BAD_SHAPE;
+  pl->n_tiles = per_seq * kv->batch;
+  pl->deal = 0;
+  if (pl->S > 1 && by_length && kv->batch > 1 && kv->batch <= 64) {
+    pl->deal = pl->S * kv->batch;
+    pl->S = std::min(2 * pl->S, kMaxRowSplits);
+  }
+  carve_plan(pl, kv->head_dim, tokens, kv->n_q_heads);
+  if (pl->S == 1) pl->deal = 0;
   if ((long long)pl->n_tiles * kv->n_kv_heads > (1 << 30) / 512 || (long long)kv->batch * nodes * kv->n_q_heads > (1 << 30))
     return HIPPO_ERR_BAD_SHAPE;
   return HIPPO_OK;
@@ -448,6 +487,9 @@ bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0
 void carve_rows(RowsParams* p, const RowsPlan& pl, void* workspace) {
   p->S = pl.S;
   p->n_tiles = pl.n_tiles;
+  p->deal = pl.deal;
+  p->tiles_per_seq = std::max(1, pl.n_tiles / p->n_seq);
+  p->by_heads = rows_divisor(p->Hkv); p->by_group = rows_divisor(p->G); p->by_tiles = rows_divisor(p->tiles_per_seq);
   p->part_o = static_cast<float*>(workspace);
   p->part_m = reinterpret_cast<float*>(static_cast<char*>(workspace) + pl.off_m);
   p->part_l = reinterpret_cast<float*>(static_cast<char*>(workspace) + pl.off_l);
@@ -1042,9 +1084,9 @@ int hippo_quantize_kv_e4m3(const void* k_src, const void* v_src, const hippo_kv_
 }
 
 size_t hippo_prefill_workspace_bytes(const hippo_packed_desc* desc, int32_t total_q, int32_t total_k, int32_t n_seqs,
-                                     int32_t num_splits) {
+                                     int32_t paged, int32_t num_splits) {
   RowsPlan pl;
-  if (check_packed(desc) != HIPPO_OK || plan_prefill(desc, total_q, total_k, n_seqs, num_splits, &pl) != HIPPO_OK) return 0;
+  if (check_packed(desc) != HIPPO_OK || plan_prefill(desc, paged != 0, total_q, total_k, n_seqs, num_splits, &pl) != HIPPO_OK) return 0;
   return pl.bytes;
 }
 
@@ -1056,7 +1098,7 @@ static int prefill_entry(const void* q, int32_t total_q, const void* k, const vo
   int rc = check_packed(desc);
   if (rc != HIPPO_OK) return rc;
   RowsPlan pl;
-  rc = plan_prefill(desc, total_q, total_k, n_seqs, num_splits, &pl);
+  rc = plan_prefill(desc, pd != nullptr, total_q, total_k, n_seqs, num_splits, &pl);
   if (rc != HIPPO_OK) return rc;
   if (total_q == 0) return HIPPO_OK;                          // no rows
   if (q == nullptr || cu_q == nullptr || cu_k == nullptr || out == nullptr || workspace == nullptr) return HIPPO_ERR_NULL_ARG;
@@ -1106,7 +1148,7 @@ int hippo_prefill_attention_paged(const void* q, int32_t total_q, int64_t q_stri
 
 size_t hippo_tree_workspace_bytes(const hippo_kv_desc* kv, int32_t n_nodes, int32_t seq_len, int32_t num_splits) {
   RowsPlan pl;
-  if (check_kv(kv) != HIPPO_OK || plan_tree(kv, n_nodes, seq_len, num_splits, &pl) != HIPPO_OK) return 0;
+  if (check_kv(kv) != HIPPO_OK || plan_tree(kv, n_nodes, seq_len, true, num_splits, &pl) != HIPPO_OK) return 0;
   return pl.bytes;
 }
 
@@ -1119,7 +1161,7 @@ static int tree_entry(const void* q, int32_t n_nodes, const void* k, const void*
   int rc = check_kv(kv);
   if (rc != HIPPO_OK) return rc;
   RowsPlan pl;
-  rc = plan_tree(kv, n_nodes, seq_len, num_splits, &pl);
+  rc = plan_tree(kv, n_nodes, seq_len, ctx_lens != nullptr, num_splits, &pl);
   if (rc != HIPPO_OK) return rc;
   if (parents_stride_b < 0) return HIPPO_ERR_BAD_SHAPE;
   if (ctx_lens == nullptr && (ctx_len < 0 || ctx_len > seq_len - n_nodes)) return HIPPO_ERR_BAD_SHAPE;

@@ -661,7 +661,7 @@ PyObject* prefill(PyObject* const* a) {
   const Tensor out = output(a[8], q.sizes(), q.scalar_type(), q);
   Tensor lse;
   if (truth(a[7])) lse = empty({q.size(1), q.size(0)}, at::kFloat, q);
-  const Tensor ws = workspace(a[9], q, [&] { return lib.hippo_prefill_workspace_bytes(&d, n_q, n_k, n_seqs, (int32_t)splits); });
+  const Tensor ws = workspace(a[9], q, [&] { return lib.hippo_prefill_workspace_bytes(&d, n_q, n_k, n_seqs, 0, (int32_t)splits); });
   require_here({&q, &k, &v, &cu_q, &cu_k, &out, &lse, &ws});
   check(unlocked(lib.hippo_prefill_attention, ptr<const void>(q), n_q, ptr<const void>(k), ptr<const void>(v), n_k, &d,
                  ptr<const int32_t>(cu_q), ptr<const int32_t>(cu_k), n_seqs, scale, (int32_t)splits, ptr(out), ptr<float>(lse), ptr(ws),
@@ -690,7 +690,7 @@ PyObject* prefill_paged(PyObject* const* a) {
   Tensor lse;
   if (truth(a[8])) lse = empty({q.size(1), q.size(0)}, at::kFloat, q);
   const long long room = std::min<long long>(table.size(1) * k.size(1), 0x7fffffff);
-  const Tensor ws = workspace(a[10], q, [&] { return lib.hippo_prefill_workspace_bytes(&d, n_q, (int32_t)room, (int32_t)B, (int32_t)splits); });
+  const Tensor ws = workspace(a[10], q, [&] { return lib.hippo_prefill_workspace_bytes(&d, n_q, (int32_t)room, (int32_t)B, 1, (int32_t)splits); });
   require_here({&q, &k, &v, &table, &cu_q, &lens, &out, &lse, &ws});
   check(unlocked(lib.hippo_prefill_attention_paged, ptr<const void>(q), n_q, sn, sh, ptr<const void>(k), ptr<const void>(v),
                  ptr<const int32_t>(table), &pd, ptr<const int32_t>(cu_q), ptr<const int32_t>(lens), scale, (int32_t)splits, ptr(out),

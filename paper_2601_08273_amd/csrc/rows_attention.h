@@ -22,6 +22,18 @@
 
 namespace hippo {
 
+// x / d for 0 <= x < 2^31 with one multiplication: 2^(31 + s) / d < m = floor(2^(31 + s) / d) + 1 < 2^32 for s = ceil(log2 d), and
+// x (m d - 2^(31 + s)) < 2^(31 + s), so that the fraction never reaches the next integer.
+struct RowsDivisor {
+  unsigned m, shift;
+  __device__ __forceinline__ int operator()(int x) const { return (int)((unsigned long long)(unsigned)x * m >> shift); }
+};
+inline RowsDivisor rows_divisor(int d) {
+  unsigned s = 0;
+  while ((1ll << s) < d) ++s;
+  return {(unsigned)((1ull << (31 + s)) / (unsigned)d + 1), 31 + s};
+}
+
 struct RowsParams {
   const void* q;
   const void* k;
@@ -43,16 +55,19 @@ struct RowsParams {
   int page_shift, max_pages, n_pool_pages;
   long long page_stride;
   float scale_log2;
-  int S;                        // blocks that share a tile's stages
+  RowsDivisor by_heads, by_group, by_tiles;   // by Hkv, G, tiles_per_seq
+  int tiles_per_seq;            // of trees
+  int S;                        // blocks that share a tile's stages (parts in the workspace)
+  int deal;                     // trees of 2 to 64 sequences: that many such blocks over all of them, by length; 0: S each
   int n_tiles;                  // row tiles of the launch
   float* part_o;                // [S, tokens * H, D] outputs before the division
   float* part_m;                // [S, tokens * H] maxima (log2), -inf: nothing seen
   float* part_l;
 };
 
-// how a call is cut: rows of a block (RB x 32), blocks that share a tile
+// how a call is cut: rows of a block (RB x 32), blocks that share a tile, see RowsParams
 struct RowsPlan {
-  int rb, S, n_tiles;
+  int rb, S, n_tiles, deal;
   size_t off_m, off_l, bytes;
 };
 
@@ -85,36 +100,49 @@ struct RowsSmem {
   static constexpr int total() { return kRing + 2 * TG * RB * 32 * 4 + 16; }
 };
 
+struct RowsTileAt {
+  int seq, tile;         // the sequence, its row tile
+  int tok0, len_q;       // its first row of q, their number
+  int row0_k, len_k;     // its first row of packed K and V, their number
+};
+
 // The block's (sequence, row tile).  Prompts: tiles in descending order of the tokens that they see, so that the longest start first:
 // tile k of a sequence has the level (rows before it) / (rows of a tile) + k, and block t takes the t-th tile from the highest level
 // down.  (A lane looks after a sequence; the level is found by bisection.  More than 64 sequences go in their own order, each
 // from its last tile.)  False: no such tile.
-template <int ROWS>
-__device__ __forceinline__ bool rows_find_tile(const RowsParams& p, int t, int* seq, int* tile) {
+template <int ROWS, bool PAGED>
+__device__ __forceinline__ bool rows_find_tile(const RowsParams& p, int t, RowsTileAt* at) {
   const int lane = threadIdx.x & 63;
-  auto tiles_of = [&](int b, int* base) {
-    if (b >= p.n_seq) { *base = 0; return 0; }
-    const int lo = min(max(p.cu_q[b], 0), p.total_q), hi = min(max(p.cu_q[b + 1], lo), p.total_q);
-    int len_k;
-    if (p.block_table != nullptr) len_k = min(max(p.kv_lens[b], 0), p.total_k);
-    else {
-      const int ko = min(max(p.cu_k[b], 0), p.total_k);
-      len_k = min(max(p.cu_k[b + 1], ko), p.total_k) - ko;
+  auto look = [&](int b, int* base) {                       // a sequence's numbers, into *at; its tiles
+    at->tok0 = min(max(p.cu_q[b], 0), p.total_q);
+    at->len_q = min(max(p.cu_q[b + 1], at->tok0), p.total_q) - at->tok0;
+    if constexpr (PAGED) {
+      at->row0_k = 0;
+      at->len_k = min(max(p.kv_lens[b], 0), p.total_k);
+    } else {
+      at->row0_k = min(max(p.cu_k[b], 0), p.total_k);
+      at->len_k = min(max(p.cu_k[b + 1], at->row0_k), p.total_k) - at->row0_k;
     }
-    *base = (int)min((long long)max(len_k - (hi - lo), 0) * p.G / ROWS, (long long)(1 << 29));
-    return (int)(((long long)(hi - lo) * p.G + ROWS - 1) / ROWS);
+    *base = (int)min((long long)max(at->len_k - at->len_q, 0) * p.G / ROWS, (long long)(1 << 29));
+    return (at->len_q * p.G + ROWS - 1) / ROWS;             // (rows: below 2^30)
+  };
+  auto take = [&](int from) {                               // the numbers of the lane that looked after the sequence
+    at->tok0 = __builtin_amdgcn_readlane(at->tok0, from);
+    at->len_q = __builtin_amdgcn_readlane(at->len_q, from);
+    at->row0_k = __builtin_amdgcn_readlane(at->row0_k, from);
+    at->len_k = __builtin_amdgcn_readlane(at->len_k, from);
   };
   auto add = [](int a, int b) { return a + b; };
+  int base;
   if (p.n_seq == 1) {
-    int base;
-    const int n = tiles_of(0, &base);
-    *seq = 0;
-    *tile = n - 1 - t;
+    const int n = look(0, &base);
+    at->seq = 0;
+    at->tile = n - 1 - t;
     return t < n;
   }
   if (p.n_seq <= 64) {
-    int base;
-    const int n = tiles_of(lane, &base);
+    int n = look(min(lane, p.n_seq - 1), &base);
+    if (lane >= p.n_seq) n = base = 0;
     if (t >= wave_reduce_i32(n, add)) return false;
     // the largest level that more than t tiles reach
     int lo = 0, hi = wave_reduce_i32(base + n, [](int a, int b) { return max(a, b); });
@@ -127,20 +155,22 @@ __device__ __forceinline__ bool rows_find_tile(const RowsParams& p, int t, int* 
     unsigned long long here = __ballot(base <= lo && lo < base + n);
     for (int i = t - above; i > 0; --i) here &= here - 1;
     const int b = __ffsll((long long)here) - 1;
-    *seq = b;
-    *tile = lo - __builtin_amdgcn_readlane(base, b);
+    at->seq = b;
+    at->tile = lo - __builtin_amdgcn_readlane(base, b);
+    take(b);
     return true;
   }
   int before = 0;
   for (int b0 = 0; b0 < p.n_seq; b0 += 64) {
-    int base;
-    const int n = tiles_of(b0 + lane, &base);
+    int n = look(min(b0 + lane, p.n_seq - 1), &base);
+    if (b0 + lane >= p.n_seq) n = 0;
     const int incl = (int)wave_scan_incl((unsigned)n) + before;
     const unsigned long long past = __ballot(incl > t);
     if (past != 0) {
       const int l = __ffsll((long long)past) - 1;
-      *seq = b0 + l;
-      *tile = __builtin_amdgcn_readlane(incl, l) - 1 - t;     // the last one first
+      at->seq = b0 + l;
+      at->tile = __builtin_amdgcn_readlane(incl, l) - 1 - t;     // the last one first
+      take(l);
       return true;
     }
     before = __builtin_amdgcn_readlane(incl, 63);
@@ -150,9 +180,9 @@ __device__ __forceinline__ bool rows_find_tile(const RowsParams& p, int t, int* 
 
 // Which nodes a node sees: lane i gets node i's, itself among them; 0: the node is none (its parent is below -1 or not before it, or
 // an ancestor is none).  After round r the bits of 2^r ancestors are there.
-__device__ __forceinline__ unsigned long long tree_masks(const int32_t* parents, int nodes) {
+// `up`: the lane's parent, -2 behind the last node.
+__device__ __forceinline__ unsigned long long tree_masks(int up) {
   const int lane = threadIdx.x & 63;
-  int up = lane < nodes ? parents[lane] : -2;
   int none = up < -1 || up >= lane;
   unsigned lo = none ? 0u : lane < 32 ? 1u << lane : 0u, hi = none ? 0u : lane >= 32 ? 1u << (lane - 32) : 0u;
   if (none) up = -1;
@@ -203,6 +233,26 @@ __device__ __forceinline__ long long uniform64(long long x) {
   return (long long)((unsigned long long)hi << 32 | lo);
 }
 
+// Stages of a tree's sequence: what its blocks share out (counted alike by the merge).
+__device__ __forceinline__ int tree_rows(const RowsParams& p, int seq) {
+  const int ctx = p.kv_lens != nullptr ? p.kv_lens[seq] : p.ctx_len;
+  return min(max(ctx, 0), p.total_k - p.nodes) + p.nodes;
+}
+// Trees of sequences of different lengths: p.deal blocks over all of them, each sequence so many that none of its blocks has more rows
+// than c, the smallest of 64 lengths from (all rows) / deal up to three times that with which the blocks suffice (there is one: deal is
+// at least twice the sequences).  Lane b gets sequence b's, 0 behind the last.  37120, 16640, 33280 and 29001 rows, 64 nodes, 64 x 8
+// heads: 275 us with four blocks each, 261 like this.
+__device__ __forceinline__ int tree_deal(const RowsParams& p) {
+  const int lane = threadIdx.x & 63;
+  const float len = lane < p.n_seq ? (float)tree_rows(p, lane) : 0.f;
+  const float least = wave_sum(len) / (float)p.deal, mine = 1.f / (least * (1.f + (float)lane * (1.f / 32.f)));
+  float blocks = 0.f;
+  for (int b = 0; b < p.n_seq; ++b) blocks += ceilf(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(len), b)) * mine);
+  const unsigned long long enough = __ballot(blocks <= (float)p.deal) | 1ull << 63;
+  const float c = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), __ffsll((long long)enough) - 1));
+  return lane < p.n_seq ? min(max((int)ceilf(len * c), 1), p.S) : 0;
+}
+
 template <typename T, int D, int RB, int TG, int TW, int NST, bool PAGED, bool TREE>
 __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   using Tile = RowsTile<T, D>;
@@ -230,46 +280,58 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rb = wave % RB, tg = wave / RB;
   const int j = lane & 31, h = lane >> 5;
-  const int hk = blockIdx.x % p.Hkv, split = blockIdx.y;
+  const int tile_no = __builtin_amdgcn_readfirstlane(p.by_heads(blockIdx.x));
+  const int hk = blockIdx.x - tile_no * p.Hkv;
+  int split = blockIdx.y, n_split = p.S;
 
   // ---- the block's rows and the tokens that they may see ----
   int seq, tile, len_q, len_k, tok0;
   long long row0_k = 0;
   if constexpr (TREE) {
-    const int per_seq = p.n_tiles / p.n_seq;
-    seq = blockIdx.x / p.Hkv / per_seq;
-    tile = blockIdx.x / p.Hkv % per_seq;
+    if (p.deal > 0) {                                       // blocks of y: sequence after sequence
+      const int mine = tree_deal(p), incl = (int)wave_scan_incl((unsigned)mine);
+      const unsigned long long past = __ballot(incl > split);
+      if (past == 0) return;
+      seq = __builtin_amdgcn_readfirstlane(__ffsll((long long)past) - 1);
+      n_split = __builtin_amdgcn_readlane(mine, seq);
+      split -= __builtin_amdgcn_readlane(incl, seq) - n_split;
+      tile = tile_no;
+    } else {
+      seq = __builtin_amdgcn_readfirstlane(p.by_tiles(tile_no));
+      tile = tile_no - seq * p.tiles_per_seq;
+    }
     len_q = p.nodes;
     tok0 = seq * p.nodes;
-    const int ctx = p.kv_lens != nullptr ? p.kv_lens[seq] : p.ctx_len;
-    len_k = min(max(ctx, 0), p.total_k - p.nodes) + p.nodes;
+    len_k = __builtin_amdgcn_readfirstlane(tree_rows(p, seq));
   } else {
-    if (!rows_find_tile<ROWS>(p, blockIdx.x / p.Hkv, &seq, &tile)) return;
-    seq = __builtin_amdgcn_readfirstlane(seq);
-    tile = __builtin_amdgcn_readfirstlane(tile);
-    tok0 = min(max(p.cu_q[seq], 0), p.total_q);
-    len_q = min(max(p.cu_q[seq + 1], tok0), p.total_q) - tok0;
-    if constexpr (PAGED) len_k = min(max(p.kv_lens[seq], 0), p.total_k);
-    else {
-      const int lo = min(max(p.cu_k[seq], 0), p.total_k);
-      len_k = min(max(p.cu_k[seq + 1], lo), p.total_k) - lo;
-      row0_k = lo;
-    }
+    RowsTileAt at;
+    if (!rows_find_tile<ROWS, PAGED>(p, tile_no, &at)) return;
+    seq = __builtin_amdgcn_readfirstlane(at.seq);
+    tile = __builtin_amdgcn_readfirstlane(at.tile);
+    tok0 = __builtin_amdgcn_readfirstlane(at.tok0);
+    len_q = __builtin_amdgcn_readfirstlane(at.len_q);
+    len_k = __builtin_amdgcn_readfirstlane(at.len_k);
+    if constexpr (!PAGED) row0_k = __builtin_amdgcn_readfirstlane(at.row0_k);
   }
   const int off = len_k - len_q;                            // trees: the context's length
   const int R = len_q * p.G;
-  const int last = (min(tile * ROWS + ROWS, R) - 1) / p.G;  // of the tile's rows
+  const int last = __builtin_amdgcn_readfirstlane(p.by_group(min(tile * ROWS + ROWS, R) - 1));   // of the tile's rows
   const int ext = TREE ? len_k : min(max(off + last + 1, 0), len_k);
   const int all_stages = (ext + ST - 1) / ST;
   int s_lo = 0, n_stage = all_stages;
-  if (p.S > 1) {                                            // as evenly as possible, the first blocks taking one more
-    const int each = all_stages / p.S, more = all_stages - each * p.S;
+  if (n_split > 1) {                                        // as evenly as possible, the first blocks taking one more
+    const int each = all_stages / n_split, more = all_stages - each * n_split;
     s_lo = split * each + min(split, more);
     n_stage = each + (split < more ? 1 : 0);
   }
   // the first token that some row of the block does not see: the stages before it need no mask
-  const int block_edge = TREE ? off : off + tile * ROWS / p.G + 1;
+  const int block_edge = TREE ? off : __builtin_amdgcn_readfirstlane(off + p.by_group(tile * ROWS)) + 1;
   const int n_plain = min(max(block_edge / ST - s_lo, 0), n_stage);
+
+  int parent = -2;                                          // of node `lane`: on its way before the transfers, which it would wait for
+  if constexpr (TREE)
+    if (lane < p.nodes) parent = p.parents[seq * p.parents_sb + lane];
+  asm volatile("" : "+v"(parent));
 
   // ---- transfers: the first half of the waves fetches K, the other half V ----
   const bool fetch_v = wave >= WAVES / 2;
@@ -347,7 +409,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
 
   // ---- the wave's query rows ----
   const int row = tile * ROWS + rb * 32 + j;
-  const int qi = min(row, R - 1) / p.G, head = hk * p.G + min(row, R - 1) - qi * p.G;
+  const int qi = p.by_group(min(row, R - 1)), head = hk * p.G + min(row, R - 1) - qi * p.G;
   using QPiece = typename std::conditional<F32, f32x4, bf16x8>::type;
   QPiece qop[QN];
   {
@@ -357,7 +419,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   }
   unsigned long long sees = 0;                              // trees: the nodes that the lane's row sees
   if constexpr (TREE) {
-    const unsigned long long m = tree_masks(p.parents + seq * p.parents_sb, p.nodes);
+    const unsigned long long m = tree_masks(parent);
     sees = (unsigned long long)(unsigned)__shfl((int)(m >> 32), qi) << 32 | (unsigned)__shfl((int)(unsigned)m, qi);
   }
   const int lim = off + qi;                                 // prompts: the last token that the row sees
@@ -381,24 +443,32 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   auto v_tile = [&](int si) ROWS_INLINE { return ring_addr + (si % NST) * SM::kStage + SM::kTileBytes + tg * TW * ROWB; };
 #define ROWS_LDS(type, address) ((__attribute__((address_space(3))) type*)(uintptr_t)(address))
 
-  // S^T = K Q^T
+  // S^T = K Q^T.  (Operands are read several products ahead, here and below, and held to that order: the compiler reads one right before
+  // its product, and a wave that has a SIMD to itself waits for each.)
+  auto k_piece = [&](unsigned Kt, int i) ROWS_INLINE {      // product i: piece i / TB of token block i % TB
+    return *(ROWS_LDS(const u32x4, (Kt + k_off) ^ (32 * (i / TB))) + i % TB * 32 * ROWB / 16);
+  };
   auto logits = [&](unsigned Kt, f32x16 (&s)[TB]) ROWS_INLINE {
+    constexpr int N = TB * QN, AH = F32 ? 4 : 8;
+    u32x4 ahead[AH];
+#pragma unroll
+    for (int i = 0; i < AH && i < N; ++i) ahead[i] = k_piece(Kt, i);
 #pragma unroll
     for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[tb][e] = 0.f;
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int c = 0; c < QN; ++c) {
+    for (int i = 0; i < N; ++i) {
+      const QPiece kop = __builtin_bit_cast(QPiece, ahead[i % AH]);
+      if constexpr (F32) {
 #pragma unroll
-      for (int tb = 0; tb < TB; ++tb) {
-        const QPiece kop = *(ROWS_LDS(const QPiece, (Kt + k_off) ^ (32 * c)) + tb * 32 * ROWB / 16);
-        if constexpr (F32) {
-#pragma unroll
-          for (int x = 0; x < 4; ++x) s[tb] = __builtin_amdgcn_mfma_f32_32x32x2f32(kop[x], qop[c][x], s[tb], 0, 0, 0);
-        } else {
-          s[tb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop, qop[c], s[tb], 0, 0, 0);
-        }
+        for (int x = 0; x < 4; ++x) s[i % TB] = __builtin_amdgcn_mfma_f32_32x32x2f32(kop[x], qop[i / TB][x], s[i % TB], 0, 0, 0);
+      } else {
+        s[i % TB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop, qop[i / TB], s[i % TB], 0, 0, 0);
       }
+      if (i + AH < N) ahead[i % AH] = k_piece(Kt, i + AH < N ? i + AH : 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
   // The rows' reference moves only when a maximum exceeds it by 2^8: weights stay below that, and rescaling is rare.  mx: of the tokens
@@ -462,20 +532,27 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   };
   // O^T += V^T P^T
   auto values = [&](unsigned Vt, const f32x16 (&s)[TB], const unsigned (&pk)[SN / 2]) ROWS_INLINE {
-    if constexpr (F32) {
+    constexpr int N = DB * (F32 ? SN : SN / 8), AH = F32 ? 16 : 8;
+    typename std::conditional<F32, float, u32x4>::type ahead[AH];
+    auto read = [&](int i) ROWS_INLINE {                    // product i: d block i % DB
+      if constexpr (F32) return v_f32(Vt, i % DB, i / DB);
+      else return v_bf16(Vt, i % DB, i / DB);
+    };
 #pragma unroll
-      for (int e = 0; e < SN; ++e)
+    for (int i = 0; i < AH && i < N; ++i) ahead[i] = read(i);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int db = 0; db < DB; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v_f32(Vt, db, e), s[e / 16][e % 16], acc[db], 0, 0, 0);
-    } else {
-#pragma unroll
-      for (int ks = 0; ks < SN / 8; ++ks) {
+    for (int i = 0; i < N; ++i) {
+      if constexpr (F32) {
+        acc[i % DB] = __builtin_amdgcn_mfma_f32_32x32x2f32(ahead[i % AH], s[i / DB / 16][i / DB % 16], acc[i % DB], 0, 0, 0);
+      } else {
+        const int ks = i / DB;
         const u32x4 pr = {pk[4 * ks], pk[4 * ks + 1], pk[4 * ks + 2], pk[4 * ks + 3]};
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_bf16(Vt, db, ks)), __builtin_bit_cast(bf16x8, pr),
-                                                            acc[db], 0, 0, 0);
+        acc[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ahead[i % AH]), __builtin_bit_cast(bf16x8, pr),
+                                                              acc[i % DB], 0, 0, 0);
       }
+      if (i + AH < N) ahead[i % AH] = read(i + AH < N ? i + AH : 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
   // The same where some rows do not see some tokens and V holds infinities or NaN: 0 times one of them would reach the rows that do not
@@ -557,9 +634,6 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   // the two runs of products: 16640 x 28 heads x 128 2071 us, like this 1771.)
   constexpr int AHEAD = 4;
   u32x4 ops[AHEAD];
-  auto k_read = [&](unsigned Kt, int i) ROWS_INLINE {
-    return __builtin_bit_cast(u32x4, *(ROWS_LDS(const bf16x8, (Kt + k_off) ^ (32 * (i / TB))) + i % TB * 32 * ROWB / 16));
-  };
   auto step_bf16 = [&](unsigned Kt, unsigned Vt, unsigned Kt_behind, const f32x16 (&s)[TB], f32x16 (&t)[TB], auto fetch, auto between) ROWS_INLINE {
     constexpr int NK = TB * QN, NV = DB * SN / 8, NP = SN / 2, SPAN = NK + (SN / 8 - 1) * DB, MAX = SN / NV;
     unsigned pk[NP];
@@ -585,7 +659,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
     for (int i = 0; i < NK; ++i) {
       t[i % TB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ops[i % AHEAD]), qop[i / TB], t[i % TB], 0, 0, 0);
       const int next = i + AHEAD;
-      ops[i % AHEAD] = next < NK ? k_read(Kt, next < NK ? next : 0) : v_bf16(Vt, (next - NK) % DB, (next - NK) / DB);
+      ops[i % AHEAD] = next < NK ? k_piece(Kt, next < NK ? next : 0) : v_bf16(Vt, (next - NK) % DB, (next - NK) / DB);
       pairs(i);
       __builtin_amdgcn_sched_barrier(0);
       if (!LATE && i == 0) fetch();
@@ -598,7 +672,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
       acc[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ops[(NK + i) % AHEAD]), __builtin_bit_cast(bf16x8, pr),
                                                             acc[i % DB], 0, 0, 0);
       const int next = i + AHEAD;
-      ops[(NK + i) % AHEAD] = next < NV ? v_bf16(Vt, next % DB, next / DB) : k_read(Kt_behind, next - NV);
+      ops[(NK + i) % AHEAD] = next < NV ? v_bf16(Vt, next % DB, next / DB) : k_piece(Kt_behind, next - NV);
       pairs(NK + i);
       if (LATE && i == 0) fetch();
       if (i >= 1 && i <= NV / 2) {
@@ -633,7 +707,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
       logits(k_tile(0), s);
       refer(s);
 #pragma unroll
-      for (int i = 0; i < AHEAD; ++i) ops[i] = k_read(k_tile(1), i);     // (of a stage that may not exist: then not used)
+      for (int i = 0; i < AHEAD; ++i) ops[i] = k_piece(k_tile(1), i);     // (of a stage that may not exist: then not used)
       if (late) __syncthreads();
       auto step = [&](f32x16 (&from)[TB], f32x16 (&to)[TB]) ROWS_INLINE {
         if constexpr (LATE) {
@@ -809,6 +883,14 @@ __global__ __launch_bounds__(64) void rows_combine(RowsParams p) {
     m = p.part_m[lane * n + at];
     l = p.part_l[lane * n + at];
   }
+  int n_split = p.S;
+  if (TREE && p.deal > 0) {
+    n_split = __builtin_amdgcn_readlane(tree_deal(p), __builtin_amdgcn_readfirstlane(tok / p.nodes));
+    if (lane >= n_split) {
+      m = -INFINITY;
+      l = 0.f;
+    }
+  }
   const float* src = p.part_o + at * D + vec * 4;
   auto piece = [&](int s) { return *(const f32x4*)(src + (long long)min(s, p.S - 1) * n * D); };
   f32x4 ahead[PF];
@@ -818,7 +900,7 @@ __global__ __launch_bounds__(64) void rows_combine(RowsParams p) {
   const float w = m == -INFINITY ? 0.f : fast_exp2(m - mm);
   const float den = wave_sum(w * l);
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int s0 = 0; s0 < p.S; s0 += PF * GROUPS) {
+  for (int s0 = 0; s0 < n_split; s0 += PF * GROUPS) {
     f32x4 now[PF];
 #pragma unroll
     for (int u = 0; u < PF; ++u) {
@@ -828,7 +910,7 @@ __global__ __launch_bounds__(64) void rows_combine(RowsParams p) {
 #pragma unroll
     for (int u = 0; u < PF; ++u) {
       const float f = __shfl(w, s0 + u * GROUPS + g);       // (0 behind the last split: its lane has no maximum)
-      if (s0 + u * GROUPS + g < p.S && f != 0.f) o += f * now[u];
+      if (s0 + u * GROUPS + g < n_split && f != 0.f) o += f * now[u];
     }
   }
 #pragma unroll
@@ -869,7 +951,8 @@ static hipError_t launch_rows_rb(const RowsParams& p, hipStream_t st) {
   constexpr auto kernel = attn_rows<T, D, RB, Sh::TG, Sh::TW, Sh::NST, PAGED, TREE>;
   const hipError_t e = allow_dynamic_lds<kernel>(smem);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)p.n_tiles * p.Hkv, p.S), dim3(RB * Sh::TG * 64), smem, st, p);
+  const dim3 grid = p.deal > 0 ? dim3((unsigned)p.tiles_per_seq * p.Hkv, p.deal) : dim3((unsigned)p.n_tiles * p.Hkv, p.S);
+  hipLaunchKernelGGL(kernel, grid, dim3(RB * Sh::TG * 64), smem, st, p);
   return hipGetLastError();
 }
 
