@@ -489,7 +489,7 @@ void carve_rows(RowsParams* p, const RowsPlan& pl, void* workspace) {
   p->n_tiles = pl.n_tiles;
   p->deal = pl.deal;
   p->tiles_per_seq = std::max(1, pl.n_tiles / p->n_seq);
-  p->by_heads = rows_divisor(p->Hkv); p->by_group = rows_divisor(p->G); p->by_tiles = rows_divisor(p->tiles_per_seq);
+  p->by_heads = divisor(p->Hkv); p->by_group = divisor(p->G); p->by_tiles = divisor(p->tiles_per_seq);
   p->part_o = static_cast<float*>(workspace);
   p->part_m = reinterpret_cast<float*>(static_cast<char*>(workspace) + pl.off_m);
   p->part_l = reinterpret_cast<float*>(static_cast<char*>(workspace) + pl.off_l);
@@ -1250,7 +1250,8 @@ int hippo_write_kv_paged(const void* k_new, const void* v_new, int32_t n_rows, i
   const int es = elem_bytes(kv->dtype);
   if (stride_n % (16 / es) || stride_h % (16 / es)) return HIPPO_ERR_BAD_ALIGN;
   const int pieces = kv->head_dim * es / 16;
-  if ((long long)n_tokens * kv->n_kv_heads * pieces > (1ll << 31)) return HIPPO_ERR_BAD_SHAPE;
+  if ((long long)n_tokens * kv->n_kv_heads * pieces > (1ll << 31) || (long long)kv->n_kv_heads * pieces > (1 << 20))
+    return HIPPO_ERR_BAD_SHAPE;
   if (n_tokens == 0 || n_rows == 0) return HIPPO_OK;          // nothing to write
   if (k_new == nullptr || v_new == nullptr || slots == nullptr || k_pool == nullptr || v_pool == nullptr) return HIPPO_ERR_NULL_ARG;
   if (k_pool == v_pool) return HIPPO_ERR_BAD_SHAPE;
@@ -1258,7 +1259,10 @@ int hippo_write_kv_paged(const void* k_new, const void* v_new, int32_t n_rows, i
     return HIPPO_ERR_BAD_ALIGN;
   WriteParams p;
   p.k = k_new; p.v = v_new; p.slots = slots; p.rows = rows; p.k_pool = k_pool; p.v_pool = v_pool;
-  p.n_tokens = n_tokens; p.n_rows = n_rows; p.Hkv = kv->n_kv_heads; p.pieces = pieces; p.page_size = kv->page_size;
+  p.n_tokens = n_tokens; p.n_rows = n_rows; p.Hkv = kv->n_kv_heads; p.pieces = pieces;
+  p.page_shift = 0;
+  while ((1 << p.page_shift) < kv->page_size) ++p.page_shift;
+  p.by_token = divisor(p.Hkv * pieces); p.by_head = divisor(pieces);
   p.n_slots = (long long)kv->n_pool_pages * kv->page_size;
   p.sn = stride_n * es; p.sh = stride_h * es;
   p.page_stride = kv->stride_page * es; p.pool_sn = kv->stride_n * es; p.pool_sh = kv->stride_h * es;

@@ -769,6 +769,14 @@ PyObject* tree_paged(PyObject* const* a) {
   return c.result();
 }
 
+// n elements of a one-dimensional tensor, from `first` on
+Tensor part(const Tensor& whole, int64_t first, int64_t n) {
+  auto impl = c10::make_intrusive<c10::TensorImpl>(c10::TensorImpl::VIEW, c10::Storage(whole.storage()), whole.key_set(), whole.dtype());
+  impl->set_storage_offset(whole.storage_offset() + first);
+  impl->set_sizes_contiguous({n});
+  return Tensor(std::move(impl));
+}
+
 // ctx_lens, new_lens, block_table, free_pages, n_free, page_size, max_tokens, slots_out, positions_out, cu_q_out, kv_lens_out, n_free_out
 PyObject* plan_pages(PyObject* const* a) {
   const Tensor &ctx = tensor(a[0]), &add = tensor(a[1]), &table = tensor(a[2]), &free_pages = tensor(a[3]), &n_free = tensor(a[4]);
@@ -782,9 +790,17 @@ PyObject* plan_pages(PyObject* const* a) {
   require_int32(table, {B, table.size(1)});
   require_int32(free_pages, {free_pages.size(0)});
   require_int32(n_free, {1});
-  const Tensor slots = output(a[7], {most}, at::kInt, ctx), positions = output(a[8], {most}, at::kInt, ctx);
-  const Tensor cu_q = output(a[9], {B + 1}, at::kInt, ctx), kv_lens = output(a[10], {B}, at::kInt, ctx);
-  const Tensor left = output(a[11], {1}, at::kInt, ctx);
+  // what is not given comes out of one allocation (five take longer than the kernel)
+  const int64_t sizes[5] = {most, most, B + 1, B, 1};
+  int64_t at[5], all = 0;
+  for (int i = 0; i < 5; ++i) {
+    at[i] = all;
+    if (a[7 + i] == Py_None) all += (sizes[i] + 3) / 4 * 4;
+  }
+  const Tensor buffer = empty({all}, at::kInt, ctx);
+  Tensor out[5];
+  for (int i = 0; i < 5; ++i) out[i] = a[7 + i] == Py_None ? part(buffer, at[i], sizes[i]) : output(a[7 + i], {sizes[i]}, at::kInt, ctx);
+  const Tensor &slots = out[0], &positions = out[1], &cu_q = out[2], &kv_lens = out[3], &left = out[4];
   require_here({&ctx, &add, &table, &free_pages, &n_free, &slots, &positions, &cu_q, &kv_lens, &left});
   check(unlocked(lib.hippo_plan_pages, ptr<const int32_t>(ctx), ptr<const int32_t>(add), (int32_t)B, ptr<int32_t>(table),
                  (int32_t)table.size(1), ptr<int32_t>(free_pages), (int32_t)free_pages.size(0), ptr<const int32_t>(n_free),

@@ -172,6 +172,19 @@ __device__ __forceinline__ int row_div_group(int r, float inv_g) { return (int)(
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// ---- division by a number that the host knows ----------------------------------------------------
+// x / d for 0 <= x < 2^31 with one multiplication: 2^(31 + s) / d < m = floor(2^(31 + s) / d) + 1 < 2^32 for s = ceil(log2 d), and
+// x (m d - 2^(31 + s)) < 2^(31 + s), so that the fraction never reaches the next integer.
+struct Divisor {
+  unsigned m, shift;
+  __device__ __forceinline__ int operator()(int x) const { return (int)((unsigned long long)(unsigned)x * m >> shift); }
+};
+inline Divisor divisor(int d) {
+  unsigned s = 0;
+  while ((1ll << s) < d) ++s;
+  return {(unsigned)((1ull << (31 + s)) / (unsigned)d + 1), 31 + s};
+}
+
 // ---- HBM -> LDS transfers without registers in between -------------------------------------------
 // 16 bytes per lane from global memory straight into LDS at lds_addr + lane*16 (lds_addr uniform).
 // Issued from inline assembly with hand-placed vmcnt waits: the compiler would otherwise wait for
@@ -454,7 +467,8 @@ struct WriteParams {
   const int32_t* rows;       // [n_tokens] or null: token t's row is t
   void* k_pool;
   void* v_pool;
-  int n_tokens, n_rows, Hkv, pieces, page_size;   // pieces: 16 bytes each, of one head's row
+  int n_tokens, n_rows, Hkv, pieces, page_shift;   // pieces: 16 bytes each, of one head's row
+  Divisor by_token, by_head;      // by a token's pieces of all heads, and of one
   long long n_slots;
   long long sn, sh, page_stride, pool_sn, pool_sh;   // bytes
 };

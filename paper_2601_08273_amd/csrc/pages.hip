@@ -10,12 +10,12 @@ namespace hippo {
 // plan
 // =================================================================================================
 // One launch.  Every block scans all the requests for itself (two rounds of prefix sums over at most 4096 of them: what is asked for
-// and given back, then what of it is admitted), and then takes its share of three lists: pages given back, pages handed out, tokens.
-// An item finds its request by bisection of a prefix sum in the LDS.  No block waits for another's writes: a page handed out is looked
+// and given back, then what of it is admitted), and then takes its share of one list: the tokens, the pages handed out, the pages
+// given back.  An item finds its request by bisection of a prefix sum in the LDS; a thread has one item of a step of the usual size, as
+// a second one is another trip to memory.  No block waits for another's writes: a page handed out is looked
 // up on the stack of free pages or, where this call put it there, in the table that it came from; only entries that no block
 // reads are written (a request either grows or gives back).  Two launches, the scans and then the lists, would cost a launch; the
 // scans cost a block about 3 us, of which the loads of the lengths are most.
-constexpr int kPlanThreads = 1024;
 constexpr int kPlanMany = 1 << 30;     // sums stop here: no stack of pages and no step is that large
 
 struct PlanSums {                      // of the requests up to and with one
@@ -23,6 +23,7 @@ struct PlanSums {                      // of the requests up to and with one
 };
 
 // Inclusive prefix sums over the block of three values of at most 2^22 each, behind `carry`, which moves on.
+template <int THREADS>
 __device__ __forceinline__ PlanSums plan_scan(PlanSums v, PlanSums* carry, int (*totals)[3]) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int in[3] = {v.given, v.pages, v.tokens};
@@ -36,7 +37,7 @@ __device__ __forceinline__ PlanSums plan_scan(PlanSums v, PlanSums* carry, int (
   __syncthreads();
   int before[3] = {carry->given, carry->pages, carry->tokens}, all[3] = {before[0], before[1], before[2]};
 #pragma unroll
-  for (int w = 0; w < kPlanThreads / 64; ++w)
+  for (int w = 0; w < THREADS / 64; ++w)
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
       if (w == wave) before[i] = all[i];
@@ -73,9 +74,10 @@ __device__ __forceinline__ PlanRequest plan_request(const PlanParams& p, int ctx
   return r;
 }
 
-__global__ __launch_bounds__(kPlanThreads) void plan_pages(PlanParams p) {
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void plan_pages(PlanParams p) {
   extern __shared__ int plan_lds[];
-  __shared__ int totals[kPlanThreads / 64][3];
+  __shared__ int totals[THREADS / 64][3];
   const int tid = threadIdx.x, B = p.B;
   int* tok_incl = plan_lds;                                 // tokens of the admitted requests up to and with each
   int* pg_incl = plan_lds + B;                              // pages
@@ -85,7 +87,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_pages(PlanParams p) {
 
   // ---- what is asked for and given back ----
   PlanSums carry = {0, 0, 0};
-  for (int b0 = 0; b0 < B; b0 += kPlanThreads) {
+  for (int b0 = 0; b0 < B; b0 += THREADS) {
     const int b = b0 + tid;
     PlanSums v = {0, 0, 0};
     int ctx = 0;
@@ -99,7 +101,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_pages(PlanParams p) {
         v.tokens = min(add, p.max_tokens + 1);              // (more than there are slots for is refused, however many)
       }
     }
-    const PlanSums s = plan_scan(v, &carry, totals);
+    const PlanSums s = plan_scan<THREADS>(v, &carry, totals);
     if (b < B) {
       ctx_of[b] = ctx;
       given_incl[b] = s.given;
@@ -111,7 +113,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_pages(PlanParams p) {
 
   // ---- what of it is admitted: as long as pages and slots last, in the order of the requests ----
   carry = {0, 0, 0};
-  for (int b0 = 0; b0 < B; b0 += kPlanThreads) {
+  for (int b0 = 0; b0 < B; b0 += THREADS) {
     const int b = b0 + tid;
     PlanSums v = {0, 0, 0};
     if (b < B) {
@@ -125,7 +127,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_pages(PlanParams p) {
       }
       if (blockIdx.x == 0) p.kv_lens[b] = admitted || add < 0 ? r.after : r.ctx;
     }
-    const PlanSums s = plan_scan(v, &carry, totals);
+    const PlanSums s = plan_scan<THREADS>(v, &carry, totals);
     if (b < B) {
       pg_incl[b] = s.pages;
       tok_incl[b] = s.tokens;
@@ -150,36 +152,44 @@ __global__ __launch_bounds__(kPlanThreads) void plan_pages(PlanParams p) {
     const int at = available - 1 - g;
     return at >= n_free ? given_page(at - n_free) : p.free_pages[at];
   };
-  const long long first = (long long)blockIdx.x * kPlanThreads + tid, step = (long long)gridDim.x * kPlanThreads;
-  for (long long i = first; i < available - n_free; i += step) p.free_pages[n_free + i] = given_page((int)i);
-  for (long long i = first; i < n_pages; i += step) {
-    const int g = (int)i, b = plan_find(pg_incl, B, g);
-    const int held = (int)(((long long)ctx_of[b] + (1 << p.page_shift) - 1) >> p.page_shift);
-    p.block_table[(long long)b * p.max_pages + held + g - (b > 0 ? pg_incl[b - 1] : 0)] = page_of(g);
-  }
-  for (long long i = first; i < p.max_tokens; i += step) {
-    int slot = -1, position = -1;
-    if (i < n_tokens) {
-      const int t = (int)i, b = plan_find(tok_incl, B, t);
+  const int pushed = available - n_free;                    // (more only where the stack holds pages twice)
+  const int step = gridDim.x * THREADS;                     // (the three counts and a step stay below 2^31)
+  for (int i = blockIdx.x * THREADS + tid; i < p.max_tokens + n_pages + pushed; i += step) {
+    if (i < p.max_tokens) {
+      int slot = -1, position = -1;
+      if (i < n_tokens) {
+        const int b = plan_find(tok_incl, B, i);
+        const int held = (int)(((long long)ctx_of[b] + (1 << p.page_shift) - 1) >> p.page_shift);
+        position = ctx_of[b] + i - (b > 0 ? tok_incl[b - 1] : 0);
+        const int column = position >> p.page_shift;
+        const int page = column < held ? p.block_table[(long long)b * p.max_pages + column]
+                                       : page_of((b > 0 ? pg_incl[b - 1] : 0) + column - held);
+        if (page >= 0 && page < p.n_pool) slot = (page << p.page_shift) + (position & ((1 << p.page_shift) - 1));
+      }
+      p.slots[i] = slot;
+      p.positions[i] = position;
+    } else if (i < p.max_tokens + n_pages) {
+      const int g = i - p.max_tokens, b = plan_find(pg_incl, B, g);
       const int held = (int)(((long long)ctx_of[b] + (1 << p.page_shift) - 1) >> p.page_shift);
-      position = ctx_of[b] + t - (b > 0 ? tok_incl[b - 1] : 0);
-      const int column = position >> p.page_shift;
-      const int page = column < held ? p.block_table[(long long)b * p.max_pages + column]
-                                     : page_of((b > 0 ? pg_incl[b - 1] : 0) + column - held);
-      if (page >= 0 && page < p.n_pool) slot = (page << p.page_shift) + (position & ((1 << p.page_shift) - 1));
+      p.block_table[(long long)b * p.max_pages + held + g - (b > 0 ? pg_incl[b - 1] : 0)] = page_of(g);
+    } else {
+      const int g = i - p.max_tokens - n_pages;
+      p.free_pages[n_free + g] = given_page(g);
     }
-    p.slots[i] = slot;
-    p.positions[i] = position;
   }
 }
 
-hipError_t launch_plan_pages(const PlanParams& p, hipStream_t st) {
-  const int smem = 4 * p.B * (int)sizeof(int);
-  const hipError_t e = allow_dynamic_lds<plan_pages>(4 * kPlanMaxBatch * (int)sizeof(int));
+template <int THREADS>
+static hipError_t launch_plan(const PlanParams& p, hipStream_t st) {
+  const hipError_t e = allow_dynamic_lds<plan_pages<THREADS>>(4 * kPlanMaxBatch * (int)sizeof(int));
   if (e != hipSuccess) return e;
-  const int blocks = std::min(kNumCU, (p.max_tokens + 4 * kPlanThreads - 1) / (4 * kPlanThreads));
-  hipLaunchKernelGGL(plan_pages, dim3(std::max(blocks, 1)), dim3(kPlanThreads), smem, st, p);
+  // a thread for every token and two pages a request, while they are on the chip together
+  const int blocks = std::min(1024 / (THREADS / 256), (p.max_tokens + 2 * p.B + THREADS - 1) / THREADS);
+  hipLaunchKernelGGL(plan_pages<THREADS>, dim3(blocks), dim3(THREADS), 4 * p.B * (int)sizeof(int), st, p);
   return hipGetLastError();
+}
+hipError_t launch_plan_pages(const PlanParams& p, hipStream_t st) {
+  return p.B <= 512 ? launch_plan<256>(p, st) : launch_plan<1024>(p, st);
 }
 
 // =================================================================================================
@@ -190,10 +200,9 @@ hipError_t launch_plan_pages(const PlanParams& p, hipStream_t st) {
 constexpr int kWriteTokens = 4;
 
 __global__ __launch_bounds__(256) void write_kv(WriteParams p) {
-  const unsigned per_token = p.Hkv * p.pieces;              // pieces of a token's K
-  const unsigned i = blockIdx.x * 256 + threadIdx.x, group = i / per_token;
-  const unsigned piece = i - group * per_token, hk = piece / p.pieces, c = piece - hk * p.pieces;
-  const int t0 = (int)(group * kWriteTokens);               // (the host keeps the threads below 2^31)
+  const int i = blockIdx.x * 256 + threadIdx.x, group = p.by_token(i);         // (the host keeps the threads below 2^31)
+  const int piece = i - group * p.Hkv * p.pieces, hk = p.by_head(piece), c = piece - hk * p.pieces;
+  const int t0 = group * kWriteTokens;
   u32x4 k[kWriteTokens], v[kWriteTokens];
   long long to[kWriteTokens];
 #pragma unroll
@@ -202,8 +211,8 @@ __global__ __launch_bounds__(256) void write_kv(WriteParams p) {
     if (t0 + u >= p.n_tokens) continue;
     const int slot = p.slots[t0 + u], row = p.rows != nullptr ? p.rows[t0 + u] : t0 + u;
     if (slot < 0 || slot >= p.n_slots || row < 0 || row >= p.n_rows) continue;
-    const int page = slot / p.page_size;
-    to[u] = page * p.page_stride + (long long)(slot - page * p.page_size) * p.pool_sn + hk * p.pool_sh + c * 16;
+    to[u] = (long long)(slot >> p.page_shift) * p.page_stride + (long long)(slot & ((1 << p.page_shift) - 1)) * p.pool_sn +
+            hk * p.pool_sh + c * 16;
     const long long from = row * p.sn + hk * p.sh + c * 16;
     k[u] = *(const u32x4*)((const char*)p.k + from);
     v[u] = *(const u32x4*)((const char*)p.v + from);

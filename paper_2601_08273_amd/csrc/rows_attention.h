@@ -22,18 +22,6 @@
 
 namespace hippo {
 
-// x / d for 0 <= x < 2^31 with one multiplication: 2^(31 + s) / d < m = floor(2^(31 + s) / d) + 1 < 2^32 for s = ceil(log2 d), and
-// x (m d - 2^(31 + s)) < 2^(31 + s), so that the fraction never reaches the next integer.
-struct RowsDivisor {
-  unsigned m, shift;
-  __device__ __forceinline__ int operator()(int x) const { return (int)((unsigned long long)(unsigned)x * m >> shift); }
-};
-inline RowsDivisor rows_divisor(int d) {
-  unsigned s = 0;
-  while ((1ll << s) < d) ++s;
-  return {(unsigned)((1ull << (31 + s)) / (unsigned)d + 1), 31 + s};
-}
-
 struct RowsParams {
   const void* q;
   const void* k;
@@ -55,7 +43,7 @@ struct RowsParams {
   int page_shift, max_pages, n_pool_pages;
   long long page_stride;
   float scale_log2;
-  RowsDivisor by_heads, by_group, by_tiles;   // by Hkv, G, tiles_per_seq
+  Divisor by_heads, by_group, by_tiles;   // by Hkv, G, tiles_per_seq
   int tiles_per_seq;            // of trees
   int S;                        // blocks that share a tile's stages (parts in the workspace)
   int deal;                     // trees of 2 to 64 sequences: that many such blocks over all of them, by length; 0: S each
