@@ -374,25 +374,26 @@ double rows_pace(int dtype, int head_dim, int rb) {
 
 // How to cut a call: the rows of a block and the blocks that share a tile's tokens, by the time that they are going to take.
 //   a block: kBlockUs besides its tokens (its start and its end), one on a compute unit at a time
-//   a call:  the longest block of all, or all blocks on all compute units; kLaunchUs
+//   a call:  the longest block of all, or all blocks on all compute units: as many rounds as that takes, a last one in proportion where
+//            the blocks' sizes are spread (short ones fill it up)
 //   blocks that share tiles: a merge, kMergeUs and kMergeMbUs for a megabyte of parts
-// rows: query rows of a KV head of one sequence, on average; seen: the tokens that the last of them sees, seen_mean: that all do; whole:
-// every block takes as many tokens as any other (trees); num_splits: the caller's.
-constexpr double kBlockUs = 4.0, kLaunchUs = 2.5, kMergeUs = 4.0, kMergeMbUs = 0.9;
-void cut_rows(RowsPlan* pl, int dtype, int head_dim, double rows, double n_seqs, double seen, double seen_mean, bool whole, int Hkv,
+// rows: query rows of a KV head of one sequence, on average; seen, seen_least: the tokens that the last and the first of them see; tree:
+// a sequence's tiles are its own; num_splits: the caller's.
+constexpr double kBlockUs = 4.0, kMergeUs = 4.0, kMergeMbUs = 0.9;
+void cut_rows(RowsPlan* pl, int dtype, int head_dim, double rows, double n_seqs, double seen, double seen_least, bool tree, int Hkv,
               double part_bytes, int num_splits) {
   static const int splits[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64};
   double best = 1e30;
   for (int rb = 8; rb >= 1; rb /= 2) {
     const double pace = rows_pace(dtype, head_dim, rb);
     if (pace == 0) continue;
-    const double tiles = n_seqs * (whole ? ceil(rows / (32 * rb)) : std::max(1.0, rows / (32 * rb) + 0.5)) * Hkv;
+    const double tiles = n_seqs * (tree ? ceil(rows / (32 * rb)) : std::max(1.0, rows / (32 * rb) + 0.5)) * Hkv;
     for (int S : splits) {
       if (num_splits > 0 ? S != 1 : S > 1 && seen < 64.0 * S) break;
       const double n = num_splits > 0 ? num_splits : S;
-      const double longest = kBlockUs + seen / 64 / n * pace, mean = kBlockUs + seen_mean / 64 / n * pace;
+      const double longest = kBlockUs + seen / 64 / n * pace, mean = kBlockUs + (seen + seen_least) / 128 / n * pace;
       const double rounds = tiles * n / kNumCU;
-      const double t = std::max(longest, whole ? ceil(rounds) * longest : rounds * mean) +
+      const double t = std::max(longest, (rounds + seen_least / seen * (ceil(rounds) - rounds)) * mean) +
                        (n > 1 ? kMergeUs + kMergeMbUs * n * part_bytes * 1e-6 : 0.0);
       if (t < best * 0.999) {
         best = t;
@@ -434,7 +435,7 @@ int plan_prefill(const hippo_packed_desc* d, bool paged, int total_q, int total_
   if (rows > (1 << 30) || (long long)total_q * d->n_q_heads > (1 << 30) || total_k > 0x7fffff00) return HIPPO_ERR_BAD_SHAPE;
   // (the lengths are on the device: taken as equal, each seeing what is there beside the others)
   const double len_q = std::max(1.0, (double)total_q / n_seqs), seen = std::max(len_q, paged ? (double)total_k : (double)total_k / n_seqs);
-  cut_rows(pl, d->dtype, d->head_dim, len_q * G, std::min<double>(n_seqs, std::max(1, total_q)), seen, seen - len_q / 2, false,
+  cut_rows(pl, d->dtype, d->head_dim, len_q * G, std::min<double>(n_seqs, std::max(1, total_q)), seen, seen - len_q, false,
            d->n_kv_heads, (double)total_q * d->n_q_heads * d->head_dim * 4, num_splits);
   pl->deal = 0;
   pl->n_tiles = (int)(rows / (32 * pl->rb) + n_seqs);
