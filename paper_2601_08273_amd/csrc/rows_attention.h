@@ -262,6 +262,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   float* stat_l = stat_m + TG * ROWS;
   int* odd_stage = (int*)(stat_l + TG * ROWS);              // the last edge stage whose V has infinities or NaN, from 1
   if (threadIdx.x == 0) *odd_stage = 0;                     // (before the barriers of the stages)
+  wait_lds();
   const unsigned ring_addr = (unsigned)(uintptr_t)ring;
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -762,6 +763,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
     }
     refer(s);
     weights(s, pk);
+    wait_lds();
     __syncthreads();
     if (__builtin_expect(*(volatile int*)odd_stage == si + 1, 0)) values_odd(v_tile(si), s, pk, vis);
     else values(v_tile(si), s, pk);
