@@ -373,27 +373,27 @@ double rows_pace(int dtype, int head_dim, int rb) {
 }
 
 // How to cut a call: the rows of a block and the blocks that share a tile's tokens, by the time that they are going to take.
-//   a block: kBlockUs besides its tokens (its start and its end), one on a compute unit at a time
+//   a block: kBlockUs (trees: kTreeBlockUs) besides its tokens (its start, its masked stages and its end), one on a compute unit at a time
 //   a call:  the longest block of all, or all blocks on all compute units: as many rounds as that takes, a last one in proportion where
 //            the blocks' sizes are spread (short ones fill it up)
 //   blocks that share tiles: a merge, kMergeUs and kMergeMbUs for a megabyte of parts
 // rows: query rows of a KV head of one sequence, on average; seen, seen_least: the tokens that the last and the first of them see; tree:
 // a sequence's tiles are its own; num_splits: the caller's.
-constexpr double kBlockUs = 4.0, kMergeUs = 4.0, kMergeMbUs = 0.9;
+constexpr double kTreeBlockUs = 4.0, kBlockUs[] = {4.0, 4.5, 7.0, 7.0}, kMergeUs = 4.0, kMergeMbUs = 0.9;       // rb 1, 2, 4, 8
 void cut_rows(RowsPlan* pl, int dtype, int head_dim, double rows, double n_seqs, double seen, double seen_least, bool tree, int Hkv,
               double part_bytes, int num_splits) {
   static const int splits[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64};
   double best = 1e30;
   for (int rb = 8; rb >= 1; rb /= 2) {
-    const double pace = rows_pace(dtype, head_dim, rb);
+    const double pace = rows_pace(dtype, head_dim, rb), block = tree ? kTreeBlockUs : kBlockUs[rb == 1 ? 0 : rb == 2 ? 1 : rb == 4 ? 2 : 3];
     if (pace == 0) continue;
     const double tiles = n_seqs * (tree ? ceil(rows / (32 * rb)) : std::max(1.0, rows / (32 * rb) + 0.5)) * Hkv;
     for (int S : splits) {
       if (num_splits > 0 ? S != 1 : S > 1 && seen < 64.0 * S) break;
       const double n = num_splits > 0 ? num_splits : S;
-      const double longest = kBlockUs + seen / 64 / n * pace, mean = kBlockUs + (seen + seen_least) / 128 / n * pace;
-      const double rounds = tiles * n / kNumCU;
-      const double t = std::max(longest, (rounds + seen_least / seen * (ceil(rounds) - rounds)) * mean) +
+      const double longest = block + seen / 64 / n * pace, mean = block + (seen + seen_least) / 128 / n * pace;
+      const double rounds = tiles * n / kNumCU, alike = (block + seen_least / 64 / n * pace) / longest;
+      const double t = std::max(longest, (rounds + alike * (ceil(rounds) - rounds)) * mean) +
                        (n > 1 ? kMergeUs + kMergeMbUs * n * part_bytes * 1e-6 : 0.0);
       if (t < best * 0.999) {
         best = t;

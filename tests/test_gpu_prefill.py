@@ -268,3 +268,46 @@ def test_no_rows(hippo):
     q, k, v = make([5], [0], 4, 2, 64, "fp32", 21)
     out, lse = hippo.hippo_prefill_attention(q, k, v, offsets([5]), offsets([0]), want_lse=True)
     assert (out == 0).all() and (lse == -float("inf")).all()
+
+
+@pytest.mark.parametrize("dtype,heads,least", [("bf16", (28, 4, 128), 1), ("bf16", (14, 2, 64), 1), ("fp32", (4, 2, 64), 1), ("fp32", (28, 4, 128), 2)])
+def test_every_tile_size(hippo, kernels, dtype, heads, least):
+    """few and many rows, so that each size of a block is taken, over lengths that end around its stages: none, one and several that need
+    no mask"""
+    H, Hkv, d = heads
+    sizes = set()
+    some = [1, 20, 31, 64, 65, 127, 128, 129, 191, 192, 256, 257, 320, 321, 385, 449, 513, 640]
+    for seqs, lens_of in ((1, some), (8, some), (24, some[7:]), (60, [64, 129, 257, 385])):
+        for n in lens_of:
+            if dtype == "fp32" and (d == 128 and n * seqs > 4000):
+                continue
+            lens = [n] * seqs
+            q, k, v = make(lens, lens, H, Hkv, d, dtype, n)
+            cu = offsets(lens)
+            call = lambda: hippo.hippo_prefill_attention(q, k, v, cu, want_lse=True)      # noqa: E731
+            out, lse = call()
+            sizes |= {int(name.split("attn_rows")[1].split("ELi")[1]) for name in kernels(call) if "attn_rows" in name}
+            first, last = slice(0, n), slice((seqs - 1) * n, seqs * n)
+            for at in (first, last):
+                ref = reference(q[at], k[at], v[at], [n], [n])
+                check(out[at], ref[0], ref[1], "%d x %d" % (seqs, n))
+                check_lse(lse[:, at], ref[2], ref[3], "%d x %d" % (seqs, n))
+            # equal rows of other sequences: the same bits from another place in the launch
+            if seqs > 2:
+                q2, k2, v2 = (torch.cat([x[first], x[n:-n], x[first]]) for x in (q, k, v))
+                again = hippo.hippo_prefill_attention(q2, k2, v2, cu)
+                assert torch.equal(again[first], again[last])
+    assert sizes == {1, 2, 4, 8} - ({1} if least == 2 else set()), sizes
+
+
+def test_two_calls_at_once(hippo):
+    """on streams of their own, each with its own workspace"""
+    lens = [400, 90]
+    a, b = make(lens, lens, 28, 4, 128, "bf16", 30), make(lens, lens, 28, 4, 128, "bf16", 31)
+    cu = offsets(lens)
+    want = [hippo.hippo_prefill_attention(*x, cu, num_splits=4) for x in (a, b)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[hippo.hippo_prefill_attention(*x, cu, num_splits=4, stream=s) for _ in range(5)] for x, s in zip((a, b), streams)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, w) for gs, w in zip(got, want) for g in gs)

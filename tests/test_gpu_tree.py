@@ -210,3 +210,28 @@ def test_long_caches(hippo, dtype, heads, n, ctx):
     q, k, v = make(len(ctx), n, max(ctx) + n, H, Hkv, d, dtype, 13)
     parents = [some_tree(n, b, padding=b) for b in range(len(ctx))]
     verify(hippo.hippo_tree_attention(q, k, v, int32(parents), int32(ctx), want_lse=True), reference(q, k, v, parents, ctx))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("B,n,longest", [(2, 5, 3000), (3, 64, 900), (17, 9, 700), (64, 3, 500), (65, 3, 500), (130, 1, 200)])
+def test_batches_of_very_different_lengths(hippo, dtype, B, n, longest):
+    """blocks are dealt out by length to 2 to 64 sequences, evenly to more"""
+    g = torch.Generator().manual_seed(B)
+    ctx = [int(longest * float(x) ** 3) for x in torch.rand(B, generator=g)]
+    ctx[0], ctx[-1] = 0, longest
+    q, k, v = make(B, n, longest + n, 4, 2, 64, dtype, 14)
+    parents = [some_tree(n, b, padding=b % max(1, n // 2)) for b in range(B)]
+    want = reference(q, k, v, parents, ctx)
+    for splits in (0, 2, 5, 64):
+        got = hippo.hippo_tree_attention(q, k, v, int32(parents), int32(ctx), num_splits=splits, want_lse=True)
+        verify(got, want, "%d sequences, %d splits" % (B, splits))
+
+
+def test_one_length_for_all_needs_no_tensor(hippo):
+    q, k, v = make(3, 7, 500, 14, 2, 64, "bf16", 15)
+    parents = some_tree(7, 1)
+    a = hippo.hippo_tree_attention(q, k, v, int32(parents), 400)
+    b = hippo.hippo_tree_attention(q, k, v, int32([parents] * 3), int32([400] * 3), num_splits=1)
+    ref = reference(q, k, v, [parents] * 3, [400] * 3)
+    check(a, ref[0], ref[1])
+    check(b, ref[0], ref[1])

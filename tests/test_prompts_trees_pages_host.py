@@ -1,0 +1,203 @@
+"""Refusals of the prompt, tree, plan and write calls, and their workspace sizes, without a GPU: the library answers before it launches
+anything, and the binding before it calls the library."""
+import ctypes as C
+import re
+
+import pytest
+import torch
+
+import paper_2601_08273_amd as h
+
+FAKE = 0x10000
+
+
+def packed(**more):
+    d = dict(n_q_heads=28, n_kv_heads=4, head_dim=128, dtype=h.DTYPE_BF16, q_stride_n=3584, q_stride_h=128, kv_stride_n=512, kv_stride_h=128)
+    d.update(more)
+    return h.PackedDesc(**d)
+
+
+def pool(**more):
+    d = dict(batch=3, n_q_heads=28, n_kv_heads=4, head_dim=128, dtype=h.DTYPE_BF16, page_size=16, max_pages=100, n_pool_pages=500,
+             stride_page=8192, stride_n=512, stride_h=128)
+    d.update(more)
+    return h.PagedKvDesc(**d)
+
+
+def cache(**more):
+    d = dict(batch=2, n_q_heads=28, n_kv_heads=4, head_dim=128, dtype=h.DTYPE_BF16, stride_b=4 * 2000 * 128, stride_h=2000 * 128, stride_n=128)
+    d.update(more)
+    return h.KvDesc(**d)
+
+
+def ref(d):
+    return None if d is None else C.byref(d)
+
+
+def prefill(q=FAKE, n_q=1000, k=FAKE, v=FAKE, n_k=1000, desc=packed(), cu_q=FAKE, cu_k=FAKE, seqs=3, splits=0, out=FAKE, lse=None, ws=FAKE,
+            ws_bytes=1 << 40):
+    return h.load().hippo_prefill_attention(q, n_q, k, v, n_k, ref(desc), cu_q, cu_k, seqs, 0.0, splits, out, lse, ws, ws_bytes, None)
+
+
+def prefill_paged(q=FAKE, n_q=1000, sn=3584, sh=128, k=FAKE, v=FAKE, table=FAKE, kv=pool(), cu_q=FAKE, lens=FAKE, splits=0, out=FAKE, ws=FAKE,
+                  ws_bytes=1 << 40):
+    return h.load().hippo_prefill_attention_paged(q, n_q, sn, sh, k, v, table, ref(kv), cu_q, lens, 0.0, splits, out, None, ws, ws_bytes, None)
+
+
+def tree(q=FAKE, nodes=16, k=FAKE, v=FAKE, kv=cache(), rows=2000, parents=FAKE, psb=16, lens=FAKE, ctx=0, splits=0, out=FAKE, lse=None, ws=FAKE,
+         ws_bytes=1 << 40):
+    return h.load().hippo_tree_attention(q, nodes, k, v, ref(kv), rows, parents, psb, lens, ctx, 0.0, splits, out, lse, ws, ws_bytes, None)
+
+
+def tree_paged(q=FAKE, nodes=16, k=FAKE, v=FAKE, table=FAKE, kv=pool(), parents=FAKE, psb=16, lens=FAKE, ctx=0, splits=0, out=FAKE, ws=FAKE,
+               ws_bytes=1 << 40):
+    return h.load().hippo_tree_attention_paged(q, nodes, k, v, table, ref(kv), parents, psb, lens, ctx, 0.0, splits, out, None, ws, ws_bytes,
+                                               None)
+
+
+def plan(ctx=FAKE, new=2 * FAKE, batch=5, table=3 * FAKE, columns=10, free=4 * FAKE, n_pool=50, n_free=5 * FAKE, page=16, most=100,
+         slots=6 * FAKE, positions=7 * FAKE, cu=8 * FAKE, lens=9 * FAKE, left=10 * FAKE):
+    return h.load().hippo_plan_pages(ctx, new, batch, table, columns, free, n_pool, n_free, page, most, slots, positions, cu, lens, left, None)
+
+
+def write(k=FAKE, v=FAKE, rows=100, sn=512, sh=128, slots=FAKE, pick=None, tokens=50, kp=2 * FAKE, vp=3 * FAKE, kv=pool()):
+    return h.load().hippo_write_kv_paged(k, v, rows, sn, sh, slots, pick, tokens, kp, vp, ref(kv), None)
+
+
+NULL, SHAPE, DTYPE, ALIGN, SMALL = (h.ERR_NULL_ARG, h.ERR_BAD_SHAPE, h.ERR_BAD_DTYPE, h.ERR_BAD_ALIGN, h.ERR_WORKSPACE_TOO_SMALL)
+
+
+@pytest.mark.parametrize("call,bad,status", [
+    (prefill, dict(q=None), NULL), (prefill, dict(k=None), NULL), (prefill, dict(v=None), NULL), (prefill, dict(desc=None), NULL),
+    (prefill, dict(cu_q=None), NULL), (prefill, dict(cu_k=None), NULL), (prefill, dict(out=None), NULL), (prefill, dict(ws=None), NULL),
+    (prefill, dict(n_q=-1), SHAPE), (prefill, dict(n_k=-1), SHAPE), (prefill, dict(seqs=0), SHAPE), (prefill, dict(seqs=65536), SHAPE),
+    (prefill, dict(splits=-1), SHAPE), (prefill, dict(n_q=1 << 28), SHAPE), (prefill, dict(n_k=0x7fffffff), SHAPE),
+    (prefill, dict(desc=packed(head_dim=96)), SHAPE), (prefill, dict(desc=packed(n_q_heads=27)), SHAPE),
+    (prefill, dict(desc=packed(n_kv_heads=0)), SHAPE), (prefill, dict(desc=packed(kv_stride_n=-512)), SHAPE),
+    (prefill, dict(desc=packed(kv_stride_n=1 << 25)), SHAPE), (prefill, dict(desc=packed(q_stride_h=-128)), SHAPE),
+    (prefill, dict(desc=packed(dtype=h.DTYPE_FP8_E4M3)), DTYPE), (prefill, dict(desc=packed(dtype=9)), DTYPE),
+    (prefill, dict(desc=packed(q_stride_n=3588)), ALIGN), (prefill, dict(desc=packed(kv_stride_h=132)), ALIGN),
+    (prefill, dict(q=FAKE + 8), ALIGN), (prefill, dict(k=FAKE + 8), ALIGN), (prefill, dict(v=FAKE + 4), ALIGN), (prefill, dict(out=FAKE + 8), ALIGN),
+    (prefill, dict(ws=FAKE + 128), ALIGN), (prefill, dict(cu_q=FAKE + 2), ALIGN), (prefill, dict(cu_k=FAKE + 1), ALIGN),
+    (prefill, dict(lse=FAKE + 2), ALIGN), (prefill, dict(ws_bytes=255), SMALL), (prefill, dict(splits=4, ws_bytes=1 << 20), SMALL),
+    (prefill_paged, dict(table=None), NULL), (prefill_paged, dict(kv=None), NULL), (prefill_paged, dict(k=None), NULL),
+    (prefill_paged, dict(lens=None), NULL), (prefill_paged, dict(cu_q=None), NULL), (prefill_paged, dict(q=None), NULL),
+    (prefill_paged, dict(kv=pool(page_size=24)), SHAPE), (prefill_paged, dict(kv=pool(page_size=8)), SHAPE),
+    (prefill_paged, dict(kv=pool(page_size=512)), SHAPE), (prefill_paged, dict(kv=pool(max_pages=0)), SHAPE),
+    (prefill_paged, dict(kv=pool(n_pool_pages=0)), SHAPE), (prefill_paged, dict(kv=pool(max_pages=1 << 28)), SHAPE),
+    (prefill_paged, dict(kv=pool(stride_page=8184)), SHAPE), (prefill_paged, dict(kv=pool(stride_n=120)), SHAPE),
+    (prefill_paged, dict(kv=pool(batch=0)), SHAPE), (prefill_paged, dict(kv=pool(head_dim=32)), SHAPE),
+    (prefill_paged, dict(kv=pool(dtype=h.DTYPE_FP8_E4M3)), DTYPE), (prefill_paged, dict(kv=pool(stride_page=8196)), ALIGN),
+    (prefill_paged, dict(sn=3585), ALIGN), (prefill_paged, dict(table=FAKE + 2), ALIGN), (prefill_paged, dict(ws_bytes=10), SMALL),
+    (tree, dict(q=None), NULL), (tree, dict(k=None), NULL), (tree, dict(v=None), NULL), (tree, dict(kv=None), NULL), (tree, dict(parents=None), NULL),
+    (tree, dict(out=None), NULL), (tree, dict(ws=None), NULL), (tree, dict(nodes=0), SHAPE), (tree, dict(nodes=65), SHAPE),
+    (tree, dict(rows=15), SHAPE), (tree, dict(splits=-1), SHAPE), (tree, dict(psb=-1), SHAPE), (tree, dict(lens=None, ctx=-1), SHAPE),
+    (tree, dict(lens=None, ctx=1985), SHAPE), (tree, dict(kv=cache(head_dim=80)), SHAPE), (tree, dict(kv=cache(n_q_heads=30)), SHAPE),
+    (tree, dict(kv=cache(batch=0)), SHAPE), (tree, dict(kv=cache(dtype=h.DTYPE_FP8_E4M3)), DTYPE), (tree, dict(kv=cache(stride_n=132)), ALIGN),
+    (tree, dict(q=FAKE + 8), ALIGN), (tree, dict(parents=FAKE + 2), ALIGN), (tree, dict(lens=FAKE + 2), ALIGN), (tree, dict(lse=FAKE + 1), ALIGN),
+    (tree, dict(ws_bytes=128), SMALL),
+    (tree_paged, dict(table=None), NULL), (tree_paged, dict(kv=None), NULL), (tree_paged, dict(parents=None), NULL),
+    (tree_paged, dict(nodes=65), SHAPE), (tree_paged, dict(kv=pool(page_size=20)), SHAPE), (tree_paged, dict(kv=pool(max_pages=0)), SHAPE),
+    (tree_paged, dict(nodes=33, kv=pool(max_pages=2)), SHAPE), (tree_paged, dict(lens=None, ctx=1585), SHAPE),
+    (tree_paged, dict(kv=pool(n_q_heads=30)), SHAPE), (tree_paged, dict(kv=pool(stride_h=4)), ALIGN), (tree_paged, dict(ws_bytes=10), SMALL),
+    (plan, dict(ctx=None), NULL), (plan, dict(new=None), NULL), (plan, dict(table=None), NULL), (plan, dict(free=None), NULL),
+    (plan, dict(n_free=None), NULL), (plan, dict(slots=None), NULL), (plan, dict(positions=None), NULL), (plan, dict(cu=None), NULL),
+    (plan, dict(lens=None), NULL), (plan, dict(left=None), NULL), (plan, dict(batch=0), SHAPE), (plan, dict(batch=4097), SHAPE),
+    (plan, dict(columns=0), SHAPE), (plan, dict(columns=(1 << 22) + 1), SHAPE), (plan, dict(batch=4096, columns=1 << 19), SHAPE),
+    (plan, dict(n_pool=0), SHAPE), (plan, dict(n_pool=(1 << 22) + 1), SHAPE), (plan, dict(most=-1), SHAPE), (plan, dict(most=(1 << 22) + 1), SHAPE),
+    (plan, dict(page=0), SHAPE), (plan, dict(page=48), SHAPE), (plan, dict(page=512), SHAPE), (plan, dict(lens=FAKE), SHAPE),
+    (plan, dict(left=5 * FAKE), SHAPE), (plan, dict(cu=2 * FAKE), SHAPE), (plan, dict(table=3 * FAKE + 2), ALIGN), (plan, dict(slots=6 * FAKE + 1), ALIGN),
+    (write, dict(k=None), NULL), (write, dict(v=None), NULL), (write, dict(slots=None), NULL), (write, dict(kp=None), NULL), (write, dict(kv=None), NULL),
+    (write, dict(tokens=-1), SHAPE), (write, dict(rows=-1), SHAPE), (write, dict(sn=-8), SHAPE), (write, dict(vp=2 * FAKE), SHAPE),
+    (write, dict(tokens=1 << 30), SHAPE), (write, dict(kv=pool(page_size=48)), SHAPE), (write, dict(kv=pool(stride_h=64)), SHAPE),
+    (write, dict(kv=pool(stride_n=128, stride_h=128, stride_page=8192)), SHAPE), (write, dict(kv=pool(dtype=h.DTYPE_FP8_E4M3)), DTYPE),
+    (write, dict(sn=516), ALIGN), (write, dict(sh=4), ALIGN), (write, dict(kp=2 * FAKE + 8), ALIGN), (write, dict(pick=FAKE + 2), ALIGN),
+    (write, dict(slots=FAKE + 1), ALIGN),
+])
+def test_arguments_are_checked(call, bad, status):
+    assert call(**bad) == status
+
+
+def test_calls_with_nothing_to_do():
+    assert prefill(n_q=0, q=None, k=None, v=None, out=None, ws=None, cu_q=None, cu_k=None) == h.OK
+    assert write(tokens=0, k=None, v=None, slots=None) == h.OK and write(rows=0, k=None, v=None) == h.OK
+
+
+def test_workspace_sizes():
+    need = h.load().hippo_prefill_workspace_bytes
+    d = packed()
+    assert need(C.byref(d), 16640, 16640, 1, 0, 0) == 256                  # as many tiles as the card has compute units: nothing to merge
+    assert need(C.byref(d), 100, 100, 1, 0, 2) >= 2 * 100 * 28 * (128 + 2) * 4
+    assert need(C.byref(d), 64, 30000, 1, 1, 0) > 256
+    for bad in ((None, 1, 1, 1, 0, 0), (C.byref(packed(head_dim=60)), 1, 1, 1, 0, 0), (C.byref(d), -1, 1, 1, 0, 0), (C.byref(d), 1, 1, 0, 0, 0)):
+        assert need(*bad) == 0
+    n = need(C.byref(d), 1000, 1000, 3, 0, 5)
+    assert prefill(splits=5, ws_bytes=n - 1) == h.ERR_WORKSPACE_TOO_SMALL
+    need = h.load().hippo_tree_workspace_bytes
+    kv = cache()
+    n = need(C.byref(kv), 16, 2000, 0)
+    assert n > 256 and tree(ws_bytes=n - 1) == h.ERR_WORKSPACE_TOO_SMALL
+    assert need(C.byref(kv), 16, 2000, 1) == 256
+    assert need(None, 16, 2000, 0) == 0 and need(C.byref(kv), 0, 2000, 0) == 0 and need(C.byref(kv), 16, 15, 0) == 0
+
+
+def int32(*shape):
+    return torch.zeros(shape, dtype=torch.int32)
+
+
+def test_the_binding_refuses_tensors_it_would_misread():
+    q, k, v, cu = torch.zeros(10, 4, 64), torch.zeros(10, 2, 64), torch.zeros(10, 2, 64), int32(3)
+    f = h.hippo_prefill_attention
+    for args in ((q.bfloat16(), k, v, cu), (q, k, v.double(), cu), (q, k[:, :, :32], v[:, :, :32], cu), (q, k[:9], v[:9], cu), (q, k, v[:9], cu),
+                 (q, k, v, cu.long()), (q, k, v, int32(1)), (q, k, v, cu, int32(4)), (q, k, v, int32(3, 1)), (q[None], k, v, cu),
+                 (q.transpose(1, 2), k, v, cu), (q, k, v, int32(6)[::2])):
+        with pytest.raises(AssertionError):
+            f(*args)
+    with pytest.raises(TypeError):
+        f(q, k, v, [0, 5, 10])
+    with pytest.raises(AssertionError):
+        f(q, k, v, cu, out=torch.zeros(10, 4, 32))
+    kp, vp, table, lens = torch.zeros(7, 16, 2, 64), torch.zeros(7, 16, 2, 64), int32(2, 3), int32(2)
+    f = h.hippo_prefill_attention_paged
+    for args in ((q, kp, vp, table.long(), cu, lens), (q, kp, vp, table, int32(2), lens), (q, kp, vp, table, cu, int32(3)), (q, kp, vp[:6], table, cu, lens),
+                 (q, kp.bfloat16(), vp.bfloat16(), table, cu, lens), (q, kp, vp, int32(3), cu, lens), (q[:, :, :32], kp, vp, table, cu, lens),
+                 (q, kp, vp, int32(3, 2).T, cu, lens)):
+        with pytest.raises(AssertionError):
+            f(*args)
+    t, kc, vc, parents = torch.zeros(2, 5, 4, 64), torch.zeros(2, 2, 30, 64), torch.zeros(2, 2, 30, 64), int32(2, 5)
+    f = h.hippo_tree_attention
+    for args in ((t, kc, vc, int32(2, 4), 3), (t, kc, vc, int32(3, 5), 3), (t, kc, vc, parents.long(), 3), (t, kc, vc, parents, -1), (t, kc, vc, parents, int32(3)),
+                 (t, kc, vc, parents, lens.long()), (t[:1], kc, vc, parents[:1], 3), (t.bfloat16(), kc, vc, parents, 3), (t, kc, vc[:, :, :29], parents, 3),
+                 (t, kc, vc, int32(2, 10)[:, ::2], 3), (t.transpose(1, 2), kc, vc, parents, 3)):
+        with pytest.raises(AssertionError):
+            f(*args)
+    f = h.hippo_tree_attention_paged
+    for args in ((t, kp, vp, int32(3, 3), parents, 3), (t, kp, vp, table.float(), parents, 3), (t, kp, vp[:, :8], table, parents, 3)):
+        with pytest.raises(AssertionError):
+            f(*args)
+    f = h.hippo_plan_pages
+    free, n_free = int32(9), int32(1)
+    for args in ((lens, int32(3), table, free, n_free, 16, 8), (lens, lens.long(), table, free, n_free, 16, 8), (lens, lens, int32(3, 3), free, n_free, 16, 8),
+                 (lens, lens, table, free[None], n_free, 16, 8), (lens, lens, table, free, int32(2), 16, 8), (lens, lens, table, free, n_free, 16, -1),
+                 (lens, lens, int32(3, 2).T, free, n_free, 16, 8)):
+        with pytest.raises(AssertionError):
+            f(*args)
+    with pytest.raises(AssertionError):
+        f(lens, lens, table, free, n_free, 16, 8, slots_out=int32(7))
+    f = h.hippo_write_kv_paged
+    slots = int32(10)
+    for args in ((k, v, slots.long(), kp, vp), (k, v[:9], slots, kp, vp), (k, v, slots, kp, vp[:6]), (k.bfloat16(), v.bfloat16(), slots, kp, vp),
+                 (k[:, :1], v[:, :1], slots, kp, vp), (k, v, slots, kp, vp, int32(9)), (k, v, int32(20)[::2], kp, vp)):
+        with pytest.raises(AssertionError):
+            f(*args)
+
+
+def test_tensors_have_to_lie_on_the_current_device():
+    q, k, cu = torch.zeros(10, 4, 64), torch.zeros(10, 2, 64), int32(3)
+    kp, table, lens = torch.zeros(7, 16, 2, 64), int32(2, 3), int32(2)
+    t, kc, parents = torch.zeros(2, 5, 4, 64), torch.zeros(2, 2, 30, 64), int32(2, 5)
+    for call in (lambda: h.hippo_prefill_attention(q, k, k, cu), lambda: h.hippo_prefill_attention_paged(q, kp, kp, table, cu, lens),
+                 lambda: h.hippo_tree_attention(t, kc, kc, parents, 3), lambda: h.hippo_tree_attention_paged(t, kp, kp, table, parents, lens),
+                 lambda: h.hippo_plan_pages(lens, lens, table, int32(9), int32(1), 16, 8), lambda: h.hippo_write_kv_paged(k, k, int32(10), kp, kp)):
+        with pytest.raises(AssertionError, match=re.escape("tensors lie on the current device")):
+            call()
