@@ -365,39 +365,51 @@ int plan_spec(int batch, int gamma, int vocab, int dtype, SpecPlan* pl) {
 // ---- attention of many rows: planning -------------------------------------------------------------
 constexpr int kMaxRowSplits = 64;   // the merge keeps a split's statistics in a lane
 
-// What a block of RB x 32 rows takes for 64 tokens, in us, measured alone on its compute unit (64 nodes over 16640 rows of 28 heads x
-// 128, 32 over 33280 of 14 x 64; fp32 64 over 16640 of 28 x 128, 16 over 2000 of 14 x 64).
-double rows_pace(int dtype, int head_dim, int rb) {
-  static const double pace[2][2][4] = {{{1.45, 2.3, 4.4, 8.2}, {0, 4.8, 8.2, 16.0}}, {{0.375, 0.33, 0.65, 1.01}, {0.61, 0.80, 0.79, 1.40}}};
-  return pace[dtype == HIPPO_DTYPE_BF16][head_dim == 128][rb == 1 ? 0 : rb == 2 ? 1 : rb == 4 ? 2 : 3];
-}
+// The blocks that a call can be cut into, and what one takes for 64 tokens, in us: measured alone on its compute unit (64 nodes over 16640
+// rows of 28 heads x 128, 32 over 33280 of 14 x 64; fp32 64 over 16640 of 28 x 128, 16 over 2000 of 14 x 64); of pairs also beside another
+// one, so that prompts from 32 to 16384 rows take the block with which they were faster.  0: there is none (fp32 x 64: pairs take 4 to
+// 40 % less than 256 rows a block).
+struct RowsBlock {
+  int rb;
+  bool pair;
+  double fixed, fixed_tree;    // its start, its masked stages and its end (trees: 2 to 8 nodes over 25 to 2876 rows)
+  double alone[2][2];          // [bf16][head_dim 128]
+  double beside[2][2];         // pairs: beside another one
+};
+const RowsBlock kRowsBlocks[] = {{8, false, 7.0, 5.5, {{0, 16.0}, {1.01, 1.40}}, {}},
+                                 {4, false, 7.0, 5.0, {{4.4, 8.2}, {0.65, 0.79}}, {}},
+                                 {4, true, 3.5, 4.5, {{4.6, 0}, {1.05, 1.15}}, {{8.1, 0}, {1.07, 1.85}}},
+                                 {2, false, 4.5, 4.9, {{2.3, 4.8}, {0.33, 0.80}}, {}},
+                                 {1, false, 4.0, 4.3, {{1.45, 0}, {0.375, 0.61}}, {}}};
 
 // How to cut a call: the rows of a block and the blocks that share a tile's tokens, by the time that they are going to take.
-//   a block: kBlockUs (trees: kTreeBlockUs) besides its tokens (its start, its masked stages and its end), one on a compute unit at a time
+//   a block: its fixed time besides its tokens, one on a compute unit at a time, or two
 //   a call:  the longest block of all, or all blocks on all compute units: as many rounds as that takes, a last one in proportion where
 //            the blocks' sizes are spread (short ones fill it up)
 //   blocks that share tiles: a merge, kMergeUs and kMergeMbUs for a megabyte of parts
 // rows: query rows of a KV head of one sequence, on average; seen, seen_least: the tokens that the last and the first of them see; tree:
 // a sequence's tiles are its own; num_splits: the caller's.
-constexpr double kTreeBlockUs = 4.0, kBlockUs[] = {4.0, 4.5, 7.0, 7.0}, kMergeUs = 4.0, kMergeMbUs = 0.9;       // rb 1, 2, 4, 8
+constexpr double kMergeUs = 2.8, kMergeMbUs = 0.9;
 void cut_rows(RowsPlan* pl, int dtype, int head_dim, double rows, double n_seqs, double seen, double seen_least, bool tree, int Hkv,
               double part_bytes, int num_splits) {
   static const int splits[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64};
   double best = 1e30;
-  for (int rb = 8; rb >= 1; rb /= 2) {
-    const double pace = rows_pace(dtype, head_dim, rb), block = tree ? kTreeBlockUs : kBlockUs[rb == 1 ? 0 : rb == 2 ? 1 : rb == 4 ? 2 : 3];
-    if (pace == 0) continue;
-    const double tiles = n_seqs * (tree ? ceil(rows / (32 * rb)) : std::max(1.0, rows / (32 * rb) + 0.5)) * Hkv;
+  for (const RowsBlock& of : kRowsBlocks) {
+    const bool bf16 = dtype == HIPPO_DTYPE_BF16, d128 = head_dim == 128;
+    const double alone = of.alone[bf16][d128], block = tree ? of.fixed_tree : of.fixed;
+    if (alone == 0) continue;
+    const double tiles = n_seqs * (tree ? ceil(rows / (32 * of.rb)) : std::max(1.0, rows / (32 * of.rb) + 0.5)) * Hkv;
     for (int S : splits) {
       if (num_splits > 0 ? S != 1 : S > 1 && seen < 64.0 * S) break;
-      const double n = num_splits > 0 ? num_splits : S;
+      const double n = num_splits > 0 ? num_splits : S, pace = of.pair && tiles * n > kNumCU ? of.beside[bf16][d128] : alone;
       const double longest = block + seen / 64 / n * pace, mean = block + (seen + seen_least) / 128 / n * pace;
-      const double rounds = tiles * n / kNumCU, alike = (block + seen_least / 64 / n * pace) / longest;
+      const double rounds = tiles * n / (of.pair ? 2 * kNumCU : kNumCU), alike = (block + seen_least / 64 / n * pace) / longest;
       const double t = std::max(longest, (rounds + alike * (ceil(rounds) - rounds)) * mean) +
                        (n > 1 ? kMergeUs + kMergeMbUs * n * part_bytes * 1e-6 : 0.0);
       if (t < best * 0.999) {
         best = t;
-        pl->rb = rb;
+        pl->rb = of.rb;
+        pl->pair = of.pair;
         pl->S = S;
       }
     }
@@ -1122,7 +1134,7 @@ static int prefill_entry(const void* q, int32_t total_q, const void* k, const vo
   }
   p.scale_log2 = scale_or_default(softmax_scale, desc->head_dim);
   carve_rows(&p, pl, workspace);
-  const hipError_t e = launch_prefill(p, pl.rb, desc->dtype, desc->head_dim, static_cast<hipStream_t>(stream));
+  const hipError_t e = launch_prefill(p, pl, desc->dtype, desc->head_dim, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? HIPPO_OK : HIPPO_ERR_HIP;
 }
 
@@ -1184,7 +1196,7 @@ static int tree_entry(const void* q, int32_t n_nodes, const void* k, const void*
   }
   p.scale_log2 = scale_or_default(softmax_scale, kv->head_dim);
   carve_rows(&p, pl, workspace);
-  const hipError_t e = launch_tree(p, pl.rb, kv->dtype, kv->head_dim, static_cast<hipStream_t>(stream));
+  const hipError_t e = launch_tree(p, pl, kv->dtype, kv->head_dim, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? HIPPO_OK : HIPPO_ERR_HIP;
 }
 

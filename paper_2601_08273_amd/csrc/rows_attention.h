@@ -53,9 +53,11 @@ struct RowsParams {
   float* part_l;
 };
 
-// how a call is cut: rows of a block (RB x 32), blocks that share a tile, see RowsParams
+// how a call is cut: rows of a block (RB x 32), two such blocks on a compute unit, blocks that share a tile, see RowsParams
 struct RowsPlan {
-  int rb, S, n_tiles, deal;
+  int rb;
+  bool pair;
+  int S, n_tiles, deal;
   size_t off_m, off_l, bytes;
 };
 
@@ -242,7 +244,7 @@ __device__ __forceinline__ int tree_deal(const RowsParams& p) {
 }
 
 template <typename T, int D, int RB, int TG, int TW, int NST, bool PAGED, bool TREE>
-__global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
+__global__ __launch_bounds__(RB * TG * 64, RB == 4 && TG == 1 ? (D * sizeof(T) == 128 ? 3 : 2) : RB * TG / 4) void attn_rows(RowsParams p) {
   using Tile = RowsTile<T, D>;
   using SM = RowsSmem<T, D, RB, TG, TW, NST>;
   constexpr bool F32 = sizeof(T) == 4;
@@ -513,7 +515,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
     const rows_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(ROWS_LDS(rows_s16x4, (Vt + v_off) ^ (64 * db + 32)) + (16 * ks + 8) * ROWB / 8);
     return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   };
-  auto token_of = [&](int e) ROWS_INLINE { return e / 16 * 32 + e % 16 / 4 * 8 + 4 * h + e % 4; };
+  auto bit_of = [](int e) ROWS_INLINE { return e % 16 / 4 * 8 + e % 4; };         // token of logit e: e / 16 * 32 + bit_of(e) + 4 h
   const unsigned v32_off = 4 * h * ROWB + (((j >> 2) ^ (h << 3)) * 16) + (j & 3) * 4;
   auto v_f32 = [&](unsigned Vt, int db, int e) ROWS_INLINE {            // (the swizzle of the token's row, apart from its part in v32_off, and 8 db pieces)
     const unsigned flip = 128 * db + ((e % 16 / 4 & 1) << 6 | (e & 3) << 4);
@@ -546,7 +548,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
   };
   // The same where some rows do not see some tokens and V holds infinities or NaN: 0 times one of them would reach the rows that do not
   // see it.  Such entries go as zeros, and each kind is counted for each row among the tokens that it sees.  Rare: written to be short.
-  auto values_odd = [&](unsigned Vt, const f32x16 (&s)[TB], const unsigned (&pk)[SN / 2], unsigned vis) ROWS_INLINE {
+  auto values_odd = [&](unsigned Vt, const f32x16 (&s)[TB], const unsigned (&pk)[SN / 2], const unsigned (&vis)[TB]) ROWS_INLINE {
 #pragma unroll 1
     for (int db = 0; db < DB; ++db) {
       f32x16 sum;
@@ -561,7 +563,7 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
             const float x = v_f32(Vt, db, e);
             const float a = kind == 0 ? (fabsf(x) < INFINITY ? x : 0.f)
                                       : (kind == 1 ? x == INFINITY : kind == 2 ? x == -INFINITY : x != x) ? 1.f : 0.f;
-            n = __builtin_amdgcn_mfma_f32_32x32x2f32(a, kind == 0 ? s[e / 16][e % 16] : (vis >> e) & 1 ? 1.f : 0.f, n, 0, 0, 0);
+            n = __builtin_amdgcn_mfma_f32_32x32x2f32(a, kind == 0 ? s[e / 16][e % 16] : vis[e / 16] & 1u << bit_of(e) ? 1.f : 0.f, n, 0, 0, 0);
           }
         } else {
 #pragma unroll
@@ -578,7 +580,8 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
                 const bool hit = kind == 1 ? v == 0x7f80u : kind == 2 ? v == 0xff80u : (v & 0x7fffu) > 0x7f80u;
                 a[i] |= (kind == 0 ? (finite ? v : 0u) : hit ? one : 0u) << (16 * y);
               }
-              const unsigned seen = ((vis >> (8 * ks + 2 * i)) & 1 ? 0x3f80u : 0u) | ((vis >> (8 * ks + 2 * i + 1)) & 1 ? 0x3f800000u : 0u);
+              const int e = 8 * ks + 2 * i;
+              const unsigned seen = (vis[e / 16] & 1u << bit_of(e) ? 0x3f80u : 0u) | (vis[e / 16] & 2u << bit_of(e) ? 0x3f800000u : 0u);
               w[i] = kind == 0 ? pk[4 * ks + i] : seen;
             }
             n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, w), n, 0, 0, 0);
@@ -746,21 +749,24 @@ __global__ __launch_bounds__(RB * TG * 64) void attn_rows(RowsParams p) {
     unsigned pk[SN / 2];
     logits(k_tile(si), s);
     look_for_odd(si);
-    const int n0 = (s_lo + si) * ST + tg * TW;
-    unsigned vis = 0;
+    // which of the lane's tokens its row sees: bit bit_of(e) of token block e / 16.  (A question for each token by itself became branches:
+    // 2.3 us a stage of a tree.)
+    unsigned vis[TB];
 #pragma unroll
-    for (int e = 0; e < SN; ++e) {
-      const int n = n0 + token_of(e);
-      bool see;
+    for (int tb = 0; tb < TB; ++tb) {
+      const int n0 = (s_lo + si) * ST + tg * TW + tb * 32 + 4 * h;
       if constexpr (TREE) {
-        const int node = n - off;
-        see = node < 0 ? sees != 0 : node < 64 && ((sees >> (node & 63)) & 1);
+        const int node = n0 - off, before = min(max(-node, 0), 31);     // rows of the context among the block's tokens
+        unsigned w = (unsigned)(sees >> min(max(node, 0), 63));
+        if (node >= 64) w = 0;
+        vis[tb] = w << before | (sees != 0 ? (1u << before) - 1 : 0u);
       } else {
-        see = n <= lim;
+        const int more = lim - n0;                          // (only bits up to 27 are asked for)
+        vis[tb] = more < 0 ? 0u : (2u << min(more, 30)) - 1;
       }
-      if (see) vis |= 1u << e;
-      else s[e / 16][e % 16] = -INFINITY;
     }
+#pragma unroll
+    for (int e = 0; e < SN; ++e) s[e / 16][e % 16] = vis[e / 16] & 1u << bit_of(e) ? s[e / 16][e % 16] : -INFINITY;
     refer(s);
     weights(s, pk);
     wait_lds();
@@ -924,37 +930,45 @@ __global__ __launch_bounds__(64) void rows_combine(RowsParams p) {
   }
 }
 
-// what a block of RB row blocks looks like: token groups, tokens of a wave in a stage, stages
-template <typename T, int D, int RB>
+// What a block of RB row blocks looks like: token groups, tokens of a wave in a stage, stages.  PAIR: one that leaves room for a second
+// on its compute unit (bf16 x 64: two more), which works while the first starts, waits for its first rows or writes its last ones: for
+// many blocks of few stages.  (200 prompts of 128 rows, 28 heads x 128: 177 us with 256 rows a block, 126 with 128 in pairs; of 14 x 64 61 and 36, in fp32
+// 177 and 101; 16 of 2048, 28 x 128: 541 and 560.)
+template <typename T, int D, int RB, bool PAIR>
 struct RowsShape {
   static constexpr bool F32 = sizeof(T) == 4, WIDE = D * sizeof(T) > 256;      // WIDE: rows of 512 bytes
-  static constexpr int TG = RB == 8 ? 1 : RB == 4 || WIDE ? 2 : RB == 2 && D == 128 ? 2 : 4;
+  static constexpr bool kThere = PAIR ? RB == 4 && !WIDE : RB == 8 ? !F32 || WIDE : RB > 1 || !WIDE;   // (as the host has them)
+  static constexpr int TG = RB == 8 || PAIR ? 1 : RB == 4 || WIDE ? 2 : RB == 2 && D == 128 ? 2 : 4;
   static constexpr int TW = RB == 8 && !F32 ? 64 : 32;
   static constexpr int STAGE = 2 * TG * TW * D * (int)sizeof(T);
   static constexpr int NST = 4 * STAGE <= 128 * 1024 ? 4 : 2;
 };
 
-template <typename T, int D, int RB, bool PAGED, bool TREE>
+template <typename T, int D, int RB, bool PAIR, bool PAGED, bool TREE>
 static hipError_t launch_rows_rb(const RowsParams& p, hipStream_t st) {
-  using Sh = RowsShape<T, D, RB>;
-  constexpr int smem = RowsSmem<T, D, RB, Sh::TG, Sh::TW, Sh::NST>::total();
-  constexpr auto kernel = attn_rows<T, D, RB, Sh::TG, Sh::TW, Sh::NST, PAGED, TREE>;
-  const hipError_t e = allow_dynamic_lds<kernel>(smem);
-  if (e != hipSuccess) return e;
-  const dim3 grid = p.deal > 0 ? dim3((unsigned)p.tiles_per_seq * p.Hkv, p.deal) : dim3((unsigned)p.n_tiles * p.Hkv, p.S);
-  hipLaunchKernelGGL(kernel, grid, dim3(RB * Sh::TG * 64), smem, st, p);
-  return hipGetLastError();
+  using Sh = RowsShape<T, D, RB, PAIR>;
+  if constexpr (!Sh::kThere) {
+    return hipErrorInvalidValue;
+  } else {
+    constexpr int smem = RowsSmem<T, D, RB, Sh::TG, Sh::TW, Sh::NST>::total();
+    static_assert(!PAIR || 2 * smem <= 160 * 1024, "");
+    constexpr auto kernel = attn_rows<T, D, RB, Sh::TG, Sh::TW, Sh::NST, PAGED, TREE>;
+    const hipError_t e = allow_dynamic_lds<kernel>(smem);
+    if (e != hipSuccess) return e;
+    const dim3 grid = p.deal > 0 ? dim3((unsigned)p.tiles_per_seq * p.Hkv, p.deal) : dim3((unsigned)p.n_tiles * p.Hkv, p.S);
+    hipLaunchKernelGGL(kernel, grid, dim3(RB * Sh::TG * 64), smem, st, p);
+    return hipGetLastError();
+  }
 }
 
 template <typename T, int D, bool PAGED, bool TREE>
-static hipError_t launch_rows_d(const RowsParams& p, int rb, hipStream_t st) {
+static hipError_t launch_rows_d(const RowsParams& p, const RowsPlan& pl, hipStream_t st) {
   hipError_t e;
-  switch (rb) {
-    case 8: e = launch_rows_rb<T, D, 8, PAGED, TREE>(p, st); break;
-    case 4: e = launch_rows_rb<T, D, 4, PAGED, TREE>(p, st); break;
-    case 2: e = launch_rows_rb<T, D, 2, PAGED, TREE>(p, st); break;
-    case 1:
-      if constexpr (!RowsShape<T, D, 1>::WIDE) { e = launch_rows_rb<T, D, 1, PAGED, TREE>(p, st); break; }
+  switch (pl.rb) {
+    case 8: e = launch_rows_rb<T, D, 8, false, PAGED, TREE>(p, st); break;
+    case 4: e = pl.pair ? launch_rows_rb<T, D, 4, true, PAGED, TREE>(p, st) : launch_rows_rb<T, D, 4, false, PAGED, TREE>(p, st); break;
+    case 2: e = launch_rows_rb<T, D, 2, false, PAGED, TREE>(p, st); break;
+    case 1: e = launch_rows_rb<T, D, 1, false, PAGED, TREE>(p, st); break;
     default: return hipErrorInvalidValue;
   }
   if (e != hipSuccess || p.S == 1) return e;
@@ -963,17 +977,17 @@ static hipError_t launch_rows_d(const RowsParams& p, int rb, hipStream_t st) {
 }
 
 template <bool TREE>
-static hipError_t launch_rows(const RowsParams& p, int rb, int dtype, int head_dim, hipStream_t st) {
+static hipError_t launch_rows(const RowsParams& p, const RowsPlan& pl, int dtype, int head_dim, hipStream_t st) {
   const bool paged = p.block_table != nullptr, bf16 = dtype == HIPPO_DTYPE_BF16;
   if (head_dim == 128) {
-    if (bf16) return paged ? launch_rows_d<uint16_t, 128, true, TREE>(p, rb, st) : launch_rows_d<uint16_t, 128, false, TREE>(p, rb, st);
-    return paged ? launch_rows_d<float, 128, true, TREE>(p, rb, st) : launch_rows_d<float, 128, false, TREE>(p, rb, st);
+    if (bf16) return paged ? launch_rows_d<uint16_t, 128, true, TREE>(p, pl, st) : launch_rows_d<uint16_t, 128, false, TREE>(p, pl, st);
+    return paged ? launch_rows_d<float, 128, true, TREE>(p, pl, st) : launch_rows_d<float, 128, false, TREE>(p, pl, st);
   }
-  if (bf16) return paged ? launch_rows_d<uint16_t, 64, true, TREE>(p, rb, st) : launch_rows_d<uint16_t, 64, false, TREE>(p, rb, st);
-  return paged ? launch_rows_d<float, 64, true, TREE>(p, rb, st) : launch_rows_d<float, 64, false, TREE>(p, rb, st);
+  if (bf16) return paged ? launch_rows_d<uint16_t, 64, true, TREE>(p, pl, st) : launch_rows_d<uint16_t, 64, false, TREE>(p, pl, st);
+  return paged ? launch_rows_d<float, 64, true, TREE>(p, pl, st) : launch_rows_d<float, 64, false, TREE>(p, pl, st);
 }
 
-hipError_t launch_prefill(const RowsParams& p, int rb, int dtype, int head_dim, hipStream_t st);
-hipError_t launch_tree(const RowsParams& p, int rb, int dtype, int head_dim, hipStream_t st);
+hipError_t launch_prefill(const RowsParams& p, const RowsPlan& pl, int dtype, int head_dim, hipStream_t st);
+hipError_t launch_tree(const RowsParams& p, const RowsPlan& pl, int dtype, int head_dim, hipStream_t st);
 
 }  // namespace hippo

@@ -3,8 +3,8 @@
 
 namespace hippo {
 
-hipError_t launch_tree(const RowsParams& p, int rb, int dtype, int head_dim, hipStream_t st) {
-  return launch_rows<true>(p, rb, dtype, head_dim, st);
+hipError_t launch_tree(const RowsParams& p, const RowsPlan& pl, int dtype, int head_dim, hipStream_t st) {
+  return launch_rows<true>(p, pl, dtype, head_dim, st);
 }
 
 }  // namespace hippo

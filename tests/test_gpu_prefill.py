@@ -190,7 +190,7 @@ def pages_of(g, k, v, lens, page, spare=3, dtype=torch.int32):
 @pytest.mark.parametrize("page", [16, 64, 256])
 @pytest.mark.parametrize("splits", [0, 5])
 def test_paged(hippo, dtype, heads, page, splits):
-    """bit for bit what the packed call gives, whatever the pages hold behind a sequence's last row"""
+    """whatever the pages hold behind a sequence's last row"""
     H, Hkv, d = heads
     lens_q, lens_k = [60, 1, 0, 129, 16], [800, 65, 30, 129, 16]
     q, k, v = make(lens_q, lens_k, H, Hkv, d, dtype, 14)
@@ -286,7 +286,8 @@ def test_every_tile_size(hippo, kernels, dtype, heads, least):
             cu = offsets(lens)
             call = lambda: hippo.hippo_prefill_attention(q, k, v, cu, want_lse=True)      # noqa: E731
             out, lse = call()
-            sizes |= {int(name.split("attn_rows")[1].split("ELi")[1]) for name in kernels(call) if "attn_rows" in name}
+            # row blocks and token groups of a block; one group of four: two such blocks on a compute unit
+            sizes |= {tuple(int(x) for x in name.split("attn_rows")[1].split("ELi")[1:3]) for name in kernels(call) if "attn_rows" in name}
             first, last = slice(0, n), slice((seqs - 1) * n, seqs * n)
             for at in (first, last):
                 ref = reference(q[at], k[at], v[at], [n], [n])
@@ -297,7 +298,29 @@ def test_every_tile_size(hippo, kernels, dtype, heads, least):
                 q2, k2, v2 = (torch.cat([x[first], x[n:-n], x[first]]) for x in (q, k, v))
                 again = hippo.hippo_prefill_attention(q2, k2, v2, cu)
                 assert torch.equal(again[first], again[last])
-    assert sizes == {1, 2, 4, 8} - ({1} if least == 2 else set()), sizes
+    assert {rb for rb, _ in sizes} >= {1, 2, 4} - ({1} if least == 2 else set()), sizes
+    assert ((4, 1) in sizes) == (least == 1), sizes
+
+
+@pytest.mark.parametrize("dtype,heads,lens,block", [
+    ("bf16", (28, 4, 128), [2500, 2561], (8, 1)), ("bf16", (14, 2, 64), [8191], (8, 1)), ("fp32", (28, 4, 128), [700] * 8, (8, 1)),
+    ("bf16", (28, 4, 128), [2049], (4, 2)), ("bf16", (14, 2, 64), [4500], (4, 2)), ("fp32", (28, 4, 64), [2500], (4, 2)),
+    ("bf16", (14, 2, 64), [1500] * 9, (4, 1)), ("bf16", (28, 4, 128), [511] * 60, (4, 1)), ("fp32", (8, 2, 64), [900] * 40, (4, 1))])
+def test_longer_prompts_of_every_block(hippo, kernels, dtype, heads, lens, block):
+    """row blocks and token groups of a block, see above"""
+    H, Hkv, d = heads
+    q, k, v = make(lens, lens, H, Hkv, d, dtype, 61)
+    cu = offsets(lens)
+    call = lambda: hippo.hippo_prefill_attention(q, k, v, cu, want_lse=True)              # noqa: E731
+    out, lse = call()
+    assert {tuple(int(x) for x in name.split("attn_rows")[1].split("ELi")[1:3]) for name in kernels(call) if "attn_rows" in name} == {block}
+    # rows at both ends and around the middle of the last sequence, each as the last row of a shorter one
+    start, n = sum(lens[:-1]), lens[-1]
+    for i in (0, 1, 255, n // 2, n // 2 + 37, n - 2, n - 1):
+        at, upto = slice(start + i, start + i + 1), slice(start, start + i + 1)
+        ref = reference(q[at], k[upto], v[upto], [1], [i + 1])
+        check(out[at], ref[0], ref[1], i)
+        check_lse(lse[:, at], ref[2], ref[3], i)
 
 
 def test_two_calls_at_once(hippo):

@@ -82,6 +82,23 @@ def test_splits(hippo, dtype, splits):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("H,Hkv,d", [(2, 1, 64), (1, 1, 128), (14, 2, 64), (8, 1, 128)])
+@pytest.mark.parametrize("n,first", [(64, 0), (64, 66), (37, 100)])
+def test_a_tree_anywhere_in_a_stage(hippo, dtype, H, Hkv, d, n, first):
+    """contexts of 66 lengths in a row, a last node that is none and whose rows of K and V are no numbers"""
+    ctx = list(range(first, first + 66))
+    q, k, v = make(66, n, max(ctx) + n, H, Hkv, d, dtype, first + n)
+    parents = [some_tree(n, 10 + b, padding=1) for b in range(66)]
+    clean_k, clean_v = k.clone(), v.clone()
+    for b, c in enumerate(ctx):
+        if b % 3:
+            k[b, :, c + n - 1:] = float("nan")
+            v[b, :, c + n - 1:] = float("nan") if b % 3 == 1 else float("inf")
+    got = hippo.hippo_tree_attention(q, k, v, int32(parents), int32(ctx), want_lse=True)
+    verify(got, reference(q, clean_k, clean_v, parents, ctx))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("n", [1, 6, 64])
 def test_a_chain_is_a_verification(hippo, dtype, n):
     """a tree without branches sees what hippo_verify_attention's rows see"""
