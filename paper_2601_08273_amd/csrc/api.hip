@@ -389,7 +389,7 @@ const RowsBlock kRowsBlocks[] = {{8, false, 7.0, 5.5, {{0, 16.0}, {1.01, 1.40}},
 //   blocks that share tiles: a merge, kMergeUs and kMergeMbUs for a megabyte of parts
 // rows: query rows of a KV head of one sequence, on average; seen, seen_least: the tokens that the last and the first of them see; tree:
 // a sequence's tiles are its own; num_splits: the caller's.
-constexpr double kMergeUs = 2.8, kMergeMbUs = 0.9;
+constexpr double kMergeUs = 2.8, kMergeMbUs = 0.75;
 void cut_rows(RowsPlan* pl, int dtype, int head_dim, double rows, double n_seqs, double seen, double seen_least, bool tree, int Hkv,
               double part_bytes, int num_splits) {
   static const int splits[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64};
