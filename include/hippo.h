@@ -490,8 +490,7 @@ int hippo_token_logprobs(const void* logits, int32_t dtype, int64_t stride_row, 
  * [total_q, H, d] contiguous, dtype desc->dtype (F32 or BF16); lse_out optional [H, total_q] fp32.  softmax_scale <= 0 means
  * 1/sqrt(d).  num_splits: blocks that share a tile of query rows (up to 64), 0 = library's choice; the result does not depend on it beyond
  * rounding.  fp32 throughout, but that over bf16 the probabilities are rounded to bf16 before their product with V (and summed as
- * rounded).  total_q = 0 does nothing.  Workspace: hippo_prefill_workspace_bytes with
- * paged 0.
+ * rounded).  total_q = 0 does nothing.  Workspace: hippo_prefill_workspace_bytes with paged 0.
  * Errors: NULL_ARG, BAD_SHAPE (also more than 65535 sequences, 2^30 query rows times heads), BAD_DTYPE, BAD_ALIGN,
  *         WORKSPACE_TOO_SMALL, HIP.
  */
@@ -510,8 +509,8 @@ int hippo_prefill_attention(const void* q, int32_t total_q, const void* k, const
 
 /*
  * The same over a paged cache (hippo_paged_kv_desc, with batch = n_seqs) that already holds the new rows: sequence b's key row n lies
- * where block_table says, and len_k = kv_lens[b] (int32 on the device, cut off at max_pages * page_size).  Workspace:
- * hippo_prefill_workspace_bytes with total_k = max_pages * page_size and paged 1.
+ * where block_table says, and len_k = kv_lens[b] (int32 on the device, cut off at max_pages * page_size).  Pools of at most 2^22 pages, here and in
+ * the tree's and the write's calls.  Workspace: hippo_prefill_workspace_bytes with total_k = max_pages * page_size and paged 1.
  */
 int hippo_prefill_attention_paged(const void* q, int32_t total_q, int64_t q_stride_n, int64_t q_stride_h,
                                   const void* k_pool, const void* v_pool, const int32_t* block_table,

@@ -14,6 +14,10 @@
 // A block has RB x TG waves: wave (rb, tg) owns rows 32 rb .. 32 rb + 31 of the block's tile and of every stage tokens
 // tg TW .. tg TW + TW - 1; the TG states of a row block meet in the LDS at the end.  K and V reach the LDS without registers in between,
 // NST stages deep.  A sequence's stages may be dealt to S blocks (few rows over many tokens): their states go to a merge.
+//
+// What bounds it: long prompts and wide trees the matrix unit, at the clock that its power leaves (16640 rows x 28 heads x 128: 1716 us,
+// 1.17 PFLOP/s, where a library product of 16384^3 reaches 1.35); few rows the cache's bytes (16 nodes x 28 heads over 16640 rows: 18 us for
+// 34 MB) and the merge's launch; short prompts a chain of trips to memory of some 4 us, beside which other blocks should run.
 #pragma once
 
 #include <type_traits>
@@ -865,7 +869,8 @@ __global__ __launch_bounds__(RB * TG * 64, RB == 4 && TG == 1 ? (D * sizeof(T) =
 }
 
 // Merge of the S blocks that shared a tile: a wave takes one (token, query head), D / 4 lanes a split's 16-byte pieces, so that 256 / D
-// splits are read at once, four of them in a row under way.  (Few rows: a block a row puts them on as many compute units.)
+// splits are read at once, four of them in a row under way.  (Few rows: a block a row puts them on as many compute units.)  Bound by the
+// parts' bytes (3 x 2091 rows x 64 heads x 128: 66 us for 240 MB), few rows by two trips to memory (32 x 16 x 28: 4.6 us).
 template <typename T, int D, bool TREE>
 __global__ __launch_bounds__(64) void rows_combine(RowsParams p) {
   constexpr int LPR = D / 4, GROUPS = 64 / LPR, PF = 4;
