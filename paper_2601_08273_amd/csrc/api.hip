@@ -365,22 +365,27 @@ int plan_spec(int batch, int gamma, int vocab, int dtype, SpecPlan* pl) {
 // ---- attention of many rows: planning -------------------------------------------------------------
 constexpr int kMaxRowSplits = 64;   // the merge keeps a split's statistics in a lane
 
-// The blocks that a call can be cut into, and what one takes for 64 tokens, in us: measured alone on its compute unit (64 nodes over 16640
-// rows of 28 heads x 128, 32 over 33280 of 14 x 64; fp32 64 over 16640 of 28 x 128, 16 over 2000 of 14 x 64); of pairs also beside another
-// one, so that prompts from 32 to 16384 rows take the block with which they were faster.  0: there is none (fp32 x 64: pairs take 4 to
-// 40 % less than 256 rows a block).
+// The blocks that a call can be cut into: row blocks, made in pairs (launch_rows_rb's).
 struct RowsBlock {
   int rb;
   bool pair;
-  double fixed, fixed_tree;    // its start, its masked stages and its end (trees: 2 to 8 nodes over 25 to 2876 rows)
-  double alone[2][2];          // [bf16][head_dim 128]
-  double beside[2][2];         // pairs: beside another one
 };
-const RowsBlock kRowsBlocks[] = {{8, false, 7.0, 5.5, {{0, 16.0}, {1.01, 1.40}}, {}},
-                                 {4, false, 7.0, 5.0, {{4.4, 8.2}, {0.65, 0.79}}, {}},
-                                 {4, true, 3.5, 4.5, {{4.6, 0}, {1.05, 1.15}}, {{8.1, 0}, {1.07, 1.85}}},
-                                 {2, false, 4.5, 4.9, {{2.3, 4.8}, {0.33, 0.80}}, {}},
-                                 {1, false, 4.0, 4.3, {{1.45, 0}, {0.375, 0.61}}, {}}};
+const RowsBlock kRowsBlocks[] = {{8, false}, {4, false}, {4, true}, {2, false}, {1, false}};
+// What a block takes, in us: `fixed` (its start, its masked stages and its end) and `pace` for 64 tokens; beside another one on its compute unit,
+// where it leaves room for one (pace_beside 0: it does not).  Pace 0: there is no such block (fp32 x 64: pairs take 4 to 40 % less than 256
+// rows a block).  bf16: fitted to 492 calls of prompts (1 to 200 of 4 to 16384 rows, 1 to 4096 over up to 30000) and 112 of trees (1 to 128 of
+// 1 to 64 nodes over 30 to 30000 rows), each timed with every block and, trees, 1 to 48 blocks a tile: what this chooses takes 1 to
+// 2 % more than the best.  fp32: 64 nodes over 16640 rows of 28 x 128, 16 over 2000 of 14 x 64, prompts of 32 to 16384 rows.
+struct RowsCost {
+  double fixed, pace, fixed_beside, pace_beside;
+};
+const RowsCost kRowsCost[2][2][2][5] = {      // [trees][bf16][head_dim 128], as kRowsBlocks
+    {{{{0, 0}, {7.0, 4.4}, {3.5, 4.6, 3.5, 8.1}, {4.5, 2.3}, {4.0, 1.45}}, {{7.0, 16.0}, {7.0, 8.2}, {0, 0}, {4.5, 4.8}, {0, 0}}},
+     {{{7.0, 1.01}, {4.5, 0.65}, {3.7, 0.98, 3.0, 1.23}, {4.5, 0.32}, {4.0, 0.34}},
+      {{7.0, 1.40}, {6.5, 0.79}, {3.5, 1.37, 3.4, 1.61}, {3.6, 1.1, 3.5, 1.1}, {5.1, 0.80}}}},
+    {{{{0, 0}, {5.0, 4.4}, {4.5, 4.6, 4.5, 8.1}, {4.9, 2.3}, {4.3, 1.45}}, {{5.5, 16.0}, {5.0, 8.2}, {0, 0}, {4.9, 4.8}, {0, 0}}},
+     {{{6.2, 1.0}, {6.5, 0.62}, {4.7, 1.04, 2.5, 1.7}, {6.0, 0.36}, {5.2, 0.37}},
+      {{8.0, 1.38}, {7.0, 0.83}, {5.5, 1.23, 4.8, 2.15}, {5.4, 1.03, 5.4, 1.45}, {5.7, 0.69}}}}};
 
 // How to cut a call: the rows of a block and the blocks that share a tile's tokens, by the time that they are going to take.
 //   a block: its fixed time besides its tokens, one on a compute unit at a time, or two
@@ -389,21 +394,23 @@ const RowsBlock kRowsBlocks[] = {{8, false, 7.0, 5.5, {{0, 16.0}, {1.01, 1.40}},
 //   blocks that share tiles: a merge, kMergeUs and kMergeMbUs for a megabyte of parts
 // rows: query rows of a KV head of one sequence, on average; seen, seen_least: the tokens that the last and the first of them see; tree:
 // a sequence's tiles are its own; num_splits: the caller's.
-constexpr double kMergeUs = 2.8, kMergeMbUs = 0.75;
+constexpr double kMergeUs = 3.0, kMergeMbUs = 0.75;
 void cut_rows(RowsPlan* pl, int dtype, int head_dim, double rows, double n_seqs, double seen, double seen_least, bool tree, int Hkv,
               double part_bytes, int num_splits) {
   static const int splits[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64};
   double best = 1e30;
-  for (const RowsBlock& of : kRowsBlocks) {
-    const bool bf16 = dtype == HIPPO_DTYPE_BF16, d128 = head_dim == 128;
-    const double alone = of.alone[bf16][d128], block = tree ? of.fixed_tree : of.fixed;
-    if (alone == 0) continue;
+  for (int b = 0; b < 5; ++b) {
+    const RowsBlock& of = kRowsBlocks[b];
+    const RowsCost& cost = kRowsCost[tree][dtype == HIPPO_DTYPE_BF16][head_dim == 128][b];
+    if (cost.pace == 0) continue;
     const double tiles = n_seqs * (tree ? ceil(rows / (32 * of.rb)) : std::max(1.0, rows / (32 * of.rb) + 0.5)) * Hkv;
     for (int S : splits) {
       if (num_splits > 0 ? S != 1 : S > 1 && seen < 64.0 * S) break;
-      const double n = num_splits > 0 ? num_splits : S, pace = of.pair && tiles * n > kNumCU ? of.beside[bf16][d128] : alone;
-      const double longest = block + seen / 64 / n * pace, mean = block + (seen + seen_least) / 128 / n * pace;
-      const double rounds = tiles * n / (of.pair ? 2 * kNumCU : kNumCU), alike = (block + seen_least / 64 / n * pace) / longest;
+      const double n = num_splits > 0 ? num_splits : S;
+      const bool two = cost.pace_beside > 0, beside = two && tiles * n > kNumCU;
+      const double fixed = beside ? cost.fixed_beside : cost.fixed, pace = beside ? cost.pace_beside : cost.pace;
+      const double longest = fixed + seen / 64 / n * pace, mean = fixed + (seen + seen_least) / 128 / n * pace;
+      const double rounds = tiles * n / (two ? 2 * kNumCU : kNumCU), alike = (fixed + seen_least / 64 / n * pace) / longest;
       const double t = std::max(longest, (rounds + alike * (ceil(rounds) - rounds)) * mean) +
                        (n > 1 ? kMergeUs + kMergeMbUs * n * part_bytes * 1e-6 : 0.0);
       if (t < best * 0.999) {

@@ -270,8 +270,9 @@ def test_no_rows(hippo):
     assert (out == 0).all() and (lse == -float("inf")).all()
 
 
-@pytest.mark.parametrize("dtype,heads,least", [("bf16", (28, 4, 128), 1), ("bf16", (14, 2, 64), 1), ("fp32", (4, 2, 64), 1), ("fp32", (28, 4, 128), 2)])
-def test_every_tile_size(hippo, kernels, dtype, heads, least):
+@pytest.mark.parametrize("dtype,heads,blocks", [("bf16", (28, 4, 128), {2, 4}), ("bf16", (14, 2, 64), {1, 2, 4}), ("fp32", (4, 2, 64), {1, 2, 4}),
+                                                ("fp32", (28, 4, 128), {2, 4})])
+def test_every_tile_size(hippo, kernels, dtype, heads, blocks):
     """few and many rows, so that each size of a block is taken, over lengths that end around its stages: none, one and several that need
     no mask"""
     H, Hkv, d = heads
@@ -298,12 +299,20 @@ def test_every_tile_size(hippo, kernels, dtype, heads, least):
                 q2, k2, v2 = (torch.cat([x[first], x[n:-n], x[first]]) for x in (q, k, v))
                 again = hippo.hippo_prefill_attention(q2, k2, v2, cu)
                 assert torch.equal(again[first], again[last])
-    assert {rb for rb, _ in sizes} >= {1, 2, 4} - ({1} if least == 2 else set()), sizes
-    assert ((4, 1) in sizes) == (least == 1), sizes
+    assert {rb for rb, _ in sizes} >= blocks, sizes
+    assert ((4, 1) in sizes) == (heads[2] == 64 or dtype == "bf16"), sizes
+
+
+def test_few_rows_over_longer_keys(hippo, kernels):
+    q, k, v = make([64], [364], 64, 8, 128, "bf16", 62)
+    cu_q, cu_k = offsets([64]), offsets([364])
+    call = lambda: hippo.hippo_prefill_attention(q, k, v, cu_q, cu_k, want_lse=True)      # noqa: E731
+    verify(call(), reference(q, k, v, [64], [364]))
+    assert {name.split("attn_rows")[1].split("ELi")[1] for name in kernels(call) if "attn_rows" in name} == {"1"}
 
 
 @pytest.mark.parametrize("dtype,heads,lens,block", [
-    ("bf16", (28, 4, 128), [2500, 2561], (8, 1)), ("bf16", (14, 2, 64), [8191], (8, 1)), ("fp32", (28, 4, 128), [700] * 8, (8, 1)),
+    ("bf16", (28, 4, 128), [4200], (8, 1)), ("bf16", (14, 2, 64), [8191], (8, 1)), ("fp32", (28, 4, 128), [700] * 8, (8, 1)),
     ("bf16", (28, 4, 128), [2049], (4, 2)), ("bf16", (14, 2, 64), [4500], (4, 2)), ("fp32", (28, 4, 64), [2500], (4, 2)),
     ("bf16", (14, 2, 64), [1500] * 9, (4, 1)), ("bf16", (28, 4, 128), [511] * 60, (4, 1)), ("fp32", (8, 2, 64), [900] * 40, (4, 1))])
 def test_longer_prompts_of_every_block(hippo, kernels, dtype, heads, lens, block):
