@@ -15,8 +15,8 @@
 // tg TW .. tg TW + TW - 1; the TG states of a row block meet in the LDS at the end.  K and V reach the LDS without registers in between,
 // NST stages deep.  A sequence's stages may be dealt to S blocks (few rows over many tokens): their states go to a merge.
 //
-// What bounds it: long prompts and wide trees the matrix unit, at the clock that its power leaves (16640 rows x 28 heads x 128: 1716 us,
-// 1.17 PFLOP/s, where a library product of 16384^3 reaches 1.35); few rows the cache's bytes (16 nodes x 28 heads over 16640 rows: 18 us for
+// What bounds it: long prompts and wide trees the matrix unit, at the clock that its power leaves (16640 rows x 28 heads x 128: 1716 to 1749 us,
+// 1.15 PFLOP/s, where a library product of 16384^3 reaches 1.35); few rows the cache's bytes (16 nodes x 28 heads over 16640 rows: 18 us for
 // 34 MB) and the merge's launch; short prompts a chain of trips to memory of some 4 us, beside which other blocks should run.
 #pragma once
 
