@@ -559,7 +559,7 @@ int hippo_tree_attention_paged(const void* q, int32_t n_nodes, const void* k_poo
  *   Both are -1 from cu_q_out[batch] on, and a slot is where its page is none of the pool's.
  * n_free_out [1]: how many pages are free then.  free_pages [n_pool_pages] and block_table [batch, max_pages] are written in place:
  * new entries only, those given back stay where they stood.  (So a call may be repeated: as long as n_free and the lengths are
- * the old ones it finds the same.)  ctx_lens, new_lens and n_free may not be outputs at the same time.
+ * the old ones it finds the same.)  ctx_lens, new_lens and n_free may not share memory with anything that is written (BAD_SHAPE).
  * Negative ctx_lens count as 0, n_free as at most n_pool_pages.  page_size a power of two, 16..256; batch <= 4096; max_tokens,
  * n_pool_pages and max_pages <= 2^22, batch * max_pages <= 2^30.  Deterministic.
  * Errors: NULL_ARG, BAD_SHAPE, BAD_ALIGN, HIP.

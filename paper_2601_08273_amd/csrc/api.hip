@@ -1243,11 +1243,18 @@ int hippo_plan_pages(const int32_t* ctx_lens, const int32_t* new_lens, int32_t b
   const void* all[] = {ctx_lens, new_lens, block_table, free_pages, n_free, slots_out, positions_out, cu_q_out, kv_lens_out, n_free_out};
   for (const void* x : all)
     if (!aligned4(x)) return HIPPO_ERR_BAD_ALIGN;
-  // every block reads the lengths and the stack's height while the first one writes the new ones
-  for (const void* in : {(const void*)ctx_lens, (const void*)new_lens, (const void*)n_free})
-    for (const void* o : {(const void*)slots_out, (const void*)positions_out, (const void*)cu_q_out, (const void*)kv_lens_out,
-                          (const void*)n_free_out})
-      if (in == o) return HIPPO_ERR_BAD_SHAPE;
+  // Every block reads the lengths and the stack's height, some of them again for each item, while others write: an input that reached into
+  // what is written would change under them, and with it the places that they look up in the table.
+  struct Span {
+    const void* first;
+    long long n;
+  };
+  for (const Span& in : {Span{ctx_lens, batch}, Span{new_lens, batch}, Span{n_free, 1}})
+    for (const Span& o : {Span{block_table, (long long)batch * max_pages}, Span{free_pages, n_pool_pages}, Span{slots_out, max_tokens},
+                          Span{positions_out, max_tokens}, Span{cu_q_out, batch + 1}, Span{kv_lens_out, batch}, Span{n_free_out, 1}}) {
+      const uintptr_t a = reinterpret_cast<uintptr_t>(in.first), b = reinterpret_cast<uintptr_t>(o.first);
+      if (a < b + o.n * sizeof(int32_t) && b < a + in.n * sizeof(int32_t) && o.n > 0) return HIPPO_ERR_BAD_SHAPE;
+    }
   PlanParams p;
   p.ctx_lens = ctx_lens; p.new_lens = new_lens; p.block_table = block_table; p.free_pages = free_pages; p.n_free = n_free;
   p.n_free_out = n_free_out; p.slots = slots_out; p.positions = positions_out; p.cu_q = cu_q_out; p.kv_lens = kv_lens_out;

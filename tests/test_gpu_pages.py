@@ -123,6 +123,27 @@ def test_a_step_may_be_repeated(hippo):
     assert all(torch.equal(a, b) for a, b in zip(first, again))
 
 
+def test_inputs_beside_outputs(hippo):
+    """all of a plan in one buffer, an input next to an output everywhere"""
+    B, columns, n_pool, most, page = 3, 4, 9, 40, 16
+    ctx, new, n_free = [20, 5, 40], [15, 30, -10], 4
+    table = [[8, 7, -1, -1], [6, -1, -1, -1], [5, 4, 3, -1]]
+    free = [0, 1, 2, 5, -1, -1, -1, -1, -1]
+    sizes = [("table", B * columns), ("ctx", B), ("slots", most), ("new", B), ("free", n_pool), ("n_free", 1), ("cu_q", B + 1), ("positions", most),
+             ("kv_lens", B), ("left", 1)]
+    whole, at, part = torch.full((sum(n for _, n in sizes),), -7, dtype=torch.int32, device="cuda"), 0, {}
+    for name, n in sizes:
+        part[name], at = whole[at:at + n], at + n
+    for name, x in (("table", sum(table, [])), ("ctx", ctx), ("new", new), ("free", free), ("n_free", [n_free])):
+        part[name].copy_(int32(x))
+    part["table"] = part["table"].view(B, columns)
+    hippo.hippo_plan_pages(part["ctx"], part["new"], part["table"], part["free"], part["n_free"], page, most, slots_out=part["slots"],
+                           positions_out=part["positions"], cu_q_out=part["cu_q"], kv_lens_out=part["kv_lens"], n_free_out=part["left"])
+    want = plan(ctx, new, np.array(table), np.array(free), n_free, page, most)
+    compare(dict(part, n_free=part["left"]), want)
+    assert part["ctx"].tolist() == ctx and part["new"].tolist() == new and part["n_free"].tolist() == [n_free]
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("Hkv,d,page", [(1, 64, 16), (2, 64, 32), (4, 128, 16), (8, 128, 256), (3, 64, 64)])
 @pytest.mark.parametrize("T", [0, 1, 3, 4, 5, 333])

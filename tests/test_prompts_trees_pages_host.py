@@ -118,6 +118,17 @@ def test_arguments_are_checked(call, bad, status):
     assert call(**bad) == status
 
 
+# batch 5: five lengths of 4 bytes each, 50 numbers of the table, 50 free pages, 100 slots and positions, six offsets
+@pytest.mark.parametrize("bad", [
+    dict(lens=FAKE + 16), dict(lens=2 * FAKE - 4), dict(left=FAKE + 16), dict(left=2 * FAKE + 4), dict(cu=5 * FAKE - 20), dict(slots=FAKE - 396),
+    dict(slots=2 * FAKE + 16), dict(positions=5 * FAKE - 200), dict(table=FAKE - 196), dict(table=5 * FAKE - 100), dict(free=2 * FAKE - 4),
+    dict(free=5 * FAKE), dict(n_free=4 * FAKE + 196), dict(ctx=9 * FAKE + 16), dict(new=3 * FAKE + 40),
+])
+def test_inputs_of_a_plan_that_reach_into_its_outputs_are_refused(bad):
+    """blocks that read them again would find other numbers than before, and take them for places in the table"""
+    assert plan(**bad) == h.ERR_BAD_SHAPE
+
+
 def test_calls_with_nothing_to_do():
     assert prefill(n_q=0, q=None, k=None, v=None, out=None, ws=None, cu_q=None, cu_k=None) == h.OK
     assert write(tokens=0, k=None, v=None, slots=None) == h.OK and write(rows=0, k=None, v=None) == h.OK
