@@ -910,8 +910,9 @@ __global__ __launch_bounds__(64) void rows_combine(RowsParams p) {
     }
 #pragma unroll
     for (int u = 0; u < PF; ++u) {
-      const float f = __shfl(w, s0 + u * GROUPS + g);       // (0 behind the last split: its lane has no maximum)
-      if (s0 + u * GROUPS + g < n_split && f != 0.f) o += f * now[u];
+      const float f = __shfl(w, s0 + u * GROUPS + g);
+      // (a part of weight 0, too: as 0 times infinity its infinities are seen here as they are inside a block)
+      if (s0 + u * GROUPS + g < n_split) o += f * now[u];
     }
   }
 #pragma unroll

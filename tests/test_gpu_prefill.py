@@ -146,6 +146,23 @@ def test_infinite_values_that_are_seen(hippo, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("splits", [0, 1, 2, 4, 31])
+@pytest.mark.parametrize("low", [-400.0, -float("inf")])
+def test_infinite_values_of_no_weight_are_seen_however_the_keys_are_split(hippo, dtype, splits, low):
+    """the first 700 of 2000 keys get weights of exp(-1000) and less, 0 in fp32: 0 times infinity is no number, in whichever part it comes about"""
+    q, k, v = make([17], [2000], 4, 2, 64, dtype, 22)
+    q[..., 0], k[..., 0], k[:700, :, 0] = 20, 0, low
+    v[5, 0, 7], v[300, 1, 9], v[600, 1, 11] = float("inf"), -float("inf"), float("nan")
+    out = hippo.hippo_prefill_attention(q, k, v, offsets([17]), offsets([2000]), num_splits=splits).float()
+    finite = torch.ones_like(out, dtype=torch.bool)
+    finite[:, :2, 7] = finite[:, 2:, 9] = finite[:, 2:, 11] = False
+    assert bool((torch.isfinite(out) == finite).all())
+    v[5, 0, 7] = v[300, 1, 9] = v[600, 1, 11] = 0
+    ref = reference(q, k[700:], v[700:], [17], [1300])
+    check(out[finite], ref[0][finite], ref[1][finite])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("splits", [1, 4])
 def test_rows_of_no_sequence_stay(hippo, dtype, splits):
     lens = [40, 3, 100]
