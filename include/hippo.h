@@ -491,8 +491,9 @@ int hippo_token_logprobs(const void* logits, int32_t dtype, int64_t stride_row, 
  * 1/sqrt(d).  num_splits: blocks that share a tile of query rows (up to 64), 0 = library's choice; the result does not depend on it beyond
  * rounding.  fp32 throughout, but that over bf16 the probabilities are rounded to bf16 before their product with V (and summed as
  * rounded).  total_q = 0 does nothing.  Workspace: hippo_prefill_workspace_bytes with paged 0.
- * Errors: NULL_ARG, BAD_SHAPE (also more than 65535 sequences, 2^30 query rows times heads), BAD_DTYPE, BAD_ALIGN,
- *         WORKSPACE_TOO_SMALL, HIP.
+ * Errors: NULL_ARG, BAD_SHAPE (also more than 65535 sequences or query heads, 2^30 query rows times heads, 0x7fffff00 rows of K and V,
+ *         strides of their rows above 2^24 elements, or 2^23 blocks and more: (total_q * H / H_kv / 256 + n_seqs) * H_kv, in fp32 with
+ *         head_dim 64 total_q * H / H_kv / 128), BAD_DTYPE, BAD_ALIGN, WORKSPACE_TOO_SMALL, HIP.
  */
 typedef struct hippo_packed_desc {
   int32_t n_q_heads, n_kv_heads, head_dim, dtype;
@@ -532,7 +533,9 @@ int hippo_prefill_attention_paged(const void* q, int32_t total_q, int64_t q_stri
  * softmax_scale, num_splits, rounding, unseen rows as hippo_prefill_attention.  Workspace: hippo_tree_workspace_bytes.
  * The accepted path's rows are afterwards moved to ctx, ctx + 1, ...: over pages by hippo_plan_pages (which gives the tree's
  * rows back) and hippo_write_kv_paged (which picks rows).
- * Errors: NULL_ARG, BAD_SHAPE, BAD_DTYPE, BAD_ALIGN, WORKSPACE_TOO_SMALL, HIP.
+ * Errors: NULL_ARG, BAD_SHAPE (also more than 65535 sequences or KV heads, 4096 query heads to one of them, 2^30 nodes times query heads of the
+ *         batch, 0x7fffff00 rows, row strides above 2^24 elements, or 2^23 blocks and more: ceil(n_nodes * H / H_kv / 256) * batch * H_kv, in fp32 with
+ *         head_dim 64 / 128), BAD_DTYPE, BAD_ALIGN, WORKSPACE_TOO_SMALL, HIP.
  */
 size_t hippo_tree_workspace_bytes(const hippo_kv_desc* kv, int32_t n_nodes, int32_t seq_len, int32_t num_splits);
 int hippo_tree_attention(const void* q, int32_t n_nodes, const void* k_cache, const void* v_cache, const hippo_kv_desc* kv,

@@ -425,6 +425,22 @@ void cut_rows(RowsPlan* pl, int dtype, int head_dim, double rows, double n_seqs,
   pl->S = (int)std::max(1.0, std::min<double>(std::min(pl->S, kMaxRowSplits), (seen + 63) / 64));
 }
 
+// A launch numbers its threads along a dimension in 32 bits, and a block has up to 512.  What is too much for the block that was chosen by
+// time goes in larger ones: tiles(rows of a block) is how many a KV head has then.
+constexpr long long kMostBlocks = (1ll << 32) / 512 - 1;
+template <typename Tiles>
+bool fit_rows(RowsPlan* pl, int dtype, int head_dim, int Hkv, Tiles tiles) {
+  while (tiles(32 * pl->rb) * Hkv > kMostBlocks) {
+    int larger = -1;
+    for (int b = 0; b < 5; ++b)                               // (from the largest down)
+      if (kRowsBlocks[b].rb > pl->rb && !kRowsBlocks[b].pair && kRowsCost[0][dtype == HIPPO_DTYPE_BF16][head_dim == 128][b].pace != 0) larger = b;
+    if (larger < 0) return false;
+    pl->rb = kRowsBlocks[larger].rb;
+    pl->pair = false;
+  }
+  return true;
+}
+
 void carve_plan(RowsPlan* pl, int head_dim, long long tokens, int H) {
   if (tokens * H > (1 << 25)) pl->S = 1;                      // (the merge's launch: 64 threads a row and head, below 2^32)
   const size_t slots = pl->S > 1 ? (size_t)pl->S * tokens * H : 0;
@@ -457,9 +473,10 @@ int plan_prefill(const hippo_packed_desc* d, bool paged, int total_q, int total_
   cut_rows(pl, d->dtype, d->head_dim, len_q * G, std::min<double>(n_seqs, std::max(1, total_q)), seen, seen - len_q, false,
            d->n_kv_heads, (double)total_q * d->n_q_heads * d->head_dim * 4, num_splits);
   pl->deal = 0;
-  pl->n_tiles = (int)(rows / (32 * pl->rb) + n_seqs);
+  auto tiles = [&](int block) { return rows / block + n_seqs; };
+  if (!fit_rows(pl, d->dtype, d->head_dim, d->n_kv_heads, tiles)) return HIPPO_ERR_BAD_SHAPE;
+  pl->n_tiles = (int)tiles(32 * pl->rb);
   carve_plan(pl, d->head_dim, total_q, d->n_q_heads);
-  if ((long long)pl->n_tiles * d->n_kv_heads > (1 << 30) / 512) return HIPPO_ERR_BAD_SHAPE;
   return HIPPO_OK;
 }
 
@@ -471,9 +488,10 @@ int plan_tree(const hippo_kv_desc* kv, int nodes, long long seq_len, bool by_len
   const long long tokens = (long long)kv->batch * nodes;
   cut_rows(pl, kv->dtype, kv->head_dim, G * nodes, kv->batch, (double)seq_len, (double)seq_len, true, kv->n_kv_heads,
            (double)tokens * kv->n_q_heads * kv->head_dim * 4, num_splits);
-  const int per_seq = (G * nodes + 32 * pl->rb - 1) / (32 * pl->rb);
-  if ((long long)per_seq * kv->batch > (1 << 30)) return HIPPO_ERR_BAD_SHAPE;
-  pl->n_tiles = per_seq * kv->batch;
+  if (tokens * kv->n_q_heads > (1 << 30)) return HIPPO_ERR_BAD_SHAPE;
+  auto tiles = [&](int block) { return (long long)((G * nodes + block - 1) / block) * kv->batch; };
+  if (!fit_rows(pl, kv->dtype, kv->head_dim, kv->n_kv_heads, tiles)) return HIPPO_ERR_BAD_SHAPE;
+  pl->n_tiles = (int)tiles(32 * pl->rb);
   pl->deal = 0;
   if (pl->S > 1 && by_length && kv->batch > 1 && kv->batch <= 64) {
     pl->deal = pl->S * kv->batch;
@@ -481,8 +499,6 @@ int plan_tree(const hippo_kv_desc* kv, int nodes, long long seq_len, bool by_len
   }
   carve_plan(pl, kv->head_dim, tokens, kv->n_q_heads);
   if (pl->S == 1) pl->deal = 0;
-  if ((long long)pl->n_tiles * kv->n_kv_heads > (1 << 30) / 512 || (long long)kv->batch * nodes * kv->n_q_heads > (1 << 30))
-    return HIPPO_ERR_BAD_SHAPE;
   return HIPPO_OK;
 }
 

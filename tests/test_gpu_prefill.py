@@ -360,3 +360,11 @@ def test_two_calls_at_once(hippo):
     got = [[hippo.hippo_prefill_attention(*x, cu, num_splits=4, stream=s) for _ in range(5)] for x, s in zip((a, b), streams)]
     torch.cuda.synchronize()
     assert all(torch.equal(g, w) for gs, w in zip(got, want) for g in gs)
+
+
+def test_more_than_two_million_blocks(hippo):
+    """8300 sequences of one row, 256 heads: a row's only key has all the weight, and its row of V is the output, bit for bit"""
+    g = torch.Generator(device="cuda").manual_seed(63)
+    q, k, v = (rows(g, 8300, 256, 64, dtype="bf16") for _ in range(3))
+    out = hippo.hippo_prefill_attention(q, k, v, torch.arange(8301, dtype=torch.int32, device="cuda"))
+    assert torch.equal(out, v)

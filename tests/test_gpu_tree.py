@@ -252,3 +252,9 @@ def test_one_length_for_all_needs_no_tensor(hippo):
     ref = reference(q, k, v, [parents] * 3, [400] * 3)
     check(a, ref[0], ref[1])
     check(b, ref[0], ref[1])
+
+
+def test_more_than_two_million_blocks(hippo):
+    """65535 trees of one node without a context, 33 heads: its row of V is the output, bit for bit"""
+    q, k, v = make(65535, 1, 1, 33, 33, 64, "bf16", 16)
+    assert torch.equal(hippo.hippo_tree_attention(q, k, v, int32([-1]), 0)[:, 0], v[:, :, 0])

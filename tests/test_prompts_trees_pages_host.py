@@ -152,6 +152,35 @@ def test_workspace_sizes():
     assert need(None, 16, 2000, 0) == 0 and need(C.byref(kv), 0, 2000, 0) == 0 and need(C.byref(kv), 16, 15, 0) == 0
 
 
+@pytest.mark.parametrize("H,Hkv,d,dtype,total,seqs", [
+    (32, 32, 128, h.DTYPE_BF16, 65535, 65535), (32, 32, 128, h.DTYPE_BF16, 1 << 24, 1), (32, 32, 128, h.DTYPE_BF16, 1 << 23, 32768),
+    (32, 32, 128, h.DTYPE_BF16, 1 << 25, 65535), (64, 8, 64, h.DTYPE_BF16, 1 << 24, 65535), (16, 16, 64, h.DTYPE_F32, 1 << 25, 65535),
+    (1, 1, 128, h.DTYPE_F32, 1 << 30, 1), (120, 120, 64, h.DTYPE_BF16, 65535, 65535), (14, 2, 64, h.DTYPE_F32, 1 << 26, 5),
+])
+def test_as_many_rows_as_the_calls_take(H, Hkv, d, dtype, total, seqs):
+    """whatever block the library would choose by time: up to 2^30 rows times heads, 65535 sequences and 2^23 - 1 blocks of the largest size"""
+    need = h.load().hippo_prefill_workspace_bytes
+    desc = packed(n_q_heads=H, n_kv_heads=Hkv, head_dim=d, dtype=dtype, q_stride_n=H * d, q_stride_h=d, kv_stride_n=Hkv * d, kv_stride_h=d)
+    for paged, total_k, splits in ((0, total, 0), (0, total, 1), (0, total, 7), (1, 131072, 0)):
+        assert need(C.byref(desc), total, total_k, seqs, paged, splits) >= 256
+
+
+@pytest.mark.parametrize("B,H,Hkv,n,rows", [(65535, 32, 32, 1, 2000), (65535, 64, 64, 64, 64), (65535, 128, 32, 64, 1000), (65535, 100, 100, 1, 30000)])
+def test_as_many_trees_as_the_calls_take(B, H, Hkv, n, rows):
+    for dtype in (h.DTYPE_BF16, h.DTYPE_F32):
+        kv = cache(batch=B, n_q_heads=H, n_kv_heads=Hkv, dtype=dtype)
+        assert h.load().hippo_tree_workspace_bytes(C.byref(kv), n, rows, 0) >= 256
+
+
+def test_more_blocks_than_a_launch_has():
+    need = h.load().hippo_prefill_workspace_bytes
+    desc = packed(n_q_heads=256, n_kv_heads=256, q_stride_n=256 * 128, kv_stride_n=256 * 128)
+    assert need(C.byref(desc), 1, 1, 32767, 0, 0) >= 256                   # 32767 x 256 = 2^23 - 256 blocks
+    assert need(C.byref(desc), 1, 1, 32768, 0, 0) == 0
+    assert prefill(desc=desc, n_q=1, n_k=1, seqs=32768) == h.ERR_BAD_SHAPE
+    assert h.load().hippo_tree_workspace_bytes(C.byref(cache(batch=65535, n_q_heads=129, n_kv_heads=129)), 1, 100, 0) == 0
+
+
 def int32(*shape):
     return torch.zeros(shape, dtype=torch.int32)
 
