@@ -530,7 +530,8 @@ int hippo_prefill_attention_paged(const void* q, int32_t total_q, int64_t q_stri
  * [B] on the DEVICE: every sequence has its own length, and a captured graph follows them; cut off at seq_len - n_nodes), or ctx_len where
  * ctx_lens is NULL.  seq_len: rows that the cache has room for.  parents [B, n_nodes] int32 on the device, parents_stride_b
  * elements from one batch element to the next (0: one tree for all).  q, out [B, n_nodes, H, d] contiguous; lse_out optional [B, H, n_nodes].
- * softmax_scale, num_splits, rounding, unseen rows as hippo_prefill_attention.  Workspace: hippo_tree_workspace_bytes.
+ * softmax_scale, num_splits, rounding, unseen rows as hippo_prefill_attention.  Workspace: hippo_tree_workspace_bytes (which does not look at
+ * kv's strides).
  * The accepted path's rows are afterwards moved to ctx, ctx + 1, ...: over pages by hippo_plan_pages (which gives the tree's
  * rows back) and hippo_write_kv_paged (which picks rows).
  * Errors: NULL_ARG, BAD_SHAPE (also more than 65535 sequences or KV heads, 4096 query heads to one of them, 2^30 nodes times query heads of the
@@ -542,7 +543,7 @@ int hippo_tree_attention(const void* q, int32_t n_nodes, const void* k_cache, co
                          int32_t seq_len, const int32_t* parents, int64_t parents_stride_b,
                          const int32_t* ctx_lens, int32_t ctx_len, float softmax_scale, int32_t num_splits,
                          void* out, float* lse_out, void* workspace, size_t workspace_bytes, void* stream);
-/* over pages: seq_len = max_pages * page_size (in hippo_tree_workspace_bytes too, whose kv's strides are then not used) */
+/* over pages: seq_len = max_pages * page_size (in hippo_tree_workspace_bytes too) */
 int hippo_tree_attention_paged(const void* q, int32_t n_nodes, const void* k_pool, const void* v_pool, const int32_t* block_table,
                                const hippo_paged_kv_desc* kv, const int32_t* parents, int64_t parents_stride_b,
                                const int32_t* ctx_lens, int32_t ctx_len, float softmax_scale, int32_t num_splits,

@@ -19,7 +19,7 @@ inline int elem_bytes(int dtype) {
 }
 
 // allow_fp8: the call takes 8-bit caches (the fp8 attention calls, the gather, their workspace query)
-int check_kv(const hippo_kv_desc* kv, bool allow_fp8 = false) {
+int check_heads(const hippo_kv_desc* kv, bool allow_fp8) {
   if (kv == nullptr) return HIPPO_ERR_NULL_ARG;
   if (kv->dtype != HIPPO_DTYPE_F32 && kv->dtype != HIPPO_DTYPE_BF16 &&
       !(allow_fp8 && kv->dtype == HIPPO_DTYPE_FP8_E4M3))
@@ -27,9 +27,15 @@ int check_kv(const hippo_kv_desc* kv, bool allow_fp8 = false) {
   if (kv->batch < 1 || kv->n_kv_heads < 1 || kv->n_q_heads < 1) return HIPPO_ERR_BAD_SHAPE;
   if (kv->n_q_heads % kv->n_kv_heads != 0) return HIPPO_ERR_BAD_SHAPE;
   if (kv->head_dim != 64 && kv->head_dim != 128) return HIPPO_ERR_BAD_SHAPE;
+  if (kv->batch > 65535 || kv->n_kv_heads > 65535) return HIPPO_ERR_BAD_SHAPE;
+  return HIPPO_OK;
+}
+
+int check_kv(const hippo_kv_desc* kv, bool allow_fp8 = false) {
+  const int rc = check_heads(kv, allow_fp8);
+  if (rc != HIPPO_OK) return rc;
   if (kv->stride_n < kv->head_dim || kv->stride_h < 0 || kv->stride_b < 0) return HIPPO_ERR_BAD_SHAPE;
   if (kv->stride_n > (1ll << 24)) return HIPPO_ERR_BAD_SHAPE;   // row offsets inside a tile stay 32-bit
-  if (kv->batch > 65535 || kv->n_kv_heads > 65535) return HIPPO_ERR_BAD_SHAPE;
   const int per16 = 16 / elem_bytes(kv->dtype);
   if (kv->stride_n % per16 || kv->stride_h % per16 || kv->stride_b % per16) return HIPPO_ERR_BAD_ALIGN;
   return HIPPO_OK;
@@ -1184,7 +1190,7 @@ int hippo_prefill_attention_paged(const void* q, int32_t total_q, int64_t q_stri
 
 size_t hippo_tree_workspace_bytes(const hippo_kv_desc* kv, int32_t n_nodes, int32_t seq_len, int32_t num_splits) {
   RowsPlan pl;
-  if (check_kv(kv) != HIPPO_OK || plan_tree(kv, n_nodes, seq_len, true, num_splits, &pl) != HIPPO_OK) return 0;
+  if (check_heads(kv, false) != HIPPO_OK || plan_tree(kv, n_nodes, seq_len, true, num_splits, &pl) != HIPPO_OK) return 0;
   return pl.bytes;
 }
 

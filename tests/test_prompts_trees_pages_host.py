@@ -152,6 +152,19 @@ def test_workspace_sizes():
     assert need(None, 16, 2000, 0) == 0 and need(C.byref(kv), 0, 2000, 0) == 0 and need(C.byref(kv), 16, 15, 0) == 0
 
 
+@pytest.mark.parametrize("dtype", [h.DTYPE_BF16, h.DTYPE_F32])
+def test_the_workspace_of_trees_does_not_hang_on_strides(dtype):
+    """over pages there are none to give"""
+    need = h.load().hippo_tree_workspace_bytes
+    kv = cache(dtype=dtype)
+    none, odd = cache(dtype=dtype, stride_b=0, stride_h=0, stride_n=0), cache(dtype=dtype, stride_b=-1, stride_h=3, stride_n=1 << 30)
+    for splits in (0, 1, 9):
+        n = need(C.byref(kv), 16, 2000, splits)
+        assert n >= 256 and need(C.byref(none), 16, 2000, splits) == n and need(C.byref(odd), 16, 2000, splits) == n
+    for bad in (dict(batch=0), dict(n_q_heads=30), dict(head_dim=80), dict(dtype=h.DTYPE_FP8_E4M3), dict(n_kv_heads=0)):
+        assert need(C.byref(cache(**dict(dict(stride_b=0, stride_h=0, stride_n=0), **bad))), 16, 2000, 0) == 0
+
+
 @pytest.mark.parametrize("H,Hkv,d,dtype,total,seqs", [
     (32, 32, 128, h.DTYPE_BF16, 65535, 65535), (32, 32, 128, h.DTYPE_BF16, 1 << 24, 1), (32, 32, 128, h.DTYPE_BF16, 1 << 23, 32768),
     (32, 32, 128, h.DTYPE_BF16, 1 << 25, 65535), (64, 8, 64, h.DTYPE_BF16, 1 << 24, 65535), (16, 16, 64, h.DTYPE_F32, 1 << 25, 65535),
