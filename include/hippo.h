@@ -488,8 +488,8 @@ int hippo_token_logprobs(const void* logits, int32_t dtype, int64_t stride_row, 
  * query row does not see, infinities and NaN included, does not reach that row.
  * q [total_q, H, d], k and v [total_k, H_kv, d], with the strides of desc: slices of one fused projection's output will do.  out
  * [total_q, H, d] contiguous, dtype desc->dtype (F32 or BF16); lse_out optional [H, total_q] fp32.  softmax_scale <= 0 means
- * 1/sqrt(d).  num_splits: blocks that share a tile of query rows (up to 64), 0 = library's choice; the result does not depend on it beyond
- * rounding.  fp32 throughout, but that over bf16 the probabilities are rounded to bf16 before their product with V (and summed as
+ * 1/sqrt(d).  num_splits: blocks that share a tile of query rows (up to 64, and up to total_k / 64), 0 = library's choice; the result does not
+ * depend on it beyond rounding.  fp32 throughout, but that over bf16 the probabilities are rounded to bf16 before their product with V (and summed as
  * rounded).  total_q = 0 does nothing.  Workspace: hippo_prefill_workspace_bytes with paged 0.
  * Errors: NULL_ARG, BAD_SHAPE (also more than 65535 sequences or query heads, 2^30 query rows times heads, 0x7fffff00 rows of K and V,
  *         strides of their rows above 2^24 elements, or 2^23 blocks and more: (total_q * H / H_kv / 256 + n_seqs) * H_kv, in fp32 with
@@ -530,8 +530,8 @@ int hippo_prefill_attention_paged(const void* q, int32_t total_q, int64_t q_stri
  * [B] on the DEVICE: every sequence has its own length, and a captured graph follows them; cut off at seq_len - n_nodes), or ctx_len where
  * ctx_lens is NULL.  seq_len: rows that the cache has room for.  parents [B, n_nodes] int32 on the device, parents_stride_b
  * elements from one batch element to the next (0: one tree for all).  q, out [B, n_nodes, H, d] contiguous; lse_out optional [B, H, n_nodes].
- * softmax_scale, num_splits, rounding, unseen rows as hippo_prefill_attention.  Workspace: hippo_tree_workspace_bytes (which does not look at
- * kv's strides).
+ * softmax_scale, num_splits (up to seq_len / 64; of 2 to 64 sequences with ctx_lens the average: long ones get more, short ones fewer), rounding,
+ * unseen rows as hippo_prefill_attention.  Workspace: hippo_tree_workspace_bytes (which does not look at kv's strides).
  * The accepted path's rows are afterwards moved to ctx, ctx + 1, ...: over pages by hippo_plan_pages (which gives the tree's
  * rows back) and hippo_write_kv_paged (which picks rows).
  * Errors: NULL_ARG, BAD_SHAPE (also more than 65535 sequences or KV heads, 4096 query heads to one of them, 2^30 nodes times query heads of the

@@ -399,10 +399,11 @@ const RowsCost kRowsCost[2][2][2][5] = {      // [trees][bf16][head_dim 128], as
 //            the blocks' sizes are spread (short ones fill it up)
 //   blocks that share tiles: a merge, kMergeUs and kMergeMbUs for a megabyte of parts
 // rows: query rows of a KV head of one sequence, on average; seen, seen_least: the tokens that the last and the first of them see; tree:
-// a sequence's tiles are its own; num_splits: the caller's.
+// a sequence's tiles are its own; num_splits: the caller's, who may know that one of the sequences is much longer than the others: as many
+// blocks as `longest`, the most tokens that one can have, has stages for.
 constexpr double kMergeUs = 3.0, kMergeMbUs = 0.75;
-void cut_rows(RowsPlan* pl, int dtype, int head_dim, double rows, double n_seqs, double seen, double seen_least, bool tree, int Hkv,
-              double part_bytes, int num_splits) {
+void cut_rows(RowsPlan* pl, int dtype, int head_dim, double rows, double n_seqs, double seen, double seen_least, double longest, bool tree,
+              int Hkv, double part_bytes, int num_splits) {
   static const int splits[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64};
   double best = 1e30;
   for (int b = 0; b < 5; ++b) {
@@ -428,7 +429,7 @@ void cut_rows(RowsPlan* pl, int dtype, int head_dim, double rows, double n_seqs,
     }
   }
   if (num_splits > 0) pl->S = num_splits;
-  pl->S = (int)std::max(1.0, std::min<double>(std::min(pl->S, kMaxRowSplits), (seen + 63) / 64));
+  pl->S = (int)std::max(1.0, std::min<double>(std::min(pl->S, kMaxRowSplits), ((num_splits > 0 ? longest : seen) + 63) / 64));
 }
 
 // A launch numbers its threads along a dimension in 32 bits, and a block has up to 512.  What is too much for the block that was chosen by
@@ -476,8 +477,8 @@ int plan_prefill(const hippo_packed_desc* d, bool paged, int total_q, int total_
   if (rows > (1 << 30) || (long long)total_q * d->n_q_heads > (1 << 30) || total_k > 0x7fffff00) return HIPPO_ERR_BAD_SHAPE;
   // (the lengths are on the device: taken as equal, each seeing what is there beside the others)
   const double len_q = std::max(1.0, (double)total_q / n_seqs), seen = std::max(len_q, paged ? (double)total_k : (double)total_k / n_seqs);
-  cut_rows(pl, d->dtype, d->head_dim, len_q * G, std::min<double>(n_seqs, std::max(1, total_q)), seen, seen - len_q, false,
-           d->n_kv_heads, (double)total_q * d->n_q_heads * d->head_dim * 4, num_splits);
+  cut_rows(pl, d->dtype, d->head_dim, len_q * G, std::min<double>(n_seqs, std::max(1, total_q)), seen, seen - len_q, total_k,
+           false, d->n_kv_heads, (double)total_q * d->n_q_heads * d->head_dim * 4, num_splits);
   pl->deal = 0;
   auto tiles = [&](int block) { return rows / block + n_seqs; };
   if (!fit_rows(pl, d->dtype, d->head_dim, d->n_kv_heads, tiles)) return HIPPO_ERR_BAD_SHAPE;
@@ -492,8 +493,8 @@ int plan_tree(const hippo_kv_desc* kv, int nodes, long long seq_len, bool by_len
   const int G = kv->n_q_heads / kv->n_kv_heads;
   if (G > 4096) return HIPPO_ERR_BAD_SHAPE;
   const long long tokens = (long long)kv->batch * nodes;
-  cut_rows(pl, kv->dtype, kv->head_dim, G * nodes, kv->batch, (double)seq_len, (double)seq_len, true, kv->n_kv_heads,
-           (double)tokens * kv->n_q_heads * kv->head_dim * 4, num_splits);
+  cut_rows(pl, kv->dtype, kv->head_dim, G * nodes, kv->batch, (double)seq_len, (double)seq_len, (double)seq_len, true,
+           kv->n_kv_heads, (double)tokens * kv->n_q_heads * kv->head_dim * 4, num_splits);
   if (tokens * kv->n_q_heads > (1 << 30)) return HIPPO_ERR_BAD_SHAPE;
   auto tiles = [&](int block) { return (long long)((G * nodes + block - 1) / block) * kv->batch; };
   if (!fit_rows(pl, kv->dtype, kv->head_dim, kv->n_kv_heads, tiles)) return HIPPO_ERR_BAD_SHAPE;

@@ -368,3 +368,13 @@ def test_more_than_two_million_blocks(hippo):
     q, k, v = (rows(g, 8300, 256, 64, dtype="bf16") for _ in range(3))
     out = hippo.hippo_prefill_attention(q, k, v, torch.arange(8301, dtype=torch.int32, device="cuda"))
     assert torch.equal(out, v)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("splits", [0, 9, 64])
+def test_a_long_sequence_beside_short_ones(hippo, dtype, splits):
+    """the caller's number of blocks a tile, though most of the sequences have no stage for them"""
+    lens_q, lens_k = [110, 5, 329, 11], [128, 5, 912, 20011]
+    q, k, v = make(lens_q, lens_k, 4, 2, 64, dtype, 64)
+    got = hippo.hippo_prefill_attention(q, k, v, offsets(lens_q), offsets(lens_k), num_splits=splits, want_lse=True)
+    verify(got, reference(q, k, v, lens_q, lens_k))

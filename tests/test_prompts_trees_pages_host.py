@@ -152,6 +152,25 @@ def test_workspace_sizes():
     assert need(None, 16, 2000, 0) == 0 and need(C.byref(kv), 0, 2000, 0) == 0 and need(C.byref(kv), 16, 15, 0) == 0
 
 
+def parts(n_bytes, rows, H, d):
+    """how many parts of an output a workspace has room for"""
+    return n_bytes // (rows * H * (d + 2) * 4)
+
+
+def test_as_many_blocks_share_a_tile_as_the_caller_says():
+    """up to 64, as long as some sequence can have a stage of 64 tokens for each"""
+    need = h.load().hippo_prefill_workspace_bytes
+    d = packed()
+    # 60 short prompts beside a long one: 4300 rows of keys, 70 each on average
+    for total_k, splits, most in ((4300, 8, 8), (4300, 64, 64), (4300, 200, 64), (640, 64, 10), (641, 64, 11), (64, 5, 1), (0, 3, 1)):
+        n = need(C.byref(d), 600, total_k, 61, 0, splits)
+        assert parts(n, 600, 28, 128) == (most if most > 1 else 0), (total_k, splits)
+    assert parts(need(C.byref(d), 600, 1600, 61, 1, 64), 600, 28, 128) == 25
+    assert parts(need(C.byref(d), 600, 30, 61, 1, 64), 600, 28, 128) == 0
+    n = h.load().hippo_tree_workspace_bytes(C.byref(cache(batch=70)), 16, 2000, 20)
+    assert parts(n, 70 * 16, 28, 128) == 20
+
+
 @pytest.mark.parametrize("dtype", [h.DTYPE_BF16, h.DTYPE_F32])
 def test_the_workspace_of_trees_does_not_hang_on_strides(dtype):
     """over pages there are none to give"""
