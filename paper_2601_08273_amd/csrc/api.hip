@@ -510,7 +510,7 @@ int plan_tree(const hippo_kv_desc* kv, int nodes, long long seq_len, bool by_len
 }
 
 // A pool as the kernels take it: every element of a page lies inside the page's stride, so that a clamped page number keeps every
-// access inside the pool.
+// access inside the pool.  (The stride of a single page is nobody's.)
 int check_pool(const hippo_paged_kv_desc* pd) {
   if (pd == nullptr) return HIPPO_ERR_NULL_ARG;
   if (pd->dtype != HIPPO_DTYPE_F32 && pd->dtype != HIPPO_DTYPE_BF16) return HIPPO_ERR_BAD_DTYPE;
@@ -518,10 +518,11 @@ int check_pool(const hippo_paged_kv_desc* pd) {
   if (pd->page_size < 16 || pd->page_size > 256 || (pd->page_size & (pd->page_size - 1))) return HIPPO_ERR_BAD_SHAPE;
   if (pd->n_pool_pages < 1 || pd->n_pool_pages > kPlanMost) return HIPPO_ERR_BAD_SHAPE;
   if (pd->stride_n < pd->head_dim || pd->stride_n > (1ll << 24) || pd->stride_h < 0) return HIPPO_ERR_BAD_SHAPE;
-  if ((long long)(pd->page_size - 1) * pd->stride_n + (long long)(pd->n_kv_heads - 1) * pd->stride_h + pd->head_dim > pd->stride_page)
+  if (pd->n_pool_pages > 1 &&
+      (long long)(pd->page_size - 1) * pd->stride_n + (long long)(pd->n_kv_heads - 1) * pd->stride_h + pd->head_dim > pd->stride_page)
     return HIPPO_ERR_BAD_SHAPE;
   const int per16 = 16 / elem_bytes(pd->dtype);
-  if (pd->stride_n % per16 || pd->stride_h % per16 || pd->stride_page % per16) return HIPPO_ERR_BAD_ALIGN;
+  if (pd->stride_n % per16 || pd->stride_h % per16 || (pd->n_pool_pages > 1 && pd->stride_page % per16)) return HIPPO_ERR_BAD_ALIGN;
   return HIPPO_OK;
 }
 

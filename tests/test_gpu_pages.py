@@ -186,6 +186,25 @@ def test_pools_of_other_strides(hippo):
         assert torch.equal(pool[(slots // 16).long(), (slots % 16).long()], new)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_a_pool_of_one_page(hippo, dtype):
+    """heads first inside the page: the stride from page to page that a view of it has is shorter than a page"""
+    g = torch.Generator(device="cuda").manual_seed(23)
+    page, H, Hkv, d, n = 64, 8, 4, 64, 50
+    k_pool, v_pool = (torch.zeros((Hkv, page, d), dtype=TYPES[dtype], device="cuda").transpose(0, 1)[None] for _ in range(2))
+    k, v, q = rows(g, n, Hkv, d, dtype=dtype), rows(g, n, Hkv, d, dtype=dtype), rows(g, n, H, d, dtype=dtype)
+    hippo.hippo_write_kv_paged(k, v, torch.arange(n, dtype=torch.int32, device="cuda"), k_pool, v_pool)
+    assert torch.equal(k_pool[0, :n], k) and torch.equal(v_pool[0, :n], v) and not k_pool[0, n:].any()
+    table, cu = int32([[0]]), int32([0, n])
+    out = hippo.hippo_prefill_attention_paged(q, k_pool, v_pool, table, cu, int32([n]))
+    assert torch.equal(out, hippo.hippo_prefill_attention_paged(q, k_pool.contiguous(), v_pool.contiguous(), table, cu, int32([n])))
+    ref = prefill_reference(q, k, v, [n], [n])
+    check(out, ref[0], ref[1])
+    parents = int32([some_tree(10, 1)])
+    out = hippo.hippo_tree_attention_paged(q[None, :10], k_pool, v_pool, table, parents, n - 10)
+    assert torch.equal(out, hippo.hippo_tree_attention_paged(q[None, :10], k_pool.contiguous(), v_pool.contiguous(), table, parents, n - 10))
+
+
 def test_a_pool_beyond_32_bit_offsets(hippo):
     pool = [torch.zeros((70000 * 16, 16, 2, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)]     # 4.6 GB each
     g = torch.Generator(device="cuda").manual_seed(2)

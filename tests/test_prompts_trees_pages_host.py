@@ -134,6 +134,15 @@ def test_calls_with_nothing_to_do():
     assert write(tokens=0, k=None, v=None, slots=None) == h.OK and write(rows=0, k=None, v=None) == h.OK
 
 
+@pytest.mark.parametrize("stride", [0, 8184, 8196, -8])
+def test_the_page_stride_of_a_single_page_is_nobodys(stride):
+    one = pool(n_pool_pages=1, stride_page=stride)
+    assert write(tokens=0, kv=one) == h.OK
+    assert prefill_paged(n_q=0, kv=one) == h.OK and tree_paged(kv=one, ws_bytes=10) == SMALL
+    assert write(tokens=0, kv=pool(n_pool_pages=2, stride_page=stride)) in (SHAPE, ALIGN)
+    assert write(tokens=0, kv=pool(n_pool_pages=1, stride_page=stride, stride_h=64)) == SHAPE
+
+
 def test_workspace_sizes():
     need = h.load().hippo_prefill_workspace_bytes
     d = packed()
