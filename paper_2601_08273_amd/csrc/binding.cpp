@@ -151,6 +151,13 @@ hippo_kv_desc describe(const Tensor& cache, long long n_q_heads) {
   return d;
 }
 bool same_layout(const Tensor& a, const Tensor& b) { return a.sizes() == b.sizes() && a.strides() == b.strides(); }
+// (the stride of a single element is nobody's)
+bool same_strides(const Tensor& a, const Tensor& b) {
+  if (a.sizes() != b.sizes()) return false;
+  for (int64_t i = 0; i < a.dim(); ++i)
+    if (a.size(i) > 1 && a.stride(i) != b.stride(i)) return false;
+  return true;
+}
 
 template <typename T = void>
 T* ptr(const Tensor& t) { return t.defined() ? (T*)t.data_ptr() : nullptr; }
@@ -617,7 +624,7 @@ void require_int32(const Tensor& t, at::IntArrayRef sizes) {
 }
 // pools [n_pages, page_size, H_kv, d], any strides with unit stride on d
 hippo_paged_kv_desc describe_pool(const Tensor& k, const Tensor& v, long long batch, long long n_q_heads, long long max_pages) {
-  REQUIRE(k.dim() == 4 && k.stride(3) == 1 && same_layout(v, k) && v.scalar_type() == k.scalar_type());
+  REQUIRE(k.dim() == 4 && k.stride(3) == 1 && same_strides(v, k) && v.scalar_type() == k.scalar_type());
   hippo_paged_kv_desc pd;
   pd.batch = (int32_t)batch;
   pd.n_q_heads = (int32_t)n_q_heads;
@@ -644,7 +651,7 @@ PyObject* prefill(PyObject* const* a) {
   const float scale = scale_or_none(a[5]);
   const long long splits = integer(a[6]);
   for (const Tensor* t : {&q, &k, &v}) require_packed(*t);
-  REQUIRE(same_layout(v, k) && v.scalar_type() == k.scalar_type() && q.scalar_type() == k.scalar_type() && q.size(2) == k.size(2));
+  REQUIRE(same_strides(v, k) && v.scalar_type() == k.scalar_type() && q.scalar_type() == k.scalar_type() && q.size(2) == k.size(2));
   REQUIRE(cu_q.dim() == 1 && cu_q.size(0) >= 2 && splits >= 0 && splits <= 0x7fffffff);
   for (const Tensor* t : {&cu_q, &cu_k}) require_int32(*t, cu_q.sizes());
   REQUIRE(a[4] != Py_None || q.size(0) == k.size(0));          // whole prompts
@@ -815,7 +822,7 @@ PyObject* write_pages(PyObject* const* a) {
   const Tensor &k = tensor(a[0]), &v = tensor(a[1]), &slots = tensor(a[2]), &k_pool = tensor(a[3]), &v_pool = tensor(a[4]);
   const Tensor rows = tensor_or_none(a[5]);
   for (const Tensor* t : {&k, &v}) require_packed(*t);
-  REQUIRE(same_layout(v, k) && v.scalar_type() == k.scalar_type());
+  REQUIRE(same_strides(v, k) && v.scalar_type() == k.scalar_type());
   REQUIRE(slots.dim() == 1 && slots.size(0) <= 0x7fffffff);
   require_int32(slots, {slots.size(0)});
   if (rows.defined()) require_int32(rows, slots.sizes());

@@ -205,6 +205,26 @@ def test_a_pool_of_one_page(hippo, dtype):
     assert torch.equal(out, hippo.hippo_tree_attention_paged(q[None, :10], k_pool.contiguous(), v_pool.contiguous(), table, parents, n - 10))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_one_token_with_k_and_v_of_other_tensors(hippo, dtype):
+    """K as a kernel of its own wrote it, V a slice of the projection; then one KV head, whose tokens are as far apart in both"""
+    g = torch.Generator(device="cuda").manual_seed(24)
+    page, H, Hkv, d = 16, 8, 2, 64
+    k_pool, v_pool = (torch.zeros((3, page, Hkv, d), dtype=TYPES[dtype], device="cuda") for _ in range(2))
+    k, v = rows(g, 1, Hkv, d, dtype=dtype), rows(g, 1, H + 2 * Hkv, d, dtype=dtype)[:, H + Hkv:]
+    q = rows(g, 1, H, d, dtype=dtype)
+    hippo.hippo_write_kv_paged(k, v, int32([21]), k_pool, v_pool)
+    assert torch.equal(k_pool[1, 5], k[0]) and torch.equal(v_pool[1, 5], v[0])
+    assert not k_pool.flatten(0, 1)[torch.arange(48) != 21].any() and not v_pool.flatten(0, 1)[torch.arange(48) != 21].any()
+    out = hippo.hippo_prefill_attention(q, k, v, int32([0, 1]))
+    ref = prefill_reference(q, k, v, [1], [1])
+    check(out, ref[0], ref[1])
+    k, v, q = rows(g, 30, 1, d, dtype=dtype), rows(g, 1, 30, d, dtype=dtype).transpose(0, 1), rows(g, 30, H, d, dtype=dtype)
+    out = hippo.hippo_prefill_attention(q, k, v, int32([0, 30]))
+    ref = prefill_reference(q, k, v, [30], [30])
+    check(out, ref[0], ref[1])
+
+
 def test_a_pool_beyond_32_bit_offsets(hippo):
     pool = [torch.zeros((70000 * 16, 16, 2, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)]     # 4.6 GB each
     g = torch.Generator(device="cuda").manual_seed(2)

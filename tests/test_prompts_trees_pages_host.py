@@ -282,3 +282,24 @@ def test_tensors_have_to_lie_on_the_current_device():
                  lambda: h.hippo_plan_pages(lens, lens, table, int32(9), int32(1), 16, 8), lambda: h.hippo_write_kv_paged(k, k, int32(10), kp, kp)):
         with pytest.raises(AssertionError, match=re.escape("tensors lie on the current device")):
             call()
+
+
+def test_strides_of_single_elements_are_nobodys():
+    """a step of one token whose K came out of another kernel and whose V is still a slice of the projection; a single KV head; a single page"""
+    cu, slots, table, lens = int32(2), int32(1), int32(1, 3), int32(1)
+    q, fused = torch.zeros(1, 4, 64), torch.zeros(1, 8, 64)
+    k, v = torch.zeros(1, 2, 64), fused[:, 6:]
+    kp = torch.zeros(7, 16, 2, 64)
+    one, other = torch.zeros(10, 1, 64), torch.zeros(1, 10, 64).transpose(0, 1)
+    page, view = torch.zeros(1, 16, 2, 64), torch.zeros(3, 16, 2, 64)[::2][:1]
+    for call in (lambda: h.hippo_prefill_attention(q, k, v, cu), lambda: h.hippo_prefill_attention(q, k, v, cu, cu),
+                 lambda: h.hippo_write_kv_paged(k, v, slots, kp, kp),
+                 lambda: h.hippo_prefill_attention(torch.zeros(10, 4, 64), one, other, cu), lambda: h.hippo_prefill_attention(q, one, other, cu, cu),
+                 lambda: h.hippo_write_kv_paged(k, k, slots, page, view), lambda: h.hippo_prefill_attention_paged(q, page, view, table, cu, lens),
+                 lambda: h.hippo_tree_attention_paged(q[None], page, view, table, int32(1, 1), 3)):
+        with pytest.raises(AssertionError, match=re.escape("tensors lie on the current device")):
+            call()
+    for call in (lambda: h.hippo_prefill_attention(torch.zeros(2, 4, 64), torch.zeros(2, 2, 64), torch.zeros(2, 8, 64)[:, 6:], cu),
+                 lambda: h.hippo_write_kv_paged(k, k, slots, kp, torch.zeros(7, 16, 4, 64)[:, :, ::2])):
+        with pytest.raises(AssertionError, match="same_strides"):
+            call()
