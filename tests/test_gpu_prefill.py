@@ -378,3 +378,46 @@ def test_a_long_sequence_beside_short_ones(hippo, dtype, splits):
     q, k, v = make(lens_q, lens_k, 4, 2, 64, dtype, 64)
     got = hippo.hippo_prefill_attention(q, k, v, offsets(lens_q), offsets(lens_k), num_splits=splits, want_lse=True)
     verify(got, reference(q, k, v, lens_q, lens_k))
+
+
+def guarded_pools(g, n_pool, page, Hkv, d, dtype):
+    """pools in the middle of larger buffers whose other pages hold no numbers, and a table of pages and of numbers just past either end of
+    the pool with the pages that those are taken for"""
+    pools = []
+    for _ in range(2):
+        whole = torch.full((n_pool + 16, page, Hkv, d), float("nan"), dtype=TYPES[dtype], device="cuda")
+        whole[8:-8] = rows(g, n_pool, page, Hkv, d, dtype=dtype)
+        pools.append(whole[8:-8])
+    table = [[2, -1, n_pool, 1, n_pool + 7, 3], [-8, n_pool - 1, 0, n_pool + 1, -2, 2]]
+    return pools, table, [[min(max(x, 0), n_pool - 1) for x in t] for t in table]
+
+
+@pytest.mark.parametrize("dtype,heads", [("bf16", (28, 4, 128)), ("bf16", (14, 2, 64)), ("fp32", (8, 2, 128)), ("fp32", (4, 2, 64))])
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("splits", [1, 3])
+def test_numbers_that_are_no_pages_are_taken_for_the_pool_s_ends(hippo, dtype, heads, page, splits):
+    H, Hkv, d = heads
+    g = torch.Generator(device="cuda").manual_seed(65)
+    (k_pool, v_pool), table, taken = guarded_pools(g, 5, page, Hkv, d, dtype)
+    lens_q, lens_k = [40, 3], [6 * page - 5, 5 * page + 1]
+    q = rows(g, 43, H, d, dtype=dtype)
+    got = hippo.hippo_prefill_attention_paged(q, k_pool, v_pool, torch.tensor(table, dtype=torch.int32, device="cuda"), offsets(lens_q),
+                                              torch.tensor(lens_k, dtype=torch.int32, device="cuda"), num_splits=splits, want_lse=True)
+    k, v = (torch.cat([x[t].flatten(0, 1)[:n] for t, n in zip(taken, lens_k)]) for x in (k_pool, v_pool))
+    verify(got, reference(q, k, v, lens_q, lens_k))
+
+
+@pytest.mark.parametrize("dtype,heads", [("bf16", (28, 4, 128)), ("bf16", (14, 2, 64)), ("fp32", (8, 2, 128)), ("fp32", (4, 2, 64))])
+@pytest.mark.parametrize("lens_q,lens_k", [([1], [1]), ([300], [300]), ([90, 0, 7], [90, 40, 700])])
+def test_a_table_much_wider_than_the_lengths(hippo, dtype, heads, lens_q, lens_k):
+    """room for 131072 rows a sequence: most of the blocks that share a tile have no stage; what the unused columns hold is not looked at"""
+    H, Hkv, d = heads
+    q, k, v = make(lens_q, lens_k, H, Hkv, d, dtype, 66)
+    g = torch.Generator(device="cuda").manual_seed(67)
+    k_pool, v_pool, table = pages_of(g, k, v, lens_k, 16)
+    wide = torch.full((len(lens_k), 8192), -9, dtype=torch.int32, device="cuda")
+    wide[:, :table.shape[1]] = table
+    lens = torch.tensor(lens_k, dtype=torch.int32, device="cuda")
+    for splits in (0, 1, 64):
+        got = hippo.hippo_prefill_attention_paged(q, k_pool, v_pool, wide, offsets(lens_q), lens, num_splits=splits, want_lse=True)
+        verify(got, reference(q, k, v, lens_q, lens_k), "%d splits" % splits)

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from attention_reference import attend, check, check_lse
-from test_gpu_prefill import TYPES, pages_of, rows
+from test_gpu_prefill import TYPES, guarded_pools, pages_of, rows
 
 pytestmark = pytest.mark.gpu
 
@@ -258,3 +258,37 @@ def test_more_than_two_million_blocks(hippo):
     """65535 trees of one node without a context, 33 heads: its row of V is the output, bit for bit"""
     q, k, v = make(65535, 1, 1, 33, 33, 64, "bf16", 16)
     assert torch.equal(hippo.hippo_tree_attention(q, k, v, int32([-1]), 0)[:, 0], v[:, :, 0])
+
+
+@pytest.mark.parametrize("dtype,heads", [("bf16", (28, 4, 128)), ("bf16", (14, 2, 64)), ("fp32", (8, 2, 128)), ("fp32", (4, 2, 64))])
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("splits", [1, 3])
+def test_numbers_that_are_no_pages_are_taken_for_the_pool_s_ends(hippo, dtype, heads, page, splits):
+    H, Hkv, d = heads
+    g = torch.Generator(device="cuda").manual_seed(17)
+    (k_pool, v_pool), table, taken = guarded_pools(g, 5, page, Hkv, d, dtype)
+    n, ctx = 11, [6 * page - 11, 5 * page - 10]
+    q = rows(g, 2, n, H, d, dtype=dtype)
+    parents = [some_tree(n, b, padding=b) for b in range(2)]
+    got = hippo.hippo_tree_attention_paged(q, k_pool, v_pool, int32(table), int32(parents), int32(ctx), num_splits=splits, want_lse=True)
+    k, v = (torch.stack([x[t].flatten(0, 1).transpose(0, 1) for t in taken]) for x in (k_pool, v_pool))
+    verify(got, reference(q, k, v, parents, ctx))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("B", [1, 3, 65])
+def test_a_cache_with_much_more_room_than_rows(hippo, dtype, B):
+    """over pages, with a table of 131072 rows: one tree, a batch dealt by length, one dealt evenly"""
+    n, ctx = 6, [(37 * b) % 150 for b in range(B)]
+    q, k, v = make(B, n, max(ctx) + n, 4, 2, 64, dtype, 18)
+    lens = [c + n for c in ctx]
+    g = torch.Generator(device="cuda").manual_seed(19)
+    packed = [torch.cat([x[b, :, :m].transpose(0, 1) for b, m in enumerate(lens)]) for x in (k, v)]
+    k_pool, v_pool, table = pages_of(g, *packed, lens, 16)
+    wide = torch.full((B, 8192), -9, dtype=torch.int32, device="cuda")
+    wide[:, :table.shape[1]] = table
+    parents = [some_tree(n, b, padding=b % 3) for b in range(B)]
+    want = reference(q, k, v, parents, ctx)
+    for splits in (0, 1, 64):
+        got = hippo.hippo_tree_attention_paged(q, k_pool, v_pool, wide, int32(parents), int32(ctx), num_splits=splits, want_lse=True)
+        verify(got, want, "%d splits" % splits)
