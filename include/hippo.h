@@ -490,7 +490,9 @@ int hippo_token_logprobs(const void* logits, int32_t dtype, int64_t stride_row, 
  * [total_q, H, d] contiguous, dtype desc->dtype (F32 or BF16); lse_out optional [H, total_q] fp32.  softmax_scale <= 0 means
  * 1/sqrt(d).  num_splits: blocks that share a tile of query rows (up to 64, and up to total_k / 64), 0 = library's choice; the result does not
  * depend on it beyond rounding.  fp32 throughout, but that over bf16 the probabilities are rounded to bf16 before their product with V (and summed as
- * rounded).  total_q = 0 does nothing.  Workspace: hippo_prefill_workspace_bytes with paged 0.
+ * rounded: lse_out is within 2^-8 of the unrounded one's, and goes with out where outputs are joined by it).  total_q = 0 does nothing.
+ * Workspace: hippo_prefill_workspace_bytes with paged 0.  It holds the parts of tiles that blocks share, and may be larger for a smaller call, which
+ * needs more blocks a tile to fill the device: ask for each.  The lengths are on the device; the library's choice takes them as alike.
  * Errors: NULL_ARG, BAD_SHAPE (also more than 65535 sequences or query heads, 2^30 query rows times heads, 0x7fffff00 rows of K and V,
  *         strides of their rows above 2^24 elements, or 2^23 blocks and more: (total_q * H / H_kv / 256 + n_seqs) * H_kv, in fp32 with
  *         head_dim 64 total_q * H / H_kv / 128), BAD_DTYPE, BAD_ALIGN, WORKSPACE_TOO_SMALL, HIP.
@@ -512,6 +514,8 @@ int hippo_prefill_attention(const void* q, int32_t total_q, const void* k, const
  * The same over a paged cache (hippo_paged_kv_desc, with batch = n_seqs) that already holds the new rows: sequence b's key row n lies
  * where block_table says, and len_k = kv_lens[b] (int32 on the device, cut off at max_pages * page_size).  Pools of at most 2^22 pages, here and in
  * the tree's and the write's calls.  Workspace: hippo_prefill_workspace_bytes with total_k = max_pages * page_size and paged 1.
+ * num_splits 0 takes a row of the table as full: beside a table much wider than the lengths a tile gets blocks without work, whose parts take
+ * memory and are merged.  num_splits 1 has none.
  */
 int hippo_prefill_attention_paged(const void* q, int32_t total_q, int64_t q_stride_n, int64_t q_stride_h,
                                   const void* k_pool, const void* v_pool, const int32_t* block_table,
@@ -531,7 +535,7 @@ int hippo_prefill_attention_paged(const void* q, int32_t total_q, int64_t q_stri
  * ctx_lens is NULL.  seq_len: rows that the cache has room for.  parents [B, n_nodes] int32 on the device, parents_stride_b
  * elements from one batch element to the next (0: one tree for all).  q, out [B, n_nodes, H, d] contiguous; lse_out optional [B, H, n_nodes].
  * softmax_scale, num_splits (up to seq_len / 64; of 2 to 64 sequences with ctx_lens the average: long ones get more, short ones fewer), rounding,
- * unseen rows as hippo_prefill_attention.  Workspace: hippo_tree_workspace_bytes (which does not look at kv's strides).
+ * lse, unseen rows as hippo_prefill_attention; num_splits 0 takes a cache of one or of more than 64 sequences as full.  Workspace: hippo_tree_workspace_bytes (which does not look at kv's strides).
  * The accepted path's rows are afterwards moved to ctx, ctx + 1, ...: over pages by hippo_plan_pages (which gives the tree's
  * rows back) and hippo_write_kv_paged (which picks rows).
  * Errors: NULL_ARG, BAD_SHAPE (also more than 65535 sequences or KV heads, 4096 query heads to one of them, 2^30 nodes times query heads of the
@@ -580,7 +584,8 @@ int hippo_plan_pages(const int32_t* ctx_lens, const int32_t* new_lens, int32_t b
  * k_new, v_new: element (row, hk, c) at row * stride_n + hk * stride_h + c, dtype kv->dtype (F32 or BF16); kv's batch, n_q_heads and
  * max_pages are not looked at.  slots, rows: int32 [n_tokens] on the device.  The pools must not overlap k_new, v_new or each
  * other.  n_tokens = 0 does nothing.
- * Errors: NULL_ARG, BAD_SHAPE (also a pool whose rows would meet), BAD_DTYPE, BAD_ALIGN, HIP.
+ * Errors: NULL_ARG, BAD_SHAPE (also a pool whose rows would meet, more than 2^31 pieces of 16 bytes in all or 2^20 a token, of K), BAD_DTYPE,
+ *         BAD_ALIGN, HIP.
  */
 int hippo_write_kv_paged(const void* k_new, const void* v_new, int32_t n_rows, int64_t stride_n, int64_t stride_h,
                          const int32_t* slots, const int32_t* rows, int32_t n_tokens,

@@ -433,14 +433,16 @@ def hippo_prefill_attention(q, k, v, cu_q, cu_k=None, softmax_scale: float = 0.0
                             out=None, workspace=None, stream=None):
     """Causal attention of packed prompts: q [T,H,d], k / v [T,Hkv,d] (slices of one fused projection's output will do), cu_q
     [n_seqs+1] int32 on the device, the sequences' offsets -> out [T,H,d] (and lse [H,T] fp32).  cu_k: offsets of longer key
-    sequences (k / v [Tk,Hkv,d]) whose last rows the queries are.  Rows of `out` that belong to no sequence stay as they were."""
+    sequences (k / v [Tk,Hkv,d]) whose last rows the queries are.  k and v have the same strides.  Rows of `out` that belong to no
+    sequence stay as they were."""
     return _call(stream, (_native or _bound()).prefill, q, k, v, cu_q, cu_k, softmax_scale, num_splits, want_lse, out, workspace)
 
 
 def hippo_prefill_attention_paged(q, k_pool, v_pool, block_table, cu_q, kv_lens, softmax_scale: float = 0.0, num_splits: int = 0,
                                   want_lse: bool = False, out=None, workspace=None, stream=None):
     """The same over pools [n_pages, page_size, Hkv, d] that hold the new rows already: block_table [n_seqs, max_pages], cu_q
-    [n_seqs+1], kv_lens [n_seqs] (rows of each sequence, the new ones included), all int32 on the device."""
+    [n_seqs+1], kv_lens [n_seqs] (rows of each sequence, the new ones included), all int32 on the device.  With a table much wider
+    than the lengths num_splits=1 saves workspace and time: the library's choice takes the table as full."""
     return _call(stream, (_native or _bound()).prefill_paged, q, k_pool, v_pool, block_table, cu_q, kv_lens, softmax_scale, num_splits,
                  want_lse, out, workspace)
 
@@ -472,8 +474,8 @@ def hippo_plan_pages(ctx_lens, new_lens, block_table, free_pages, n_free, page_s
 
 
 def hippo_write_kv_paged(k_new, v_new, slots, k_pool, v_pool, rows=None, stream=None) -> None:
-    """k_new / v_new [T,Hkv,d] into the pools [n_pages, page_size, Hkv, d]: row t (rows[t] where `rows` is given) to slot slots[t];
-    tokens with a slot or row of -1 are skipped."""
+    """k_new / v_new [T,Hkv,d] (of the same strides) into the pools [n_pages, page_size, Hkv, d]: row t (rows[t] where `rows` is given)
+    to slot slots[t]; tokens with a slot or row of -1 are skipped."""
     return _call(stream, (_native or _bound()).write_pages, k_new, v_new, slots, k_pool, v_pool, rows)
 
 

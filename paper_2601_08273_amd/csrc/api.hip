@@ -380,8 +380,10 @@ const RowsBlock kRowsBlocks[] = {{8, false}, {4, false}, {4, true}, {2, false}, 
 // What a block takes, in us: `fixed` (its start, its masked stages and its end) and `pace` for 64 tokens; beside another one on its compute unit,
 // where it leaves room for one (pace_beside 0: it does not).  Pace 0: there is no such block (fp32 x 64: pairs take 4 to 40 % less than 256
 // rows a block).  bf16: fitted to 492 calls of prompts (1 to 200 of 4 to 16384 rows, 1 to 4096 over up to 30000) and 112 of trees (1 to 128 of
-// 1 to 64 nodes over 30 to 30000 rows), each timed with every block and, trees, 1 to 48 blocks a tile: what this chooses takes 1 to
-// 2 % more than the best.  fp32: 64 nodes over 16640 rows of 28 x 128, 16 over 2000 of 14 x 64, prompts of 32 to 16384 rows.
+// 1 to 64 nodes over 30 to 30000 rows), each timed with every block and, trees, 1 to 48 blocks a tile, by random steps that lower the mean
+// logarithm of (time of the block that this chooses) / (least time): 1.2 and 2.2 % (prompts, 64 and 128 channels), 2.7 and 2.2 % (trees), at
+// worst 44 %.  The times are in profiles/rows_blocks_timings.txt; caches and tables with much more room than rows are not among them.
+// fp32: from 64 nodes over 16640 rows of 28 x 128, 16 over 2000 of 14 x 64, prompts of 32 to 16384 rows.
 struct RowsCost {
   double fixed, pace, fixed_beside, pace_beside;
 };

@@ -8,16 +8,18 @@
 //   S^T = K Q^T      A = 32 tokens of K, B = 32 query rows: lane (j = lane % 32, h = lane / 32) gets query row j's logits of tokens
 //                    8 (e / 4) + 4 h + e % 4 of the block, e = 0..15
 //   O^T = V^T P^T    B = those same registers (the order of the tokens in a contraction is free), A = V^T by transposing LDS reads
-//   softmax          one pass, with a running maximum and sum per row; a row's tokens lie in lanes j and j + 32, so one exchange of the
-//                    wave's halves completes a maximum
+//   softmax          one pass, with a running maximum and sum per row (the online softmax of Milakov and Gimelshein, 2018; its lazy form, in which
+//                    the reference follows only a rise beyond a threshold, is published, too); a row's tokens lie in lanes j and j + 32,
+//                    so one exchange of the wave's halves completes a maximum
 //
 // A block has RB x TG waves: wave (rb, tg) owns rows 32 rb .. 32 rb + 31 of the block's tile and of every stage tokens
 // tg TW .. tg TW + TW - 1; the TG states of a row block meet in the LDS at the end.  K and V reach the LDS without registers in between,
 // NST stages deep.  A sequence's stages may be dealt to S blocks (few rows over many tokens): their states go to a merge.
 //
 // What bounds it: long prompts and wide trees the matrix unit, at the clock that its power leaves (16640 rows x 28 heads x 128: 1716 to 1749 us,
-// 1.15 PFLOP/s, where a library product of 16384^3 reaches 1.35); few rows the cache's bytes (16 nodes x 28 heads over 16640 rows: 18 us for
-// 34 MB) and the merge's launch; short prompts a chain of trips to memory of some 4 us, beside which other blocks should run.
+// 1.15 PFLOP/s, where a library product of 16384^3 reaches 1.35); few rows over a long cache a block's start, its stages one behind the
+// other and the merge's launch (16 nodes x 28 heads over 16640 rows: 128 blocks of eight or nine stages, 18 us for 34 MB, of which the bytes alone
+// would be 5); short prompts a chain of trips to memory of some 4 us, beside which other blocks should run.
 #pragma once
 
 #include <type_traits>
